@@ -1,0 +1,122 @@
+// Types and launchers of the backend operators (internal to the library).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/wwws_backend.h"
+
+namespace wwws {
+
+// Kinds of device-side problems, kept as a bit mask in the workspace's error word.
+enum BackendError : uint32_t { bePage = 1, beToken = 2, beMask = 4, beOffset = 8 };
+
+struct SeqBatch {
+    const int32_t* q_start; const int32_t* kv_len; const int32_t* page_table;
+    uint32_t n_seqs, n_tokens, max_q_len, max_kv_len, table_stride;
+};
+
+struct Pages {
+    uint8_t* k; uint8_t* v; float* k_scale; float* v_scale;
+    uint32_t n_pages, n_kv_heads, page_shift;
+};
+
+// A partial attention result: running maximum, sum and weighted values of one row (see kernels_attend.cu).
+struct AttendScratch {
+    float* part_o;       // [slots][rows][head_dim]
+    float2* part_ml;     // [slots][rows]
+    uint32_t* ticket;    // [slots], zero between calls
+};
+
+struct AttendArgs {
+    SeqBatch b; Pages p; AttendScratch s;
+    const uint8_t* q; uint8_t* out; uint64_t q_stride, out_stride;   // strides in elements
+    uint32_t group;      // query heads per kv head
+    float scale_log2;    // softmax scale * log2(e)
+    uint32_t window, sinks;
+    uint32_t* err;
+};
+
+struct ShapeArgs {
+    wwws_shaping s;
+    const uint8_t* in; uint8_t* out; uint64_t in_stride, out_stride;
+    uint32_t n_rows, vocab, slice, n_slices;
+    int32_t* token; unsigned long long* best; uint32_t* ticket;     // best, ticket: [n_rows], zero between calls
+    uint32_t* err;
+};
+
+constexpr uint32_t kDecodeSlots = 2 * 148 * 4;      // partial results of the row kernel: two per block of its largest grid
+constexpr uint32_t kDecodeRows = 16;
+
+cudaError_t launch_cache_append(const SeqBatch& b, const Pages& p, const void* k, uint64_t k_stride, const void* v, uint64_t v_stride,
+                                uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
+cudaError_t launch_cache_read(const SeqBatch& b, const Pages& p, const int32_t* row_start, uint64_t n_rows, void* k_out, void* v_out,
+                              uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
+cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
+cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s);
+uint32_t shape_slice(uint32_t n_rows, uint32_t vocab);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void report(uint32_t* err, uint32_t bit) { atomicOr(err, bit); }
+
+// The place of sequence i in the batch; false (and reported) when its offsets or lengths break the batch's bounds, and
+// the sequence is then skipped.
+__device__ __forceinline__ bool sequence(const SeqBatch& b, uint32_t i, int& q0, int& q_len, int& kv, uint32_t* err)
+{
+    q0 = b.q_start[i]; q_len = b.q_start[i + 1] - q0; kv = b.kv_len[i];
+    const bool ok = q0 >= 0 && q_len >= 0 && uint32_t(q_len) <= b.max_q_len && uint32_t(q0) + uint32_t(q_len) <= b.n_tokens &&
+                    kv >= 0 && uint32_t(kv) <= b.max_kv_len;
+    if (!ok) report(err, beOffset);
+    return ok;
+}
+
+// Two-element vectors of the activation type, and the float conversions the kernels need.
+template <bool BF> struct Act;
+template <> struct Act<true> {
+    using T = __nv_bfloat16;
+    static __device__ __forceinline__ float lo(uint32_t v) { return __uint_as_float(v << 16); }
+    static __device__ __forceinline__ float hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)   // a in the low half, both rounded to nearest even
+    {
+        uint32_t r; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a)); return r;
+    }
+};
+template <> struct Act<false> {
+    using T = __half;
+    static __device__ __forceinline__ float lo(uint32_t v) { return __half2float(__ushort_as_half(uint16_t(v))); }
+    static __device__ __forceinline__ float hi(uint32_t v) { return __half2float(__ushort_as_half(uint16_t(v >> 16))); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)
+    {
+        uint32_t r; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a)); return r;
+    }
+};
+
+// Cache codes -> two activation elements.  CACHE: wwws_cache_kind.  `pair` holds the two codes in bytes 0 and 1 ... see each.
+// int8 -> f16: 0x6400 | (code ^ 0x80) is 1024 + 128 + code, exact in f16, so one subtraction of 1152 leaves the code.
+// int8 -> bf16: bf16 has 7 fraction bits: 0x4300 | low 7 bits is 128 + low7; less 0x4300 | sign bit (128, or 256 when set).
+// e4m3 -> f16: the hardware conversion, exact.  e4m3 -> bf16: sign and the 7 exponent/fraction bits moved to bf16's fields read as
+// value * 2^-120 (exponent biases 7 and 127); the product with 2^120 is exact, subnormal codes included.
+template <bool BF, int CACHE> __device__ __forceinline__ uint32_t widen(uint32_t two)   // codes in bits 0-7 and 8-15
+{
+    if constexpr (CACHE == WWWS_CACHE_INT8) {
+        if constexpr (BF) {
+            const uint32_t u = __byte_perm(two, 0x43434343u, 0x4140);
+            uint32_t r; asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(u & 0xff7fff7fu), "r"(u & 0xff80ff80u)); return r;
+        } else {
+            const uint32_t u = __byte_perm(two ^ 0x8080u, 0x64646464u, 0x4140);
+            uint32_t r; asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(u), "r"(0x64806480u)); return r;
+        }
+    } else {
+        if constexpr (BF) {
+            const uint32_t u = __byte_perm(two, 0u, 0x1404);            // codes in the high byte of each half
+            const uint32_t w = (u & 0x80008000u) | ((u >> 4) & 0x07f007f0u);
+            uint32_t r; asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x7b807b80u)); return r;
+        } else {
+            uint32_t r; asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(uint16_t(two))); return r;
+        }
+    }
+}
+#endif
+
+}  // namespace wwws
