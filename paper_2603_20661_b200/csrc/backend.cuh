@@ -10,7 +10,7 @@
 namespace wwws {
 
 // Kinds of device-side problems, kept as a bit mask in the workspace's error word.
-enum BackendError : uint32_t { bePage = 1, beToken = 2, beMask = 4, beOffset = 8 };
+enum BackendError : uint32_t { bePage = 1, beToken = 2, beMask = 4, beOffset = 8, beTimeout = 16 };
 
 struct SeqBatch {
     const int32_t* q_start; const int32_t* kv_len; const int32_t* page_table;
@@ -22,7 +22,8 @@ struct Pages {
     uint32_t n_pages, n_kv_heads, page_shift;
 };
 
-// A partial attention result: running maximum, sum and weighted values of one row (see kernels_attend.cu).
+// Partial attention results (running maximum, sum and weighted values of a row) of the blocks that share a unit; the row kernel and the
+// tile kernel use the same memory, one after the other.
 struct AttendScratch {
     float* part_o;       // [slots][rows][head_dim]
     float2* part_ml;     // [slots][rows]
@@ -35,6 +36,7 @@ struct AttendArgs {
     uint32_t group;      // query heads per kv head
     float scale_log2;    // softmax scale * log2(e)
     uint32_t window, sinks;
+    uint32_t few_rows;   // sequences with at most this many rows per kv head (new tokens * group) go to the row kernel, others to the tile kernel
     uint32_t* err;
 };
 
@@ -48,12 +50,14 @@ struct ShapeArgs {
 
 constexpr uint32_t kDecodeSlots = 2 * 148 * 4;      // partial results of the row kernel: two per block of its largest grid
 constexpr uint32_t kDecodeRows = 16;
+constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 
 cudaError_t launch_cache_append(const SeqBatch& b, const Pages& p, const void* k, uint64_t k_stride, const void* v, uint64_t v_stride,
                                 uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
 cudaError_t launch_cache_read(const SeqBatch& b, const Pages& p, const int32_t* row_start, uint64_t n_rows, void* k_out, void* v_out,
                               uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
 cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
+cudaError_t launch_attend_tile(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s);
 uint32_t shape_slice(uint32_t n_rows, uint32_t vocab);
 

@@ -70,9 +70,10 @@ uint64_t carve(const wwws_backend_config& c, uint8_t* base, wwws_backend* b)
     uint8_t* err = take(256);
     uint8_t* best = take(8ull * c.max_rows);
     uint8_t* row_ticket = take(4ull * c.max_rows);
-    uint8_t* ticket = c.n_heads ? take(4ull * kDecodeSlots) : nullptr;
-    uint8_t* part_ml = c.n_heads ? take(8ull * kDecodeSlots * kDecodeRows) : nullptr;
-    uint8_t* part_o = c.n_heads ? take(4ull * kDecodeSlots * kDecodeRows * c.head_dim) : nullptr;
+    constexpr uint64_t kRowSlots = uint64_t(kDecodeSlots) * kDecodeRows, kTileRows = uint64_t(kTileSlots) * 256, rows = kRowSlots > kTileRows ? kRowSlots : kTileRows;
+    uint8_t* ticket = c.n_heads ? take(4ull * (kDecodeSlots > kTileSlots ? kDecodeSlots : kTileSlots)) : nullptr;
+    uint8_t* part_ml = c.n_heads ? take(8 * rows) : nullptr;
+    uint8_t* part_o = c.n_heads ? take(4 * rows * c.head_dim) : nullptr;
     if (b) {
         b->err = reinterpret_cast<uint32_t*>(err);
         b->best = reinterpret_cast<unsigned long long*>(best);
@@ -217,7 +218,15 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
     a.window = window < batch->max_kv_len ? window : 0;          // one that hides nothing is none
     a.sinks = sinks < batch->max_kv_len ? sinks : batch->max_kv_len;
     a.err = b->err;
-    return launched(b, launch_attend_rows(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend");
+    // Sequences go by their rows per kv head (new tokens * group): up to 16, one tile of the row kernel, are bound by the cache's bytes; above
+    // that the tile kernel's 128-row tiles.  Both run only where the host's counts allow both kinds.
+    a.few_rows = kDecodeRows;
+    const bool many = uint64_t(batch->max_q_len) * a.group > a.few_rows;
+    const bool few = !many || uint64_t(batch->n_tokens) != uint64_t(batch->n_seqs) * batch->max_q_len;
+    cudaError_t e = cudaSuccess;
+    if (many) e = launch_attend_tile(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+    if (e == cudaSuccess && few) e = launch_attend_rows(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+    return launched(b, e, "wwws_attend");
 }
 
 wwws_status wwws_shape_logits(wwws_backend* b, const wwws_shaping* s, uint32_t n_rows, uint32_t vocab, uint32_t dtype, const void* logits, uint64_t stride, void* out, uint64_t out_stride, int32_t* token)
@@ -259,6 +268,7 @@ wwws_status wwws_backend_sync(wwws_backend* b)
     if (bits & bePage) text += "a page id outside the pool; ";
     if (bits & beToken) text += "a token id outside the vocabulary; ";
     if (bits & beMask) text += "a mask index outside the masks; ";
+    if (bits & beTimeout) return fail(b, WWWS_ERR_TIMEOUT, "a wait inside wwws_attend ran out; its results are not to be trusted");
     if (bits & beOffset) text += "offsets or lengths outside the batch's bounds; ";
     return fail(b, bits & (bePage | beToken | beMask) ? WWWS_ERR_INDEX : WWWS_ERR_ARG, text + "what they named was skipped");
 }

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
         unsigned long long x = 0;
         if (base + tid < a.b.n_seqs) {
             int q0, q_len, kv;
-            if (sequence(a.b, base + tid, q0, q_len, kv, a.err) && q_len)
+            if (sequence(a.b, base + tid, q0, q_len, kv, a.err) && q_len && uint32_t(q_len) * G <= a.few_rows)
                 x = (unsigned long long)((uint32_t(q_len) * G + kDecodeRows - 1) / kDecodeRows) * span_of<TK>(q_len, kv, a.window, a.sinks).tiles;
         }
         const unsigned long long own = x;
@@ -249,7 +249,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
                 s[nt][0] *= f0; s[nt][1] *= f1; s[nt][2] *= f0; s[nt][3] *= f1;
             }
             // hidden keys, where the tile has any
-            if (key0 + TK - 1 > first_place || (a.window && key0 < last_place - int(a.window) + 1 && key0 + TK > int(a.sinks))) {
+            const bool masked = key0 + TK - 1 > first_place || (a.window && key0 < last_place - int(a.window) + 1 && key0 + TK > int(a.sinks));
+            if (masked) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -279,6 +280,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
                     const float2 v2 = *reinterpret_cast<const float2*>(scales + TK + nt * 8 + 2 * c);
                     const float f0 = v2.x * kLift, f1 = v2.y * kLift;
                     p0 *= f0; p1 *= f1; p2 *= f0; p3 *= f1;
+                    if (masked) {               // a hidden value's scale may be NaN
+                        p0 = s[nt][0] == -INFINITY ? 0.0f : p0; p1 = s[nt][1] == -INFINITY ? 0.0f : p1;
+                        p2 = s[nt][2] == -INFINITY ? 0.0f : p2; p3 = s[nt][3] == -INFINITY ? 0.0f : p3;
+                    }
                 }
                 pf[nt / 2][(nt & 1) * 2] = A::pack(p0, p1);
                 pf[nt / 2][(nt & 1) * 2 + 1] = A::pack(p2, p3);

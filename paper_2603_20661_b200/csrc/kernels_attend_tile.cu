@@ -1,0 +1,680 @@
+// Attention of many rows per kv head over the paged cache (chunks of prompts, whole prompts): tcgen05 tiles fed by TMA.
+//
+// A block works on 256 rows of one (sequence, kv head) at a time, as two tiles of 128: a row is a (new token, query head) pair,
+// the query heads of a kv head side by side, so every key tile serves all of them.  Per tile of 128 keys
+//     S = Q K^T            128 x 128 x head_dim into tensor memory, fp32
+//     P = 2^(x - m)        x = scale * log2(e) * S, one row per thread: running maximum and sum without any exchange between threads
+//     O = O + P V          P back into tensor memory over S, rounded to the activation type; O stays in tensor memory, fp32
+// One warp issues all matrix instructions in the order PV0 S0 PV1 S1: while the tensor cores work on one row tile, the four warps of the
+// other turn its S into P.  m is allowed to lag behind the true maximum by a factor 2^kLag, so that O is rescaled (a pass over
+// tensor memory) in the first few tiles only; the result is the same sum, since numerator and denominator share m.
+//   - Bound by the exponentials and the tensor cores about equally (head_dim 128: 2 x 16,384 exponentials at 16 a clock and
+//     4 x 128^3 multiply-adds, 2,048 clocks each per key tile).
+//   - Work is cut by key tiles, as in kernels_attend.cu: all (unit, tile) pairs laid end to end, an equal share for each of 148
+//     blocks, cut units joined by the last of their blocks.  The position of a share is found from closed sums (floor_sum), so
+//     causal triangles, windows and ragged lengths need no plan.
+//   - K and V tiles come by TMA page by page into the 128-byte-swizzled layout that the matrix instructions read; pages that no row
+//     sees are fetched from beyond the tensor's end, which fills zeros.
+//   - Quantised caches: codes land in a staging ring, four more warps widen them into the operand layout (exactly: 16-bit floats
+//     hold the codes); scales multiply the scores (keys) and the weights (values) in fp32.
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "backend.cuh"
+#include "tcgen.cuh"
+
+namespace wwws {
+namespace {
+
+constexpr int kBM = 128, kBN = 128;
+constexpr float kLow = -3.0e38f;
+
+template <bool BF, int CACHE, int D> struct Cfg {
+    static constexpr bool kQuant = CACHE != WWWS_CACHE_16;
+    static constexpr int kSlabs = D / 64;
+    static constexpr int kQ = kBM * D * 2;                  // one row tile of queries
+    static constexpr int kTile = kBN * D * 2;               // one operand tile of keys or values
+    static constexpr int kCodes = kBN * D;                  // the same as codes
+    static constexpr int kStages = kQuant ? (D == 128 ? 3 : 6) : (D == 128 ? 4 : 8);
+    static constexpr int kStaging = kQuant ? (D == 128 ? 3 : 6) : 0;
+    static constexpr int kScales = kQuant ? 4 * 2 * kBN * 4 : 0;            // four tiles' key and value scales
+    static constexpr int kOffRing = 2 * kQ;
+    static constexpr int kOffStaging = kOffRing + kStages * kTile;
+    static constexpr int kOffScales = kOffStaging + kStaging * kCodes;
+    static constexpr int kOffBars = kOffScales + kScales;
+    static constexpr int kSmem = kOffBars + 512 + 1024;                     // the rings start at a 1,024-byte boundary
+    static constexpr int kThreads = kQuant ? 448 : 320;
+    static constexpr int kWarpConvert = 8, kWarpMma = kQuant ? 12 : 8, kWarpLoad = kWarpMma + 1;
+    static constexpr float kLag = !BF && kQuant ? 3.0f : 8.0f;              // f16 weights: 2^lag * lift * 516 (largest value scale) < 65,504
+    static constexpr float kLift = !BF && kQuant ? 8.0f : 1.0f;
+    static constexpr uint32_t kColS = 0, kColO = 256, kCols = 512;
+};
+
+// ---- the linear space of (unit, kv head, key tile) ----
+
+__device__ __forceinline__ long long floor_sum(long long n, long long m, long long a, long long b)    // sum_{i<n} floor((a i + b) / m), a, b >= 0
+{
+    long long s = 0;
+    while (true) {        // Euclid's steps on (a, m), as in the published algorithm for lattice points under a line
+        if (a >= m) { s += (n - 1) * n / 2 * (a / m); a %= m; }
+        if (b >= m) { s += n * (b / m); b %= m; }
+        const long long y = a * n + b;
+        if (y < m) return s;
+        n = y / m; b = y % m;
+        const long long t = m; m = a; a = t;
+    }
+}
+
+struct Seq {
+    int q0, q_len, kv, place0, units;      // units: blocks of `step` tokens
+};
+struct Space {
+    int step;                              // tokens of a unit: two row tiles
+    int window, sink_tiles;
+    __device__ __forceinline__ void span(const Seq& s, int u, int& hi, int& lo, int& lo_tile, int& n_sink, int& tiles) const
+    {
+        hi = min(s.kv, s.place0 + min(s.q_len, (u + 1) * step));
+        lo = window ? max(0, s.place0 + u * step - window + 1) : 0;
+        if (hi <= 0) { hi = 0; lo = lo_tile = n_sink = 0; tiles = 1; return; }     // nothing seen: one empty tile, the rows get zeros
+        lo_tile = lo / kBN;
+        n_sink = min(sink_tiles, lo_tile);
+        tiles = n_sink + (hi + kBN - 1) / kBN - lo_tile;
+    }
+    // tiles of the first n units
+    __device__ long long sum(const Seq& s, int n) const
+    {
+        if (n <= 0) return 0;
+        long long total = 0;
+        int last = n;
+        if (n == s.units) { int hi, lo, lt, ns, t; span(s, n - 1, hi, lo, lt, ns, t); total += t; last = n - 1; }
+        if (last == 0) return total;
+        // units [0, last) are whole: their keys end at place0 + (u + 1) step
+        int first = 0;
+        if (s.place0 + step <= 0) first = min(last, (-s.place0) / step);           // units that see nothing: one tile each
+        total += first;
+        total += floor_sum(last - first, kBN, step, (long long)s.place0 + (long long)(first + 1) * step + kBN - 1);
+        if (window) {                                                              // less floor((place0 + u step - window + 1) / 128) - sink tiles, where positive
+            const long long b = (long long)s.place0 - window + 1 - (long long)sink_tiles * kBN;
+            long long u0 = b >= 0 ? 0 : (-b + step - 1) / step;
+            if (u0 < last) total -= floor_sum(last - u0, kBN, step, b + u0 * step);
+        }
+        return total;
+    }
+};
+
+struct Segment {
+    int q0, place0, q_len, kv;
+    int tok0;                  // first token of the unit within the sequence's new tokens
+    int h, t0, t1, tiles;
+    int hi, lo, lo_tile, n_sink;
+    uint32_t seq;
+    bool two;                  // the second row tile has tokens
+    __device__ __forceinline__ int tile_key(int t) const { return (t < n_sink ? t : lo_tile + t - n_sink) * kBN; }
+};
+
+// Walks a block's share [x, end); every role holds one.
+struct Walk {
+    long long x, end, base;    // base: linear position of (seq, unit)'s first tile
+    uint32_t i; int u;
+    Seq s; int tiles, hi, lo, lo_tile, n_sink;
+
+    __device__ __forceinline__ bool load(const AttendArgs& a, const Space& sp)
+    {
+        int q0, q_len, kv;
+        if (!sequence(a.b, i, q0, q_len, kv, a.err) || uint32_t(q_len) * a.group <= a.few_rows) { s.units = 0; return false; }
+        s = Seq{ q0, q_len, kv, kv - q_len, (q_len + sp.step - 1) / sp.step };
+        return true;
+    }
+    __device__ __forceinline__ void spans(const Space& sp) { sp.span(s, u, hi, lo, lo_tile, n_sink, tiles); }
+    __device__ __forceinline__ bool next(const AttendArgs& a, const Space& sp, Segment& g)
+    {
+        if (x >= end) return false;
+        const uint32_t Hkv = a.p.n_kv_heads;
+        while (x >= base + (long long)tiles * Hkv) {
+            base += (long long)tiles * Hkv;
+            if (++u >= s.units) {
+                u = 0;
+                do { ++i; } while (i < a.b.n_seqs && !load(a, sp));
+                if (i >= a.b.n_seqs) { x = end; return false; }
+            }
+            spans(sp);
+        }
+        const long long rel = x - base;
+        g.h = int(rel / tiles); g.t0 = int(rel % tiles);
+        g.t1 = int(min((long long)tiles, g.t0 + (end - x)));
+        g.tiles = tiles; g.hi = hi; g.lo = lo; g.lo_tile = lo_tile; g.n_sink = n_sink; g.seq = i;
+        g.q0 = s.q0; g.place0 = s.place0; g.q_len = s.q_len; g.kv = s.kv; g.tok0 = u * sp.step;
+        g.two = g.tok0 + sp.step / 2 < s.q_len;
+        x += g.t1 - g.t0;
+        return true;
+    }
+};
+
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+template <bool BF, int CACHE, int D>
+__global__ void __launch_bounds__(Cfg<BF, CACHE, D>::kThreads, 1)
+k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
+{
+    using C = Cfg<BF, CACHE, D>;
+    using A = Act<BF>;
+    constexpr bool kQuant = C::kQuant;
+    extern __shared__ uint8_t raw[];
+    uint8_t* smem = raw + ((1024 - (smem_at(raw) & 1023)) & 1023);
+    const uint32_t base = smem_at(smem);
+    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready / PV done per row tile, join
+    const uint32_t bars = base + C::kOffBars;
+    auto kv_full = [&](int s) { return bars + 8 * s; };
+    auto kv_empty = [&](int s) { return bars + 8 * (C::kStages + s); };
+    auto st_full = [&](int s) { return bars + 8 * (2 * C::kStages + s); };
+    auto st_empty = [&](int s) { return bars + 8 * (2 * C::kStages + C::kStaging + s); };
+    constexpr int kRest = 2 * (C::kStages + C::kStaging);
+    const uint32_t q_full = bars + 8 * kRest, q_empty = q_full + 8;
+    auto s_full = [&](int w) { return q_full + 16 + 8 * w; };
+    auto p_full = [&](int w) { return q_full + 32 + 8 * w; };
+    auto o_done = [&](int w) { return q_full + 48 + 8 * w; };
+    const uint32_t join = q_full + 64;
+    static_assert(8 * (kRest + 9) <= 400, "barriers fit");
+    uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [4..] the share's start
+    volatile uint32_t* dead = words + 1;
+    long long* start = reinterpret_cast<long long*>(words + 4);                     // [0] linear base, [1] seq | unit << 32
+
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const uint32_t Hkv = a.p.n_kv_heads, G = a.group;
+    const int tq = kBM / int(G);                                                    // tokens of a row tile
+    const Space sp{ 2 * tq, int(a.window), int((a.sinks + kBN - 1) / kBN) };
+
+    // ---- the block's share ----
+    long long* prefix = reinterpret_cast<long long*>(smem);                         // [n_seqs + 1], over the rings before they are used
+    __shared__ long long warp_sum[32];
+    long long carry = 0;
+    for (uint32_t b0 = 0; b0 < a.b.n_seqs; b0 += C::kThreads) {
+        long long v = 0;
+        Walk w; w.i = b0 + tid;
+        if (w.i < a.b.n_seqs && w.load(a, sp)) v = sp.sum(w.s, w.s.units);
+        long long inc = v;
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, m); if (lane >= m) inc += y; }
+        if (lane == 31) warp_sum[warp] = inc;
+        __syncthreads();
+        long long before = carry;
+        for (int k = 0; k < C::kThreads / 32; ++k) { if (k < warp) before += warp_sum[k]; carry += warp_sum[k]; }
+        if (w.i < a.b.n_seqs) prefix[w.i] = before + inc - v;
+        __syncthreads();
+    }
+    const long long total = carry * Hkv;
+    const long long share = max((total + gridDim.x - 1) / gridDim.x, 2ll);
+    const long long begin = blockIdx.x * share, end = min(total, begin + share);
+    if (begin >= end) return;
+    if (tid == 0) {
+        const long long per_head = begin / Hkv;
+        uint32_t i = 0, hi = a.b.n_seqs;
+        while (hi - i > 1) { const uint32_t mid = (i + hi) >> 1; if (prefix[mid] <= per_head) i = mid; else hi = mid; }
+        Walk w; w.i = i; w.load(a, sp);
+        int u = 0, uh = w.s.units;
+        while (uh - u > 1) { const int mid = (u + uh) >> 1; if (prefix[i] + sp.sum(w.s, mid) <= per_head) u = mid; else uh = mid; }
+        start[0] = (prefix[i] + sp.sum(w.s, u)) * Hkv;
+        start[1] = (long long)i | (long long)u << 32;
+        words[1] = 0;
+        for (int s = 0; s < C::kStages; ++s) { bar_init(kv_full(s), kQuant ? 128 : 1); bar_init(kv_empty(s), 1); }
+        for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), 128); }
+        bar_init(q_full, 1); bar_init(q_empty, 1);
+        for (int w2 = 0; w2 < 2; ++w2) { bar_init(s_full(w2), 1); bar_init(p_full(w2), 128); bar_init(o_done(w2), 1); }
+        bar_init(join, 256);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();                                                                // the share is known, prefix is done with
+    if (warp == 0) tmem_alloc(smem_at(words), C::kCols);
+    // query rows that no copy fills (128 is no multiple of the group) are zero
+    for (int e = tid; e < 2 * C::kQ / 16; e += C::kThreads) reinterpret_cast<uint4*>(smem)[e] = make_uint4(0, 0, 0, 0);
+    fence_async_proxy();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = words[0];
+
+    Walk walk;
+    walk.x = begin; walk.end = end; walk.base = start[0]; walk.i = uint32_t(start[1]); walk.u = int(start[1] >> 32);
+    walk.load(a, sp); walk.spans(sp);
+    Segment g;
+#define WAIT(bar, parity) __all_sync(0xffffffffu, bar_wait(bar, parity, dead))
+
+    if (warp == C::kWarpLoad) {
+        // ---- copies: queries of a segment, then its key and value tiles in turn ----
+        const uint32_t page_tokens = 1u << a.p.page_shift;
+        constexpr int kBoxSlabs = kQuant ? 1 : C::kSlabs;
+        const int n_box = kBN / int(page_tokens) * kBoxSlabs;
+        const int nowhere = int(a.p.n_pages * Hkv) << a.p.page_shift;               // beyond the last row: zeros
+        long long it = 0, seg = 0;
+        bool ok = true;
+        while (ok && walk.next(a, sp, g)) {
+            if (seg && !(ok = WAIT(q_empty, uint32_t(seg - 1) & 1))) break;
+            if (lane == 0) {
+                const uint32_t one = uint32_t(tq) * G * 128 * C::kSlabs;            // bytes of one row tile
+                bar_expect(q_full, g.two ? 2 * one : one);
+                for (int w = 0; w < (g.two ? 2 : 1); ++w)
+                    for (int d = 0; d < C::kSlabs; ++d) tma_3d(base + w * C::kQ + d * (kBM * 128), &q_map, d * 64, g.h * int(G), g.q0 + g.tok0 + w * tq, q_full);
+            }
+            ++seg;
+            for (int t = g.t0; ok && t < g.t1; ++t) {
+                // a lane per box: the page's row in the pool, or nowhere
+                int row = nowhere;
+                const int b = lane / kBoxSlabs, key0 = g.tile_key(t), key = key0 + b * int(page_tokens);
+                if (lane < n_box && key < g.hi && (!a.window || key + int(page_tokens) > g.lo || key < int(a.sinks))) {
+                    const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
+                    if (page < a.p.n_pages) row = int((page * Hkv + uint32_t(g.h)) << a.p.page_shift);
+                    else report(a.err, bePage);
+                }
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    constexpr int N = kQuant ? C::kStaging : C::kStages;
+                    const int s = int(it % N);
+                    const uint32_t full = kQuant ? st_full(s) : kv_full(s), empty = kQuant ? st_empty(s) : kv_empty(s);
+                    if (it >= N && !(ok = WAIT(empty, uint32_t(it / N - 1) & 1))) break;
+                    if (lane == 0) bar_expect(full, kQuant ? C::kCodes : C::kTile);
+                    __syncwarp();
+                    if (lane < n_box) {
+                        const CUtensorMap* map = kv ? &v_map : &k_map;
+                        if constexpr (kQuant) tma_2d(base + C::kOffStaging + s * C::kCodes + b * int(page_tokens) * D, map, 0, row, full);
+                        else tma_2d(base + C::kOffRing + s * C::kTile + lane % kBoxSlabs * (kBN * 128) + b * int(page_tokens) * 128, map, lane % kBoxSlabs * 64, row, full);
+                    }
+                    ++it;
+                }
+            }
+        }
+        if (*dead) {      // leave no copy in flight behind
+            constexpr int N = kQuant ? C::kStaging : C::kStages;
+            for (long long k = it > N ? it - N : 0; k < it; ++k) {
+                const long long t0 = clock64();
+                while (!bar_try(kQuant ? st_full(int(k % N)) : kv_full(int(k % N)), uint32_t(k / N) & 1) && clock64() - t0 < 100000000ll) {}
+            }
+        }
+    } else if (warp == C::kWarpMma) {
+        // ---- matrix instructions: S of the first tile, then per tile PV and the next S, the two row tiles in turn ----
+        constexpr uint32_t kDescS = mma_desc(BF, false, kBN), kDescO = mma_desc(BF, true, D);
+        long long it = 0, seg = 0;                              // ring items and tiles so far (the parity of p_full goes by tiles of each row tile)
+        long long tiles_of[2] = { 0, 0 };
+        bool ok = true;
+        auto scores = [&](int w, int s) {
+            if (lane == 0) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t at = k / 4 * (kBM * 128) + k % 4 * 32;
+                    mma_ss(tmem + C::kColS + w * 128, smem_desc(base + w * C::kQ + at, 16, 1024), smem_desc(base + C::kOffRing + s * C::kTile + at, 16, 1024), kDescS, k > 0);
+                }
+                tc_commit(s_full(w));
+            }
+            __syncwarp();
+        };
+        auto values = [&](int w, int s, bool add) {
+            if (lane == 0) {
+#pragma unroll
+                for (int k = 0; k < kBN / 16; ++k)
+                    mma_ts(tmem + C::kColO + w * D, tmem + C::kColS + w * 128 + k * 8, smem_desc(base + C::kOffRing + s * C::kTile + k * 2048, kBN * 128, 1024), kDescO, add || k > 0);
+                tc_commit(o_done(w));
+            }
+            __syncwarp();
+        };
+        auto commit = [&](uint32_t bar) { if (lane == 0) tc_commit(bar); __syncwarp(); };
+        while (ok && walk.next(a, sp, g)) {
+            const int nw = g.two ? 2 : 1, n = g.t1 - g.t0;
+            if (!(ok = WAIT(q_full, uint32_t(seg) & 1))) break;
+            if (!(ok = WAIT(kv_full(int(it % C::kStages)), uint32_t(it / C::kStages) & 1))) break;
+            tc_after();
+            for (int w = 0; w < nw; ++w) scores(w, int(it % C::kStages));
+            commit(kv_empty(int(it % C::kStages)));
+            for (int j = 0; ok && j < n; ++j) {
+                const long long iv = it + 1, ik = it + 2;
+                if (!(ok = WAIT(kv_full(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
+                for (int w = 0; ok && w < nw; ++w) {
+                    if (!(ok = WAIT(p_full(w), uint32_t(tiles_of[w]) & 1))) break;
+                    tc_after();
+                    ++tiles_of[w];
+                    values(w, int(iv % C::kStages), j > 0);
+                    if (j + 1 < n) {
+                        if (w == 0 && !(ok = WAIT(kv_full(int(ik % C::kStages)), uint32_t(ik / C::kStages) & 1))) break;
+                        scores(w, int(ik % C::kStages));
+                    }
+                }
+                if (!ok) break;
+                // both tiles' instructions up to here must be done before the stages are filled again
+                commit(kv_empty(int(iv % C::kStages)));
+                if (j + 1 < n) commit(kv_empty(int(ik % C::kStages)));
+                it += 2;
+            }
+            commit(q_empty);
+            ++seg;
+        }
+    } else if (kQuant && warp >= C::kWarpConvert && warp < C::kWarpConvert + 4) {
+        // ---- widening: codes of a staged tile to the operand layout, scales beside them ----
+        if constexpr (kQuant) {
+            const int t128 = tid - C::kWarpConvert * 32;
+            constexpr int kChunks = D / 16;                     // 16 codes each
+            long long it = 0;
+            bool ok = true;
+            while (ok && walk.next(a, sp, g)) {
+                for (int t = g.t0; ok && t < g.t1; ++t) {
+                    const int key0 = g.tile_key(t);
+                    auto seen = [&](int key) { return key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)); };
+                    // this thread's key's scales
+                    float scale[2] = { 0.0f, 0.0f };
+                    if (seen(key0 + t128)) {
+                        const int key = key0 + t128;
+                        const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
+                        if (page < a.p.n_pages) {
+                            const uint64_t cell = ((uint64_t(page) * Hkv + uint32_t(g.h)) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1));
+                            scale[0] = __ldg(a.p.k_scale + cell); scale[1] = __ldg(a.p.v_scale + cell);
+                        }
+                    }
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int ss = int(it % C::kStaging), s = int(it % C::kStages);
+                        if (!(ok = WAIT(st_full(ss), uint32_t(it / C::kStaging) & 1))) break;
+                        if (it >= C::kStages && !(ok = WAIT(kv_empty(s), uint32_t(it / C::kStages - 1) & 1))) break;
+                        const uint8_t* from = smem + C::kOffStaging + ss * C::kCodes;
+                        uint8_t* to = smem + C::kOffRing + s * C::kTile;
+#pragma unroll
+                        for (int e = 0; e < kChunks; ++e) {
+                            const int c = t128 % kChunks, r = t128 / kChunks + e * (128 / kChunks);
+                            uint4 x = *reinterpret_cast<const uint4*>(from + r * D + c * 16);
+                            if (!seen(key0 + r)) x = make_uint4(0, 0, 0, 0);
+                            const uint4 lo = make_uint4(widen<BF, CACHE>(x.x & 0xffffu), widen<BF, CACHE>(x.x >> 16), widen<BF, CACHE>(x.y & 0xffffu), widen<BF, CACHE>(x.y >> 16));
+                            const uint4 hi = make_uint4(widen<BF, CACHE>(x.z & 0xffffu), widen<BF, CACHE>(x.z >> 16), widen<BF, CACHE>(x.w & 0xffffu), widen<BF, CACHE>(x.w >> 16));
+                            uint8_t* row = to + c / 4 * (kBN * 128) + r * 128;
+                            const int p0 = ((2 * (c % 4)) ^ (r & 7)) * 16, p1 = ((2 * (c % 4) + 1) ^ (r & 7)) * 16;
+                            if (c < 4) { *reinterpret_cast<uint4*>(row + p0) = lo; *reinterpret_cast<uint4*>(row + p1) = hi; }
+                            else { *reinterpret_cast<uint4*>(row + p1) = hi; *reinterpret_cast<uint4*>(row + p0) = lo; }   // the other order: no bank twice
+                        }
+                        float* sc = reinterpret_cast<float*>(smem + C::kOffScales) + ((it / 2) % 4 * 2 + kv) * kBN;
+                        sc[t128] = kv ? scale[1] * C::kLift : scale[0] * a.scale_log2;
+                        fence_async_proxy();
+                        bar_arrive(kv_full(s));
+                        bar_arrive(st_empty(ss));
+                        ++it;
+                    }
+                }
+            }
+        }
+    } else if (warp < 8) {
+        // ---- softmax of one row tile, a row per thread ----
+        const int w = warp / 4, r = tid % 128;
+        const uint32_t lanes = uint32_t(warp % 4 * 32) << 16;
+        const uint32_t tS = tmem + C::kColS + w * 128 + lanes, tO = tmem + C::kColO + w * D + lanes;
+        long long it = 0, n_done = 0, joins = 0;             // tiles of the block (ring items / 2), tiles of this row tile, joins
+        bool ok = true;
+        while (ok && walk.next(a, sp, g)) {
+            const int n = g.t1 - g.t0;
+            const bool work = w == 0 || g.two;
+            const int tok = g.tok0 + w * tq + r / int(G);
+            const bool row_on = r < tq * int(G) && tok < g.q_len;
+            const int place = g.place0 + tok;
+            // places of the row tile's first and last row
+            const int place_a = g.place0 + g.tok0 + w * tq, place_b = g.place0 + min(g.q_len - 1, g.tok0 + w * tq + tq - 1);
+            float m = kLow, l = 0.0f;
+            if (work) {
+                for (int j = 0; j < n; ++j) {
+                    const int key0 = g.tile_key(g.t0 + j);
+                    const long long ring_k = 2 * (it + j);
+                    if (!(ok = WAIT(s_full(w), uint32_t(n_done) & 1))) break;
+                    tc_after();
+                    const bool masked = key0 + kBN - 1 > place_a || (a.window && key0 < place_b - int(a.window) + 1 && key0 + kBN > int(a.sinks));
+                    const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + ((it + j) % 4 * 2) * kBN;
+                    if constexpr (kQuant) { if (!(ok = WAIT(kv_full(int((ring_k + 1) % C::kStages)), uint32_t((ring_k + 1) / C::kStages) & 1))) break; }
+                    // x of 32 columns: scaled (f = 1 afterwards) where the tile is masked or quantised, raw otherwise
+                    const float f = kQuant || masked ? 1.0f : a.scale_log2;
+                    auto fetch = [&](int c0, float (&x)[32]) {
+                        uint32_t v[32];
+                        tm_ld32(tS + c0, v);
+                        tm_wait_ld32(v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+                        if constexpr (kQuant) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 k4 = *reinterpret_cast<const float4*>(ks + c0 + e);
+                                x[e] *= k4.x; x[e + 1] *= k4.y; x[e + 2] *= k4.z; x[e + 3] *= k4.w;
+                            }
+                        }
+                        if (masked) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const int key = key0 + c0 + e;
+                                const bool hidden = key > place || (a.window && key <= place - int(a.window) && key >= int(a.sinks));
+                                x[e] = hidden ? -INFINITY : kQuant ? x[e] : x[e] * a.scale_log2;
+                            }
+                        }
+                    };
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kBN; c0 += 32) {
+                        float x[32];
+                        fetch(c0, x);
+                        float t0 = x[0] * f, t1 = x[1] * f;
+                        if (f >= 0.0f) {
+                            float u0 = x[0], u1 = x[1];
+#pragma unroll
+                            for (int e = 2; e < 32; e += 2) { u0 = fmaxf(u0, x[e]); u1 = fmaxf(u1, x[e + 1]); }
+                            t0 = fmaxf(u0, u1) * f; t1 = t0;
+                        } else {
+#pragma unroll
+                            for (int e = 2; e < 32; ++e) t0 = fmaxf(t0, x[e] * f);
+                        }
+                        top = fmaxf(top, fmaxf(t0, t1));
+                    }
+                    if (!row_on) top = m;
+                    if (__any_sync(0xffffffffu, top > m + C::kLag)) {
+                        const float mn = fmaxf(m, top), shrink = ex2(m - mn);
+                        if (j > 0) {                            // O so far shrinks too, once the last product into it is done
+                            if (!(ok = WAIT(o_done(w), uint32_t(n_done - 1) & 1))) break;
+                            tc_after();
+#pragma unroll 1
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                uint32_t v[32];
+                                tm_ld32(tO + c0, v);
+                                tm_wait_ld32(v);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * shrink);
+                                tm_st32(tO + c0, v);
+                            }
+                        }
+                        l *= shrink; m = mn;
+                    }
+                    const uint64_t f2 = pack2(f, f), m2 = pack2(-m, -m);
+                    uint64_t sum = pack2(0.0f, 0.0f);
+                    // P takes the place of S from its first column on: 64 columns of S give 32 of P, so a column is never written before it was read
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kBN; c0 += 64) {
+                        uint32_t p[32];
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            float x[32];
+                            fetch(c0 + half * 32, x);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                float y0, y1;
+                                unpack2(fma2(pack2(x[e], x[e + 1]), f2, m2), y0, y1);
+                                y0 = ex2(y0); y1 = ex2(y1);
+                                const uint64_t y = pack2(y0, y1);
+                                sum = add2(sum, y);
+                                if constexpr (kQuant) {
+                                    const float2 v2 = *reinterpret_cast<const float2*>(ks + kBN + c0 + half * 32 + e);
+                                    y0 *= v2.x; y1 *= v2.y;
+                                    if (masked) { y0 = x[e] == -INFINITY ? 0.0f : y0; y1 = x[e + 1] == -INFINITY ? 0.0f : y1; }      // a hidden value's scale may be NaN
+                                }
+                                p[half * 16 + e / 2] = A::pack(y0, y1);
+                            }
+                        }
+                        tm_st32(tS + c0 / 2, p);
+                    }
+                    float s0, s1;
+                    unpack2(sum, s0, s1);
+                    l += s0 + s1;
+                    if constexpr (!kQuant) {
+                        // values that no row of the unit sees are zeroed in shared memory: a weight of 0 does not silence a NaN
+                        const bool edge = key0 + kBN > g.hi || (a.window && key0 < g.lo && key0 + kBN > int(a.sinks));
+                        if (edge && w == 0) {
+                            const long long iv = ring_k + 1;
+                            if (!(ok = WAIT(kv_full(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
+                            const int key = key0 + r;
+                            if (!(key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)))) {
+                                for (int d = 0; d < C::kSlabs; ++d)
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e)
+                                        *reinterpret_cast<uint4*>(smem + C::kOffRing + int(iv % C::kStages) * C::kTile + d * (kBN * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_async_proxy();
+                        }
+                    }
+                    tm_wait_st();
+                    tc_before();
+                    bar_arrive(p_full(w));
+                    ++n_done;
+                }
+            }
+            if (!ok) break;
+            it += n;
+            if (work) {
+                if (!(ok = WAIT(o_done(w), uint32_t(n_done - 1) & 1))) break;
+                tc_after();
+            }
+            const bool whole = g.t0 == 0 && g.t1 == g.tiles;
+            const long long x0 = walk.x - n;
+            const uint32_t slot = 2 * blockIdx.x + (x0 == begin ? 0 : 1);
+            uint8_t* dst = a.out + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.out_stride + (uint64_t(g.h) * G + r % G) * D) * 2;
+            if (work) {
+                const float inv = l > 0.0f ? (1.0f / C::kLift) / l : l;
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    uint32_t v[32];
+                    tm_ld32(tO + c0, v);
+                    tm_wait_ld32(v);
+                    if (whole) {
+                        if (row_on) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8) {
+                                uint32_t o[4];
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) o[q] = A::pack(__uint_as_float(v[e + 2 * q]) * inv, __uint_as_float(v[e + 2 * q + 1]) * inv);
+                                *reinterpret_cast<uint4*>(dst + (c0 + e) * 2) = make_uint4(o[0], o[1], o[2], o[3]);
+                            }
+                        }
+                    } else if (row_on) {
+                        float4* part = reinterpret_cast<float4*>(a.s.part_o) + (uint64_t(slot) * 2 + w) * (D / 4) * kBM + r;      // [slot][row tile][D / 4][128] float4
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            part[(c0 / 4 + e) * kBM] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+                    }
+                }
+                if (!whole && row_on) a.s.part_ml[(slot * 2 + w) * kBM + r] = make_float2(m, l);
+                tc_before();
+            }
+            if (!whole) {
+                // the unit's blocks are consecutive; the last to arrive joins their parts in that order
+                const long long u0 = x0 - g.t0, u1 = u0 + g.tiles;
+                const uint32_t blk0 = uint32_t(u0 / share), blk1 = uint32_t((u1 - 1) / share);
+                const uint32_t first_slot = 2 * blk0 + (u0 % share ? 1 : 0);
+                __threadfence();
+                bar_arrive(join);
+                if (!(ok = WAIT(join, uint32_t(joins) & 1))) break;
+                ++joins;
+                if (tid == 0) { __threadfence(); words[2] = atomicAdd(&a.s.ticket[first_slot], 1u) == blk1 - blk0; }
+                __syncwarp();
+                bar_arrive(join);
+                if (!(ok = WAIT(join, uint32_t(joins) & 1))) break;
+                ++joins;
+                if (words[2]) {
+                    __threadfence();
+                    if (row_on && work) {
+                        float mm = kLow;
+                        for (uint32_t b = blk0; b <= blk1; ++b) mm = fmaxf(mm, __ldcg(a.s.part_ml + ((b == blk0 ? first_slot : 2 * b) * 2 + w) * kBM + r).x);
+                        float ll = 0.0f;
+                        for (uint32_t b = blk0; b <= blk1; ++b) { const float2 ml = __ldcg(a.s.part_ml + ((b == blk0 ? first_slot : 2 * b) * 2 + w) * kBM + r); ll += ml.y * ex2(ml.x - mm); }
+                        const float inv = ll > 0.0f ? (1.0f / C::kLift) / ll : ll;
+#pragma unroll 1
+                        for (int d4 = 0; d4 < D / 4; d4 += 2) {
+                            float o[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+                            for (uint32_t b = blk0; b <= blk1; ++b) {
+                                const uint32_t s = (b == blk0 ? first_slot : 2 * b) * 2 + w;
+                                const float e0 = ex2(__ldcg(a.s.part_ml + s * kBM + r).x - mm);
+                                const float4* part = reinterpret_cast<const float4*>(a.s.part_o) + uint64_t(s) * (D / 4) * kBM + r;
+                                const float4 p = __ldcg(part + d4 * kBM), q = __ldcg(part + (d4 + 1) * kBM);
+                                o[0] += p.x * e0; o[1] += p.y * e0; o[2] += p.z * e0; o[3] += p.w * e0;
+                                o[4] += q.x * e0; o[5] += q.y * e0; o[6] += q.z * e0; o[7] += q.w * e0;
+                            }
+                            *reinterpret_cast<uint4*>(dst + d4 * 8) = make_uint4(A::pack(o[0] * inv, o[1] * inv), A::pack(o[2] * inv, o[3] * inv), A::pack(o[4] * inv, o[5] * inv), A::pack(o[6] * inv, o[7] * inv));
+                        }
+                    }
+                    if (tid == 0) a.s.ticket[first_slot] = 0;
+                }
+            }
+        }
+    }
+#undef WAIT
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    if (tid == 0 && words[1]) report(a.err, beTimeout);
+    if (warp == 0) { tc_after(); tmem_free(tmem, C::kCols); }
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder()
+{
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(p) : nullptr;
+    }();
+    return f;
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tile(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s)
+{
+    const EncodeTiled encode = encoder();
+    if (!encode) return cudaErrorNotSupported;
+    const bool quant = cache != WWWS_CACHE_16;
+    const CUtensorMapDataType act = dtype == WWWS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    CUtensorMap maps[3];
+    {
+        const cuuint64_t dims[3] = { head_dim, uint64_t(a.p.n_kv_heads) * a.group, a.b.n_tokens };
+        const cuuint64_t strides[2] = { head_dim * 2ull, a.q_stride * 2ull };
+        const cuuint32_t box[3] = { 64, a.group, 128 / a.group }, ones[3] = { 1, 1, 1 };
+        if (encode(&maps[0], act, 3, const_cast<uint8_t*>(a.q), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) return cudaErrorInvalidValue;
+    }
+    for (int kv = 0; kv < 2; ++kv) {
+        const cuuint64_t dims[2] = { head_dim, uint64_t(a.p.n_pages) * a.p.n_kv_heads << a.p.page_shift };
+        const cuuint64_t strides[1] = { head_dim * (quant ? 1ull : 2ull) };
+        const cuuint32_t box[2] = { quant ? head_dim : 64, 1u << a.p.page_shift }, ones[2] = { 1, 1 };
+        if (encode(&maps[1 + kv], quant ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : act, 2, kv ? a.p.v : a.p.k, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   quant ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    auto go = [&](auto bf, auto kind, auto dim) -> cudaError_t {
+        using C = Cfg<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
+        static_assert(C::kSmem <= 232448 - 512, "shared memory of a block");
+        static_assert(C::kOffBars >= 2048 * 8, "the prefix fits over the rings");
+        auto kernel = k_attend_tile<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
+        if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem); e != cudaSuccess) return e;
+        // no more blocks than tiles the bounds allow
+        const uint64_t step = 2 * (128 / a.group), units = a.b.n_tokens / step + a.b.n_seqs;
+        const uint64_t tiles = units * a.p.n_kv_heads * ((a.b.max_kv_len + kBN - 1) / kBN);
+        kernel<<<uint32_t(tiles < kTileBlocks ? (tiles ? tiles : 1) : kTileBlocks), C::kThreads, C::kSmem, s>>>(a, maps[0], maps[1], maps[2]);
+        return cudaGetLastError();
+    };
+    using std::integral_constant;
+    auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? go(bf, kind, integral_constant<int, 64>()) : go(bf, kind, integral_constant<int, 128>()); };
+    auto kind = [&](auto bf) {
+        return cache == WWWS_CACHE_16 ? dim(bf, integral_constant<int, 0>()) : cache == WWWS_CACHE_INT8 ? dim(bf, integral_constant<int, 1>()) : dim(bf, integral_constant<int, 2>());
+    };
+    return dtype == WWWS_BF16 ? kind(std::true_type()) : kind(std::false_type());
+}
+
+}  // namespace wwws

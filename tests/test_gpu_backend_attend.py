@@ -68,7 +68,7 @@ def test_large_scores_keep_their_softmax(cache, lens):
     check(case)
 
 
-@pytest.mark.parametrize("lens", [[(1, 70), (1, 9)], [(70, 70), (140, 150)]], ids=["decode", "prompts"])
+@pytest.mark.parametrize("lens", [[(1, 70), (1, 9)], [(4, 70), (3, 9)], [(70, 70), (140, 150)]], ids=["decode", "few", "prompts"])
 def test_nan_row_of_a_quantised_cache_reaches_only_rows_that_see_it(lens):
     case = Case(lens, kv_heads=2, group=4, dim=64, page=16, dtype=BF16, cache="int8", seed=7)
     for place in (0, 64):
