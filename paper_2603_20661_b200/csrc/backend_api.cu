@@ -57,6 +57,7 @@ const char* check_config(const wwws_backend_config* c)
     if (c->max_seqs < 1 || c->max_seqs > 2048) return "max_seqs must be 1..2048";
     if (c->max_tokens < 1 || c->max_tokens >= (1u << 27) || uint64_t(c->max_tokens) * c->n_kv_heads >= (1ull << 31)) return "max_tokens must be 1..2^27-1 and max_tokens * n_kv_heads < 2^31";
     if (c->max_pages < 1 || uint64_t(c->max_pages) * c->page_tokens >= (1u << 30)) return "max_pages must be >= 1 and max_pages * page_tokens < 2^30";
+    if (uint64_t(c->max_pages) * c->page_tokens * c->n_kv_heads >= (1ull << 37)) return "max_pages * page_tokens * n_kv_heads must be < 2^37";
     if (c->dtype != WWWS_BF16 && c->dtype != WWWS_F16) return "dtype must be WWWS_BF16 or WWWS_F16";
     if (c->cache > WWWS_CACHE_E4M3) return "cache must be a wwws_cache_kind";
     return nullptr;

@@ -103,55 +103,52 @@ struct Space {
     }
 };
 
-struct Segment {
-    int q0, place0, q_len, kv;
-    int tok0;                  // first token of the unit within the sequence's new tokens
-    int h, t0, t1, tiles;
+// Walks a block's share, segment by segment: a segment is a run of key tiles of one (sequence, unit, kv head).  Every role holds one.
+// Positions are relative to the share's begin.
+struct Walk {
+    int y, end, base;          // base: position of the first tile of (seq, u) and kv head 0
+    uint32_t seq; int u;
+    int q0, q_len, kv;
+    // the segment
+    int h, t0, t1, tiles;      // key tiles [t0, t1) of the unit's `tiles`
     int hi, lo, lo_tile, n_sink;
-    uint32_t seq;
-    bool two;                  // the second row tile has tokens
+
+    __device__ __forceinline__ bool load(const AttendArgs& a)
+    {
+        return sequence(a.b, seq, q0, q_len, kv, a.err) && uint32_t(q_len) * a.group > a.few_rows;
+    }
+    __device__ __forceinline__ Seq as_seq(const Space& sp) const { return Seq{ q0, q_len, kv, kv - q_len, (q_len + sp.step - 1) / sp.step }; }
+    __device__ __forceinline__ void span(const Space& sp) { sp.span(as_seq(sp), u, hi, lo, lo_tile, n_sink, tiles); }
+    __device__ __forceinline__ bool next(const AttendArgs& a, const Space& sp)
+    {
+        if (y >= end) return false;
+        while (y >= base + tiles * int(a.p.n_kv_heads)) {
+            base += tiles * int(a.p.n_kv_heads);
+            if (++u * sp.step >= q_len) {
+                u = 0;
+                do { ++seq; } while (seq < a.b.n_seqs && !load(a));
+                if (seq >= a.b.n_seqs) { y = end; return false; }
+            }
+            span(sp);
+        }
+        h = (y - base) / tiles; t0 = (y - base) % tiles;
+        t1 = min(tiles, t0 + end - y);
+        y += t1 - t0;
+        return true;
+    }
+    __device__ __forceinline__ int tok0(const Space& sp) const { return u * sp.step; }             // first token of the unit
+    __device__ __forceinline__ bool two(const Space& sp) const { return u * sp.step + sp.step / 2 < q_len; }   // the second row tile has tokens
     __device__ __forceinline__ int tile_key(int t) const { return (t < n_sink ? t : lo_tile + t - n_sink) * kBN; }
 };
 
-// Walks a block's share [x, end); every role holds one.
-struct Walk {
-    long long x, end, base;    // base: linear position of (seq, unit)'s first tile
-    uint32_t i; int u;
-    Seq s; int tiles, hi, lo, lo_tile, n_sink;
-
-    __device__ __forceinline__ bool load(const AttendArgs& a, const Space& sp)
-    {
-        int q0, q_len, kv;
-        if (!sequence(a.b, i, q0, q_len, kv, a.err) || uint32_t(q_len) * a.group <= a.few_rows) { s.units = 0; return false; }
-        s = Seq{ q0, q_len, kv, kv - q_len, (q_len + sp.step - 1) / sp.step };
-        return true;
-    }
-    __device__ __forceinline__ void spans(const Space& sp) { sp.span(s, u, hi, lo, lo_tile, n_sink, tiles); }
-    __device__ __forceinline__ bool next(const AttendArgs& a, const Space& sp, Segment& g)
-    {
-        if (x >= end) return false;
-        const uint32_t Hkv = a.p.n_kv_heads;
-        while (x >= base + (long long)tiles * Hkv) {
-            base += (long long)tiles * Hkv;
-            if (++u >= s.units) {
-                u = 0;
-                do { ++i; } while (i < a.b.n_seqs && !load(a, sp));
-                if (i >= a.b.n_seqs) { x = end; return false; }
-            }
-            spans(sp);
-        }
-        const long long rel = x - base;
-        g.h = int(rel / tiles); g.t0 = int(rel % tiles);
-        g.t1 = int(min((long long)tiles, g.t0 + (end - x)));
-        g.tiles = tiles; g.hi = hi; g.lo = lo; g.lo_tile = lo_tile; g.n_sink = n_sink; g.seq = i;
-        g.q0 = s.q0; g.place0 = s.place0; g.q_len = s.q_len; g.kv = s.kv; g.tok0 = u * sp.step;
-        g.two = g.tok0 + sp.step / 2 < s.q_len;
-        x += g.t1 - g.t0;
-        return true;
-    }
-};
-
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+__device__ __forceinline__ void scale2(uint32_t* x, uint64_t by)
+{
+    float y0, y1;
+    unpack2(mul2(pack2(__uint_as_float(x[0]), __uint_as_float(x[1])), by), y0, y1);
+    x[0] = __float_as_uint(y0); x[1] = __float_as_uint(y1);
+}
 
 template <bool BF, int CACHE, int D>
 __global__ void __launch_bounds__(Cfg<BF, CACHE, D>::kThreads, 1)
@@ -178,7 +175,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     static_assert(8 * (kRest + 9) <= 400, "barriers fit");
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [4..] the share's start
     volatile uint32_t* dead = words + 1;
-    long long* start = reinterpret_cast<long long*>(words + 4);                     // [0] linear base, [1] seq | unit << 32
+    int* start = reinterpret_cast<int*>(words + 4);                                 // [0] base, [1] sequence, [2] unit
 
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const uint32_t Hkv = a.p.n_kv_heads, G = a.group;
@@ -191,8 +188,8 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     long long carry = 0;
     for (uint32_t b0 = 0; b0 < a.b.n_seqs; b0 += C::kThreads) {
         long long v = 0;
-        Walk w; w.i = b0 + tid;
-        if (w.i < a.b.n_seqs && w.load(a, sp)) v = sp.sum(w.s, w.s.units);
+        Walk w; w.seq = b0 + tid;
+        if (w.seq < a.b.n_seqs && w.load(a)) { const Seq q = w.as_seq(sp); v = sp.sum(q, q.units); }
         long long inc = v;
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, m); if (lane >= m) inc += y; }
@@ -200,7 +197,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         __syncthreads();
         long long before = carry;
         for (int k = 0; k < C::kThreads / 32; ++k) { if (k < warp) before += warp_sum[k]; carry += warp_sum[k]; }
-        if (w.i < a.b.n_seqs) prefix[w.i] = before + inc - v;
+        if (w.seq < a.b.n_seqs) prefix[w.seq] = before + inc - v;
         __syncthreads();
     }
     const long long total = carry * Hkv;
@@ -211,11 +208,11 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         const long long per_head = begin / Hkv;
         uint32_t i = 0, hi = a.b.n_seqs;
         while (hi - i > 1) { const uint32_t mid = (i + hi) >> 1; if (prefix[mid] <= per_head) i = mid; else hi = mid; }
-        Walk w; w.i = i; w.load(a, sp);
-        int u = 0, uh = w.s.units;
-        while (uh - u > 1) { const int mid = (u + uh) >> 1; if (prefix[i] + sp.sum(w.s, mid) <= per_head) u = mid; else uh = mid; }
-        start[0] = (prefix[i] + sp.sum(w.s, u)) * Hkv;
-        start[1] = (long long)i | (long long)u << 32;
+        Walk w; w.seq = i; w.load(a);
+        const Seq q = w.as_seq(sp);
+        int u = 0, uh = q.units;
+        while (uh - u > 1) { const int mid = (u + uh) >> 1; if (prefix[i] + sp.sum(q, mid) <= per_head) u = mid; else uh = mid; }
+        start[0] = int((prefix[i] + sp.sum(q, u)) * Hkv - begin); start[1] = int(i); start[2] = u;
         words[1] = 0;
         for (int s = 0; s < C::kStages; ++s) { bar_init(kv_full(s), kQuant ? 128 : 1); bar_init(kv_empty(s), 1); }
         for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), 128); }
@@ -234,10 +231,9 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     tc_after();
     const uint32_t tmem = words[0];
 
-    Walk walk;
-    walk.x = begin; walk.end = end; walk.base = start[0]; walk.i = uint32_t(start[1]); walk.u = int(start[1] >> 32);
-    walk.load(a, sp); walk.spans(sp);
-    Segment g;
+    Walk g;
+    g.y = 0; g.end = int(end - begin); g.base = start[0]; g.seq = uint32_t(start[1]); g.u = start[2];
+    g.load(a); g.span(sp);
 #define WAIT(bar, parity) __all_sync(0xffffffffu, bar_wait(bar, parity, dead))
 
     if (warp == C::kWarpLoad) {
@@ -246,15 +242,15 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         constexpr int kBoxSlabs = kQuant ? 1 : C::kSlabs;
         const int n_box = kBN / int(page_tokens) * kBoxSlabs;
         const int nowhere = int(a.p.n_pages * Hkv) << a.p.page_shift;               // beyond the last row: zeros
-        long long it = 0, seg = 0;
+        uint32_t it = 0, seg = 0;
         bool ok = true;
-        while (ok && walk.next(a, sp, g)) {
+        while (ok && g.next(a, sp)) {
             if (seg && !(ok = WAIT(q_empty, uint32_t(seg - 1) & 1))) break;
             if (lane == 0) {
                 const uint32_t one = uint32_t(tq) * G * 128 * C::kSlabs;            // bytes of one row tile
-                bar_expect(q_full, g.two ? 2 * one : one);
-                for (int w = 0; w < (g.two ? 2 : 1); ++w)
-                    for (int d = 0; d < C::kSlabs; ++d) tma_3d(base + w * C::kQ + d * (kBM * 128), &q_map, d * 64, g.h * int(G), g.q0 + g.tok0 + w * tq, q_full);
+                bar_expect(q_full, g.two(sp) ? 2 * one : one);
+                for (int w = 0; w < (g.two(sp) ? 2 : 1); ++w)
+                    for (int d = 0; d < C::kSlabs; ++d) tma_3d(base + w * C::kQ + d * (kBM * 128), &q_map, d * 64, g.h * int(G), g.q0 + g.tok0(sp) + w * tq, q_full);
             }
             ++seg;
             for (int t = g.t0; ok && t < g.t1; ++t) {
@@ -285,7 +281,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         }
         if (*dead) {      // leave no copy in flight behind
             constexpr int N = kQuant ? C::kStaging : C::kStages;
-            for (long long k = it > N ? it - N : 0; k < it; ++k) {
+            for (uint32_t k = it > N ? it - N : 0; k < it; ++k) {
                 const long long t0 = clock64();
                 while (!bar_try(kQuant ? st_full(int(k % N)) : kv_full(int(k % N)), uint32_t(k / N) & 1) && clock64() - t0 < 100000000ll) {}
             }
@@ -293,8 +289,8 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     } else if (warp == C::kWarpMma) {
         // ---- matrix instructions: S of the first tile, then per tile PV and the next S, the two row tiles in turn ----
         constexpr uint32_t kDescS = mma_desc(BF, false, kBN), kDescO = mma_desc(BF, true, D);
-        long long it = 0, seg = 0;                              // ring items and tiles so far (the parity of p_full goes by tiles of each row tile)
-        long long tiles_of[2] = { 0, 0 };
+        uint32_t it = 0, seg = 0;                              // ring items and tiles so far (the parity of p_full goes by tiles of each row tile)
+        uint32_t tiles_of[2] = { 0, 0 };
         bool ok = true;
         auto scores = [&](int w, int s) {
             if (lane == 0) {
@@ -311,21 +307,21 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             if (lane == 0) {
 #pragma unroll
                 for (int k = 0; k < kBN / 16; ++k)
-                    mma_ts(tmem + C::kColO + w * D, tmem + C::kColS + w * 128 + k * 8, smem_desc(base + C::kOffRing + s * C::kTile + k * 2048, kBN * 128, 1024), kDescO, add || k > 0);
+                    mma_ts(tmem + C::kColO + w * D, tmem + C::kColS + w * 128 + 64 + k * 8, smem_desc(base + C::kOffRing + s * C::kTile + k * 2048, kBN * 128, 1024), kDescO, add || k > 0);
                 tc_commit(o_done(w));
             }
             __syncwarp();
         };
         auto commit = [&](uint32_t bar) { if (lane == 0) tc_commit(bar); __syncwarp(); };
-        while (ok && walk.next(a, sp, g)) {
-            const int nw = g.two ? 2 : 1, n = g.t1 - g.t0;
+        while (ok && g.next(a, sp)) {
+            const int nw = g.two(sp) ? 2 : 1, n = g.t1 - g.t0;
             if (!(ok = WAIT(q_full, uint32_t(seg) & 1))) break;
             if (!(ok = WAIT(kv_full(int(it % C::kStages)), uint32_t(it / C::kStages) & 1))) break;
             tc_after();
             for (int w = 0; w < nw; ++w) scores(w, int(it % C::kStages));
             commit(kv_empty(int(it % C::kStages)));
             for (int j = 0; ok && j < n; ++j) {
-                const long long iv = it + 1, ik = it + 2;
+                const uint32_t iv = it + 1, ik = it + 2;
                 if (!(ok = WAIT(kv_full(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
                 for (int w = 0; ok && w < nw; ++w) {
                     if (!(ok = WAIT(p_full(w), uint32_t(tiles_of[w]) & 1))) break;
@@ -351,9 +347,9 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         if constexpr (kQuant) {
             const int t128 = tid - C::kWarpConvert * 32;
             constexpr int kChunks = D / 16;                     // 16 codes each
-            long long it = 0;
+            uint32_t it = 0;
             bool ok = true;
-            while (ok && walk.next(a, sp, g)) {
+            while (ok && g.next(a, sp)) {
                 for (int t = g.t0; ok && t < g.t1; ++t) {
                     const int key0 = g.tile_key(t);
                     auto seen = [&](int key) { return key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)); };
@@ -401,120 +397,125 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         const int w = warp / 4, r = tid % 128;
         const uint32_t lanes = uint32_t(warp % 4 * 32) << 16;
         const uint32_t tS = tmem + C::kColS + w * 128 + lanes, tO = tmem + C::kColO + w * D + lanes;
-        long long it = 0, n_done = 0, joins = 0;             // tiles of the block (ring items / 2), tiles of this row tile, joins
+        uint32_t it = 0, n_done = 0, joins = 0;             // tiles of the block (ring items / 2), tiles of this row tile, joins
         bool ok = true;
-        while (ok && walk.next(a, sp, g)) {
+        while (ok && g.next(a, sp)) {
             const int n = g.t1 - g.t0;
-            const bool work = w == 0 || g.two;
-            const int tok = g.tok0 + w * tq + r / int(G);
+            const bool work = w == 0 || g.two(sp);
+            const int tok = g.tok0(sp) + w * tq + r / int(G);
             const bool row_on = r < tq * int(G) && tok < g.q_len;
-            const int place = g.place0 + tok;
+            const int place = (g.kv - g.q_len) + tok;
             // places of the row tile's first and last row
-            const int place_a = g.place0 + g.tok0 + w * tq, place_b = g.place0 + min(g.q_len - 1, g.tok0 + w * tq + tq - 1);
+            const int place_a = (g.kv - g.q_len) + g.tok0(sp) + w * tq, place_b = (g.kv - g.q_len) + min(g.q_len - 1, g.tok0(sp) + w * tq + tq - 1);
             float m = kLow, l = 0.0f;
             if (work) {
                 for (int j = 0; j < n; ++j) {
                     const int key0 = g.tile_key(g.t0 + j);
-                    const long long ring_k = 2 * (it + j);
+                    const uint32_t ring_k = 2 * (it + j);
                     if (!(ok = WAIT(s_full(w), uint32_t(n_done) & 1))) break;
                     tc_after();
                     const bool masked = key0 + kBN - 1 > place_a || (a.window && key0 < place_b - int(a.window) + 1 && key0 + kBN > int(a.sinks));
                     const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + ((it + j) % 4 * 2) * kBN;
                     if constexpr (kQuant) { if (!(ok = WAIT(kv_full(int((ring_k + 1) % C::kStages)), uint32_t((ring_k + 1) / C::kStages) & 1))) break; }
-                    // x of 32 columns: scaled (f = 1 afterwards) where the tile is masked or quantised, raw otherwise
+                    // 32 columns of S from c0 on: scaled (f = 1 afterwards) where the tile is masked or quantised, raw otherwise
                     const float f = kQuant || masked ? 1.0f : a.scale_log2;
-                    auto fetch = [&](int c0, float (&x)[32]) {
-                        uint32_t v[32];
-                        tm_ld32(tS + c0, v);
-                        tm_wait_ld32(v);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+                    auto prepare = [&](uint32_t* x, int c0) {
                         if constexpr (kQuant) {
 #pragma unroll
                             for (int e = 0; e < 32; e += 4) {
-                                const float4 k4 = *reinterpret_cast<const float4*>(ks + c0 + e);
-                                x[e] *= k4.x; x[e + 1] *= k4.y; x[e + 2] *= k4.z; x[e + 3] *= k4.w;
+                                const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(ks + c0 + e);
+                                scale2(x + e, k4.x); scale2(x + e + 2, k4.y);
                             }
                         }
                         if (masked) {
+                            const int last = place - key0 - c0, before = a.window ? last - int(a.window) : -1, sunk = int(a.sinks) - key0 - c0;
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
-                                const int key = key0 + c0 + e;
-                                const bool hidden = key > place || (a.window && key <= place - int(a.window) && key >= int(a.sinks));
-                                x[e] = hidden ? -INFINITY : kQuant ? x[e] : x[e] * a.scale_log2;
+                                const bool hidden = e > last || (e <= before && e >= sunk);
+                                x[e] = hidden ? 0xff800000u : kQuant ? x[e] : __float_as_uint(__uint_as_float(x[e]) * a.scale_log2);
                             }
                         }
                     };
-                    float top = -INFINITY;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kBN; c0 += 32) {
-                        float x[32];
-                        fetch(c0, x);
-                        float t0 = x[0] * f, t1 = x[1] * f;
+                    float t0 = f < 0.0f ? INFINITY : -INFINITY, t1 = t0, t2 = t0, t3 = t0;
+                    auto extreme = [&](const uint32_t* x) {
+                        auto X = [&](int e) { return __uint_as_float(x[e]); };
                         if (f >= 0.0f) {
-                            float u0 = x[0], u1 = x[1];
 #pragma unroll
-                            for (int e = 2; e < 32; e += 2) { u0 = fmaxf(u0, x[e]); u1 = fmaxf(u1, x[e + 1]); }
-                            t0 = fmaxf(u0, u1) * f; t1 = t0;
+                            for (int e = 0; e < 32; e += 8) {
+                                t0 = fmaxf(fmaxf(t0, X(e)), X(e + 1)); t1 = fmaxf(fmaxf(t1, X(e + 2)), X(e + 3));
+                                t2 = fmaxf(fmaxf(t2, X(e + 4)), X(e + 5)); t3 = fmaxf(fmaxf(t3, X(e + 6)), X(e + 7));
+                            }
                         } else {
 #pragma unroll
-                            for (int e = 2; e < 32; ++e) t0 = fmaxf(t0, x[e] * f);
+                            for (int e = 0; e < 32; e += 4) { t0 = fminf(t0, X(e)); t1 = fminf(t1, X(e + 1)); t2 = fminf(t2, X(e + 2)); t3 = fminf(t3, X(e + 3)); }
                         }
-                        top = fmaxf(top, fmaxf(t0, t1));
-                    }
-                    if (!row_on) top = m;
+                    };
+                    // the maximum: the first 64 columns are read twice (tensor memory is cheaper than 64 more registers), the others stay
+                    uint32_t xa[32], xb[32];
+                    tm_ld32(tS, xa); tm_ld32(tS + 32, xb);
+                    tm_wait_ld32(xa); tie32(xb);
+                    prepare(xa, 0); extreme(xa);
+                    prepare(xb, 32); extreme(xb);
+                    tm_ld32(tS + 64, xa); tm_ld32(tS + 96, xb);
+                    tm_wait_ld32(xa); tie32(xb);
+                    prepare(xa, 64); extreme(xa);
+                    prepare(xb, 96); extreme(xb);
+                    t0 = f >= 0.0f ? fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * f : fminf(fminf(t0, t1), fminf(t2, t3)) * f;
+                    const float top = row_on ? t0 : m;
                     if (__any_sync(0xffffffffu, top > m + C::kLag)) {
                         const float mn = fmaxf(m, top), shrink = ex2(m - mn);
                         if (j > 0) {                            // O so far shrinks too, once the last product into it is done
                             if (!(ok = WAIT(o_done(w), uint32_t(n_done - 1) & 1))) break;
                             tc_after();
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 32) {
-                                uint32_t v[32];
-                                tm_ld32(tO + c0, v);
-                                tm_wait_ld32(v);
+                            for (int c0 = 0; c0 < D; c0 += 16) {
+                                uint32_t v[16];
+                                tm_ld16(tO + c0, v);
+                                tm_wait_ld16(v);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * shrink);
-                                tm_st32(tO + c0, v);
+                                for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * shrink);
+                                tm_st16(tO + c0, v);
                             }
                         }
                         l *= shrink; m = mn;
                     }
                     const uint64_t f2 = pack2(f, f), m2 = pack2(-m, -m);
-                    uint64_t sum = pack2(0.0f, 0.0f);
-                    // P takes the place of S from its first column on: 64 columns of S give 32 of P, so a column is never written before it was read
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kBN; c0 += 64) {
-                        uint32_t p[32];
+                    uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
+                    auto weights = [&](const uint32_t* x, int c0) {
+                        uint32_t p[16];
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            float x[32];
-                            fetch(c0 + half * 32, x);
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
-                                float y0, y1;
-                                unpack2(fma2(pack2(x[e], x[e + 1]), f2, m2), y0, y1);
-                                y0 = ex2(y0); y1 = ex2(y1);
-                                const uint64_t y = pack2(y0, y1);
-                                sum = add2(sum, y);
-                                if constexpr (kQuant) {
-                                    const float2 v2 = *reinterpret_cast<const float2*>(ks + kBN + c0 + half * 32 + e);
-                                    y0 *= v2.x; y1 *= v2.y;
-                                    if (masked) { y0 = x[e] == -INFINITY ? 0.0f : y0; y1 = x[e + 1] == -INFINITY ? 0.0f : y1; }      // a hidden value's scale may be NaN
-                                }
-                                p[half * 16 + e / 2] = A::pack(y0, y1);
+                        for (int e = 0; e < 32; e += 2) {
+                            float y0, y1;
+                            unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), f2, m2), y0, y1);
+                            y0 = ex2(y0); y1 = ex2(y1);
+                            const uint64_t y = pack2(y0, y1);
+                            if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
+                            if constexpr (kQuant) {
+                                unpack2(mul2(y, *reinterpret_cast<const uint64_t*>(ks + kBN + c0 + e)), y0, y1);
+                                if (masked) { y0 = x[e] == 0xff800000u ? 0.0f : y0; y1 = x[e + 1] == 0xff800000u ? 0.0f : y1; }      // a hidden value's scale may be NaN
                             }
+                            p[e / 2] = A::pack(y0, y1);
                         }
-                        tm_st32(tS + c0 / 2, p);
-                    }
+                        tm_st16(tS + 64 + c0 / 2, p);           // P lies over the columns of S that are in registers
+                    };
+                    weights(xa, 64);
+                    tm_ld32(tS, xa);
+                    weights(xb, 96);
+                    tm_wait_ld32(xa);
+                    tm_ld32(tS + 32, xb);
+                    prepare(xa, 0);
+                    weights(xa, 0);
+                    tm_wait_ld32(xb);
+                    prepare(xb, 32);
+                    weights(xb, 32);
                     float s0, s1;
-                    unpack2(sum, s0, s1);
+                    unpack2(add2(sum_a, sum_b), s0, s1);
                     l += s0 + s1;
                     if constexpr (!kQuant) {
                         // values that no row of the unit sees are zeroed in shared memory: a weight of 0 does not silence a NaN
                         const bool edge = key0 + kBN > g.hi || (a.window && key0 < g.lo && key0 + kBN > int(a.sinks));
                         if (edge && w == 0) {
-                            const long long iv = ring_k + 1;
+                            const uint32_t iv = ring_k + 1;
                             if (!(ok = WAIT(kv_full(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
                             const int key = key0 + r;
                             if (!(key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)))) {
@@ -539,7 +540,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 tc_after();
             }
             const bool whole = g.t0 == 0 && g.t1 == g.tiles;
-            const long long x0 = walk.x - n;
+            const long long x0 = begin + g.y - n;
             const uint32_t slot = 2 * blockIdx.x + (x0 == begin ? 0 : 1);
             uint8_t* dst = a.out + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.out_stride + (uint64_t(g.h) * G + r % G) * D) * 2;
             if (work) {
