@@ -216,6 +216,8 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
     a.q = static_cast<const uint8_t*>(q); a.out = static_cast<uint8_t*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.group = b->cfg.n_heads / b->cfg.n_kv_heads;
     a.scale_log2 = float(double(scale) * 1.4426950408889634);
+    // a product that has to keep -infinity at hidden keys: the smallest normal number stands for 0 (scores of any size times it are below 4)
+    if (a.scale_log2 == 0.0f) a.scale_log2 = 0x1p-126f;
     a.window = window < batch->max_kv_len ? window : 0;          // one that hides nothing is none
     a.sinks = sinks < batch->max_kv_len ? sinks : batch->max_kv_len;
     a.err = b->err;

@@ -52,6 +52,8 @@ template <bool BF, int CACHE, int D> struct Cfg {
 };
 
 // ---- the linear space of (unit, kv head, key tile) ----
+// A unit counts kUnitCost tiles more than it has: what loading its queries and storing its result costs, in tiles.
+constexpr int kUnitCost = 2;
 
 __device__ __forceinline__ long long floor_sum(long long n, long long m, long long a, long long b)    // sum_{i<n} floor((a i + b) / m), a, b >= 0
 {
@@ -81,11 +83,11 @@ struct Space {
         n_sink = min(sink_tiles, lo_tile);
         tiles = n_sink + (hi + kBN - 1) / kBN - lo_tile;
     }
-    // tiles of the first n units
+    // cost of the first n units, in tiles
     __device__ long long sum(const Seq& s, int n) const
     {
         if (n <= 0) return 0;
-        long long total = 0;
+        long long total = (long long)n * kUnitCost;
         int last = n;
         if (n == s.units) { int hi, lo, lt, ns, t; span(s, n - 1, hi, lo, lt, ns, t); total += t; last = n - 1; }
         if (last == 0) return total;
@@ -111,7 +113,9 @@ struct Walk {
     int q0, q_len, kv;
     // the segment
     int h, t0, t1, tiles;      // key tiles [t0, t1) of the unit's `tiles`
+    int from;                  // position of tile t0
     int hi, lo, lo_tile, n_sink;
+    bool more;
 
     __device__ __forceinline__ bool load(const AttendArgs& a)
     {
@@ -122,18 +126,23 @@ struct Walk {
     __device__ __forceinline__ bool next(const AttendArgs& a, const Space& sp)
     {
         if (y >= end) return false;
-        while (y >= base + tiles * int(a.p.n_kv_heads)) {
-            base += tiles * int(a.p.n_kv_heads);
-            if (++u * sp.step >= q_len) {
-                u = 0;
-                do { ++seq; } while (seq < a.b.n_seqs && !load(a));
-                if (seq >= a.b.n_seqs) { y = end; return false; }
+        while (true) {
+            while (y >= base + (tiles + kUnitCost) * int(a.p.n_kv_heads)) {
+                base += (tiles + kUnitCost) * int(a.p.n_kv_heads);
+                if (++u * sp.step >= q_len) {
+                    u = 0;
+                    do { ++seq; } while (seq < a.b.n_seqs && !load(a));
+                    if (seq >= a.b.n_seqs) { y = end; return false; }
+                }
+                span(sp);
             }
-            span(sp);
+            h = (y - base) / (tiles + kUnitCost); t0 = (y - base) % (tiles + kUnitCost);
+            from = y;
+            y += tiles + kUnitCost - t0;
+            if (t0 < tiles) break;
+            if (y >= end) return false;         // the share began behind the unit's last tile
         }
-        h = (y - base) / tiles; t0 = (y - base) % tiles;
-        t1 = min(tiles, t0 + end - y);
-        y += t1 - t0;
+        t1 = min(tiles, t0 + end - from);
         return true;
     }
     __device__ __forceinline__ int tok0(const Space& sp) const { return u * sp.step; }             // first token of the unit
@@ -231,9 +240,21 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     tc_after();
     const uint32_t tmem = words[0];
 
-    Walk g;
-    g.y = 0; g.end = int(end - begin); g.base = start[0]; g.seq = uint32_t(start[1]); g.u = start[2];
-    g.load(a); g.span(sp);
+    // each warp's walk lives in shared memory: its first lane steps it, and it takes no registers from the loops below
+    __shared__ Walk walks[C::kThreads / 32];
+    Walk& g = walks[warp];
+    if (lane == 0) {
+        Walk w;
+        w.y = 0; w.end = int(end - begin); w.base = start[0]; w.seq = uint32_t(start[1]); w.u = start[2];
+        w.load(a); w.span(sp);
+        g = w;
+    }
+    auto next = [&] {
+        __syncwarp();
+        if (lane == 0) { Walk w = g; w.more = w.next(a, sp); g = w; }
+        __syncwarp();
+        return g.more;
+    };
 #define WAIT(bar, parity) __all_sync(0xffffffffu, bar_wait(bar, parity, dead))
 
     if (warp == C::kWarpLoad) {
@@ -244,7 +265,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         const int nowhere = int(a.p.n_pages * Hkv) << a.p.page_shift;               // beyond the last row: zeros
         uint32_t it = 0, seg = 0;
         bool ok = true;
-        while (ok && g.next(a, sp)) {
+        while (ok && next()) {
             if (seg && !(ok = WAIT(q_empty, uint32_t(seg - 1) & 1))) break;
             if (lane == 0) {
                 const uint32_t one = uint32_t(tq) * G * 128 * C::kSlabs;            // bytes of one row tile
@@ -313,7 +334,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             __syncwarp();
         };
         auto commit = [&](uint32_t bar) { if (lane == 0) tc_commit(bar); __syncwarp(); };
-        while (ok && g.next(a, sp)) {
+        while (ok && next()) {
             const int nw = g.two(sp) ? 2 : 1, n = g.t1 - g.t0;
             if (!(ok = WAIT(q_full, uint32_t(seg) & 1))) break;
             if (!(ok = WAIT(kv_full(int(it % C::kStages)), uint32_t(it / C::kStages) & 1))) break;
@@ -332,6 +353,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         if (w == 0 && !(ok = WAIT(kv_full(int(ik % C::kStages)), uint32_t(ik / C::kStages) & 1))) break;
                         scores(w, int(ik % C::kStages));
                     }
+                    if (j + 2 >= n && w == nw - 1 && (j + 2 == n || n == 1)) commit(q_empty);      // the segment's last scores are issued
                 }
                 if (!ok) break;
                 // both tiles' instructions up to here must be done before the stages are filled again
@@ -339,7 +361,6 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 if (j + 1 < n) commit(kv_empty(int(ik % C::kStages)));
                 it += 2;
             }
-            commit(q_empty);
             ++seg;
         }
     } else if (kQuant && warp >= C::kWarpConvert && warp < C::kWarpConvert + 4) {
@@ -349,7 +370,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             constexpr int kChunks = D / 16;                     // 16 codes each
             uint32_t it = 0;
             bool ok = true;
-            while (ok && g.next(a, sp)) {
+            while (ok && next()) {
                 for (int t = g.t0; ok && t < g.t1; ++t) {
                     const int key0 = g.tile_key(t);
                     auto seen = [&](int key) { return key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)); };
@@ -399,7 +420,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         const uint32_t tS = tmem + C::kColS + w * 128 + lanes, tO = tmem + C::kColO + w * D + lanes;
         uint32_t it = 0, n_done = 0, joins = 0;             // tiles of the block (ring items / 2), tiles of this row tile, joins
         bool ok = true;
-        while (ok && g.next(a, sp)) {
+        while (ok && next()) {
             const int n = g.t1 - g.t0;
             const bool work = w == 0 || g.two(sp);
             const int tok = g.tok0(sp) + w * tq + r / int(G);
@@ -417,8 +438,20 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                     const bool masked = key0 + kBN - 1 > place_a || (a.window && key0 < place_b - int(a.window) + 1 && key0 + kBN > int(a.sinks));
                     const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + ((it + j) % 4 * 2) * kBN;
                     if constexpr (kQuant) { if (!(ok = WAIT(kv_full(int((ring_k + 1) % C::kStages)), uint32_t((ring_k + 1) / C::kStages) & 1))) break; }
-                    // 32 columns of S from c0 on: scaled (f = 1 afterwards) where the tile is masked or quantised, raw otherwise
-                    const float f = kQuant || masked ? 1.0f : a.scale_log2;
+                    // the columns [c0, c0 + 32) that this row sees, a bit each
+                    auto visible = [&](int c0) {
+                        const int end = min(max(place - key0 - c0 + 1, 0), 32);                       // columns before `end` are not ahead of the row
+                        uint32_t bits = end == 32 ? ~0u : (1u << end) - 1;
+                        if (a.window) {
+                            const int from = min(max(place - key0 - c0 + 1 - int(a.window), 0), 32);  // columns before `from` have left the window, unless they are sinks
+                            const int sunk = min(max(int(a.sinks) - key0 - c0, 0), 32);
+                            bits &= (from == 32 ? 0u : ~0u << from) | (sunk == 32 ? ~0u : (1u << sunk) - 1);
+                        }
+                        return bits;
+                    };
+                    // 32 columns of S from c0 on, with key scales (which hold the softmax scale) where the cache has them
+                    const float f = kQuant ? 1.0f : a.scale_log2;
+                    const uint32_t kHidden = f < 0.0f ? 0x7f800000u : 0xff800000u;                    // x f = -infinity
                     auto prepare = [&](uint32_t* x, int c0) {
                         if constexpr (kQuant) {
 #pragma unroll
@@ -428,40 +461,37 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                             }
                         }
                         if (masked) {
-                            const int last = place - key0 - c0, before = a.window ? last - int(a.window) : -1, sunk = int(a.sinks) - key0 - c0;
+                            const uint32_t bits = visible(c0);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const bool hidden = e > last || (e <= before && e >= sunk);
-                                x[e] = hidden ? 0xff800000u : kQuant ? x[e] : __float_as_uint(__uint_as_float(x[e]) * a.scale_log2);
-                            }
+                            for (int e = 0; e < 32; ++e) x[e] = bits & (1u << e) ? x[e] : kHidden;
                         }
                     };
-                    float t0 = f < 0.0f ? INFINITY : -INFINITY, t1 = t0, t2 = t0, t3 = t0;
-                    auto extreme = [&](const uint32_t* x) {
-                        auto X = [&](int e) { return __uint_as_float(x[e]); };
+                    // the whole row is in registers for its maximum; its first 32 columns are read again later (tensor memory is cheaper than
+                    // 32 more registers)
+                    uint32_t x0[32], x[96];
+                    tm_ld32(tS, x0);
+#pragma unroll
+                    for (int c0 = 0; c0 < 96; c0 += 32) tm_ld32(tS + 32 + c0, x + c0);
+                    tm_wait_ld32(x0);
+#pragma unroll
+                    for (int c0 = 0; c0 < 96; c0 += 32) tie32(x + c0);
+                    prepare(x0, 0);
+#pragma unroll
+                    for (int c0 = 0; c0 < 96; c0 += 32) prepare(x + c0, 32 + c0);
+                    auto X = [&](int e) { return __uint_as_float(e < 32 ? x0[e] : x[e - 32]); };
+                    float top = m;
+                    if (row_on) {
+                        float t0 = X(0), t1 = X(1), t2 = X(2), t3 = X(3);
                         if (f >= 0.0f) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
-                                t0 = fmaxf(fmaxf(t0, X(e)), X(e + 1)); t1 = fmaxf(fmaxf(t1, X(e + 2)), X(e + 3));
-                                t2 = fmaxf(fmaxf(t2, X(e + 4)), X(e + 5)); t3 = fmaxf(fmaxf(t3, X(e + 6)), X(e + 7));
-                            }
+                            for (int e = 4; e < kBN; e += 4) { t0 = fmaxf(t0, X(e)); t1 = fmaxf(t1, X(e + 1)); t2 = fmaxf(t2, X(e + 2)); t3 = fmaxf(t3, X(e + 3)); }
+                            top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * f;
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) { t0 = fminf(t0, X(e)); t1 = fminf(t1, X(e + 1)); t2 = fminf(t2, X(e + 2)); t3 = fminf(t3, X(e + 3)); }
+                            for (int e = 4; e < kBN; e += 4) { t0 = fminf(t0, X(e)); t1 = fminf(t1, X(e + 1)); t2 = fminf(t2, X(e + 2)); t3 = fminf(t3, X(e + 3)); }
+                            top = fminf(fminf(t0, t1), fminf(t2, t3)) * f;
                         }
-                    };
-                    // the maximum: the first 64 columns are read twice (tensor memory is cheaper than 64 more registers), the others stay
-                    uint32_t xa[32], xb[32];
-                    tm_ld32(tS, xa); tm_ld32(tS + 32, xb);
-                    tm_wait_ld32(xa); tie32(xb);
-                    prepare(xa, 0); extreme(xa);
-                    prepare(xb, 32); extreme(xb);
-                    tm_ld32(tS + 64, xa); tm_ld32(tS + 96, xb);
-                    tm_wait_ld32(xa); tie32(xb);
-                    prepare(xa, 64); extreme(xa);
-                    prepare(xb, 96); extreme(xb);
-                    t0 = f >= 0.0f ? fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * f : fminf(fminf(t0, t1), fminf(t2, t3)) * f;
-                    const float top = row_on ? t0 : m;
+                    }
                     if (__any_sync(0xffffffffu, top > m + C::kLag)) {
                         const float mn = fmaxf(m, top), shrink = ex2(m - mn);
                         if (j > 0) {                            // O so far shrinks too, once the last product into it is done
@@ -481,33 +511,30 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                     }
                     const uint64_t f2 = pack2(f, f), m2 = pack2(-m, -m);
                     uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
-                    auto weights = [&](const uint32_t* x, int c0) {
+                    auto weights = [&](const uint32_t* v, int c0) {
                         uint32_t p[16];
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             float y0, y1;
-                            unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), f2, m2), y0, y1);
+                            unpack2(fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, m2), y0, y1);
                             y0 = ex2(y0); y1 = ex2(y1);
                             const uint64_t y = pack2(y0, y1);
                             if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
                             if constexpr (kQuant) {
                                 unpack2(mul2(y, *reinterpret_cast<const uint64_t*>(ks + kBN + c0 + e)), y0, y1);
-                                if (masked) { y0 = x[e] == 0xff800000u ? 0.0f : y0; y1 = x[e + 1] == 0xff800000u ? 0.0f : y1; }      // a hidden value's scale may be NaN
+                                if (masked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
                             }
                             p[e / 2] = A::pack(y0, y1);
                         }
-                        tm_st16(tS + 64 + c0 / 2, p);           // P lies over the columns of S that are in registers
+                        tm_st16(tS + 64 + c0 / 2, p);           // P lies over columns of S that are in registers
                     };
-                    weights(xa, 64);
-                    tm_ld32(tS, xa);
-                    weights(xb, 96);
-                    tm_wait_ld32(xa);
-                    tm_ld32(tS + 32, xb);
-                    prepare(xa, 0);
-                    weights(xa, 0);
-                    tm_wait_ld32(xb);
-                    prepare(xb, 32);
-                    weights(xb, 32);
+                    weights(x, 32);
+                    tm_ld32(tS, x0);
+                    weights(x + 32, 64);
+                    weights(x + 64, 96);
+                    tm_wait_ld32(x0);
+                    prepare(x0, 0);
+                    weights(x0, 0);
                     float s0, s1;
                     unpack2(add2(sum_a, sum_b), s0, s1);
                     l += s0 + s1;
@@ -540,7 +567,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 tc_after();
             }
             const bool whole = g.t0 == 0 && g.t1 == g.tiles;
-            const long long x0 = begin + g.y - n;
+            const long long x0 = begin + g.from;
             const uint32_t slot = 2 * blockIdx.x + (x0 == begin ? 0 : 1);
             uint8_t* dst = a.out + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.out_stride + (uint64_t(g.h) * G + r % G) * D) * 2;
             if (work) {
