@@ -42,10 +42,16 @@ template <bool BF, int CACHE, int D> struct Cfg {
     static constexpr int kOffRing = 2 * kQ;
     static constexpr int kOffStaging = kOffRing + kStages * kTile;
     static constexpr int kOffScales = kOffStaging + kStaging * kCodes;
-    static constexpr int kOffBars = kOffScales + kScales;
+    static constexpr int kOffExchange = kOffScales + kScales;               // quantised: two floats per row, row tile and half: maximum, sum
+    static constexpr int kOffBars = kOffExchange + (kQuant ? 2 * 4 * kBM * 4 : 0);
     static constexpr int kSmem = kOffBars + 512 + 1024;                     // the rings start at a 1,024-byte boundary
-    static constexpr int kThreads = kQuant ? 448 : 320;
-    static constexpr int kWarpConvert = 8, kWarpMma = kQuant ? 12 : 8, kWarpLoad = kWarpMma + 1;
+    // Threads per row: one where the scores are used as they come; two for a quantised cache, whose scales have to be fetched for every column
+    // (a thread per row, 24 int8 prompts: 0.79 ms, two 0.62; two prompts of 8,192 tokens in 16 bits: 1.03 ms with one, 1.10 with two).
+    static constexpr int kHalves = kQuant ? 2 : 1;
+    static constexpr int kSoftmaxWarps = 8 * kHalves, kConvert = kQuant ? 64 : 0;   // kConvert: threads of the widening warps
+    static constexpr int kWarpConvert = kSoftmaxWarps, kWarpMma = kWarpConvert + kConvert / 32, kWarpLoad = kWarpMma + 1;
+    static constexpr int kThreads = (kWarpLoad + 1) * 32;
+    static constexpr uint32_t kColP = kQuant ? 0 : 64;      // where P lies over S: the columns whose scores are in registers by then
     static constexpr float kLag = !BF && kQuant ? 3.0f : 8.0f;              // f16 weights: 2^lag * lift * 516 (largest value scale) < 65,504
     static constexpr float kLift = !BF && kQuant ? 8.0f : 1.0f;
     static constexpr uint32_t kColS = 0, kColO = 256, kCols = 512;
@@ -152,6 +158,9 @@ struct Walk {
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+// The largest of three (NaN only if all are).
+__device__ __forceinline__ float max3(float a, float b, float c) { float d; asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+
 __device__ __forceinline__ void scale2(uint32_t* x, uint64_t by)
 {
     float y0, y1;
@@ -169,7 +178,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024 - (smem_at(raw) & 1023)) & 1023);
     const uint32_t base = smem_at(smem);
-    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready / PV done per row tile, join
+    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready (its first half, all of it) / PV done per row tile, join, pairs of warps
     const uint32_t bars = base + C::kOffBars;
     auto kv_full = [&](int s) { return bars + 8 * s; };
     auto kv_empty = [&](int s) { return bars + 8 * (C::kStages + s); };
@@ -180,13 +189,15 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     auto s_full = [&](int w) { return q_full + 16 + 8 * w; };
     auto p_full = [&](int w) { return q_full + 32 + 8 * w; };
     auto o_done = [&](int w) { return q_full + 48 + 8 * w; };
-    const uint32_t join = q_full + 64;
-    static_assert(8 * (kRest + 9) <= 400, "barriers fit");
+    auto p_half = [&](int w) { return q_full + 64 + 8 * w; };
+    const uint32_t join = q_full + 80;
+    auto pair_bar = [&](int k) { return q_full + 88 + 8 * k; };
+    static_assert(8 * (kRest + 19) <= 400, "barriers fit");
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [4..] the share's start
     volatile uint32_t* dead = words + 1;
     int* start = reinterpret_cast<int*>(words + 4);                                 // [0] base, [1] sequence, [2] unit
 
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
     const uint32_t Hkv = a.p.n_kv_heads, G = a.group;
     const int tq = kBM / int(G);                                                    // tokens of a row tile
     const Space sp{ 2 * tq, int(a.window), int((a.sinks + kBN - 1) / kBN) };
@@ -223,11 +234,12 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         while (uh - u > 1) { const int mid = (u + uh) >> 1; if (prefix[i] + sp.sum(q, mid) <= per_head) u = mid; else uh = mid; }
         start[0] = int((prefix[i] + sp.sum(q, u)) * Hkv - begin); start[1] = int(i); start[2] = u;
         words[1] = 0;
-        for (int s = 0; s < C::kStages; ++s) { bar_init(kv_full(s), kQuant ? 128 : 1); bar_init(kv_empty(s), 1); }
-        for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), 128); }
+        for (int s = 0; s < C::kStages; ++s) { bar_init(kv_full(s), kQuant ? C::kConvert : 1); bar_init(kv_empty(s), 1); }
+        for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), C::kConvert); }
         bar_init(q_full, 1); bar_init(q_empty, 1);
-        for (int w2 = 0; w2 < 2; ++w2) { bar_init(s_full(w2), 1); bar_init(p_full(w2), 128); bar_init(o_done(w2), 1); }
-        bar_init(join, 256);
+        for (int w2 = 0; w2 < 2; ++w2) { bar_init(s_full(w2), 1); bar_init(p_full(w2), 128 * C::kHalves); bar_init(p_half(w2), 128); bar_init(o_done(w2), 1); }
+        bar_init(join, 256 * C::kHalves);
+        for (int k = 0; k < 8; ++k) bar_init(pair_bar(k), 64);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();                                                                // the share is known, prefix is done with
@@ -238,7 +250,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     tc_before();
     __syncthreads();
     tc_after();
-    const uint32_t tmem = words[0];
+    const uint32_t tmem = __shfl_sync(0xffffffffu, words[0], 0);
 
     // each warp's walk lives in shared memory: its first lane steps it, and it takes no registers from the loops below
     __shared__ Walk walks[C::kThreads / 32];
@@ -266,14 +278,6 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         uint32_t it = 0, seg = 0;
         bool ok = true;
         while (ok && next()) {
-            if (seg && !(ok = WAIT(q_empty, uint32_t(seg - 1) & 1))) break;
-            if (lane == 0) {
-                const uint32_t one = uint32_t(tq) * G * 128 * C::kSlabs;            // bytes of one row tile
-                bar_expect(q_full, g.two(sp) ? 2 * one : one);
-                for (int w = 0; w < (g.two(sp) ? 2 : 1); ++w)
-                    for (int d = 0; d < C::kSlabs; ++d) tma_3d(base + w * C::kQ + d * (kBM * 128), &q_map, d * 64, g.h * int(G), g.q0 + g.tok0(sp) + w * tq, q_full);
-            }
-            ++seg;
             for (int t = g.t0; ok && t < g.t1; ++t) {
                 // a lane per box: the page's row in the pool, or nowhere
                 int row = nowhere;
@@ -297,6 +301,16 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         else tma_2d(base + C::kOffRing + s * C::kTile + lane % kBoxSlabs * (kBN * 128) + b * int(page_tokens) * 128, map, lane % kBoxSlabs * 64, row, full);
                     }
                     ++it;
+                    if (t == g.t0 && kv == 0) {         // the segment's queries go behind its first keys: they wait for the last segment's scores
+                        if (seg && !(ok = WAIT(q_empty, uint32_t(seg - 1) & 1))) break;
+                        if (lane == 0) {
+                            const uint32_t one = uint32_t(tq) * G * 128 * C::kSlabs;            // bytes of one row tile
+                            bar_expect(q_full, g.two(sp) ? 2 * one : one);
+                            for (int w = 0; w < (g.two(sp) ? 2 : 1); ++w)
+                                for (int d = 0; d < C::kSlabs; ++d) tma_3d(base + w * C::kQ + d * (kBM * 128), &q_map, d * 64, g.h * int(G), g.q0 + g.tok0(sp) + w * tq, q_full);
+                        }
+                        ++seg;
+                    }
                 }
             }
         }
@@ -313,29 +327,26 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         uint32_t it = 0, seg = 0;                              // ring items and tiles so far (the parity of p_full goes by tiles of each row tile)
         uint32_t tiles_of[2] = { 0, 0 };
         bool ok = true;
+        const uint32_t one = elect_one();
+        auto commit = [&](uint32_t bar) { tc_commit_one(one, bar); };
         auto scores = [&](int w, int s) {
-            if (lane == 0) {
+            const uint64_t qa = smem_desc(base + w * C::kQ, 16, 1024), kb = smem_desc(base + C::kOffRing + s * C::kTile, 16, 1024);
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t at = k / 4 * (kBM * 128) + k % 4 * 32;
-                    mma_ss(tmem + C::kColS + w * 128, smem_desc(base + w * C::kQ + at, 16, 1024), smem_desc(base + C::kOffRing + s * C::kTile + at, 16, 1024), kDescS, k > 0);
-                }
-                tc_commit(s_full(w));
-            }
-            __syncwarp();
+            for (int k = 0; k < D / 16; ++k)                    // (descriptors count 16 bytes)
+                mma_ss(one, tmem + C::kColS + w * 128, qa + (k / 4 * (kBM * 128) + k % 4 * 32) / 16, kb + (k / 4 * (kBN * 128) + k % 4 * 32) / 16, kDescS, k > 0);
+            commit(s_full(w));
         };
-        auto values = [&](int w, int s, bool add) {
-            if (lane == 0) {
+        // the eight steps of 16 keys, [from, to) in the order in which P is written
+        auto values = [&](int w, int s, bool add, auto from, auto to) {
+            constexpr int order[8] = { 2, 3, 4, 5, 6, 7, 0, 1 };
+            const uint64_t vb = smem_desc(base + C::kOffRing + s * C::kTile, kBN * 128, 1024);
 #pragma unroll
-                for (int k = 0; k < kBN / 16; ++k)
-                    mma_ts(tmem + C::kColO + w * D, tmem + C::kColS + w * 128 + 64 + k * 8, smem_desc(base + C::kOffRing + s * C::kTile + k * 2048, kBN * 128, 1024), kDescO, add || k > 0);
-                tc_commit(o_done(w));
-            }
-            __syncwarp();
+            for (int i = decltype(from)::value; i < decltype(to)::value; ++i)
+                mma_ts(one, tmem + C::kColO + w * D, tmem + C::kColS + w * 128 + C::kColP + order[i] * 8, vb + order[i] * 2048 / 16, kDescO, add || i > 0);
         };
-        auto commit = [&](uint32_t bar) { if (lane == 0) tc_commit(bar); __syncwarp(); };
+        using std::integral_constant;
         while (ok && next()) {
-            const int nw = g.two(sp) ? 2 : 1, n = g.t1 - g.t0;
+            const int nw = __shfl_sync(0xffffffffu, g.two(sp) ? 2 : 1, 0), n = __shfl_sync(0xffffffffu, g.t1 - g.t0, 0);
             if (!(ok = WAIT(q_full, uint32_t(seg) & 1))) break;
             if (!(ok = WAIT(kv_full(int(it % C::kStages)), uint32_t(it / C::kStages) & 1))) break;
             tc_after();
@@ -345,10 +356,16 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 const uint32_t iv = it + 1, ik = it + 2;
                 if (!(ok = WAIT(kv_full(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
                 for (int w = 0; ok && w < nw; ++w) {
+                    if constexpr (!kQuant) {                    // the first half of P is worked on while the second is made
+                        if (!(ok = WAIT(p_half(w), uint32_t(tiles_of[w]) & 1))) break;
+                        tc_after();
+                        values(w, int(iv % C::kStages), j > 0, integral_constant<int, 0>(), integral_constant<int, 4>());
+                    }
                     if (!(ok = WAIT(p_full(w), uint32_t(tiles_of[w]) & 1))) break;
                     tc_after();
                     ++tiles_of[w];
-                    values(w, int(iv % C::kStages), j > 0);
+                    values(w, int(iv % C::kStages), j > 0, integral_constant<int, kQuant ? 0 : 4>(), integral_constant<int, 8>());
+                    commit(o_done(w));
                     if (j + 1 < n) {
                         if (w == 0 && !(ok = WAIT(kv_full(int(ik % C::kStages)), uint32_t(ik / C::kStages) & 1))) break;
                         scores(w, int(ik % C::kStages));
@@ -363,25 +380,29 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             }
             ++seg;
         }
-    } else if (kQuant && warp >= C::kWarpConvert && warp < C::kWarpConvert + 4) {
+    } else if (kQuant && warp >= C::kWarpConvert && warp < C::kWarpMma) {
         // ---- widening: codes of a staged tile to the operand layout, scales beside them ----
         if constexpr (kQuant) {
-            const int t128 = tid - C::kWarpConvert * 32;
+            const int t = tid - C::kWarpConvert * 32;
             constexpr int kChunks = D / 16;                     // 16 codes each
             uint32_t it = 0;
             bool ok = true;
             while (ok && next()) {
-                for (int t = g.t0; ok && t < g.t1; ++t) {
-                    const int key0 = g.tile_key(t);
+                for (int tile = g.t0; ok && tile < g.t1; ++tile) {
+                    const int key0 = g.tile_key(tile);
                     auto seen = [&](int key) { return key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)); };
-                    // this thread's key's scales
-                    float scale[2] = { 0.0f, 0.0f };
-                    if (seen(key0 + t128)) {
-                        const int key = key0 + t128;
-                        const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
-                        if (page < a.p.n_pages) {
-                            const uint64_t cell = ((uint64_t(page) * Hkv + uint32_t(g.h)) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1));
-                            scale[0] = __ldg(a.p.k_scale + cell); scale[1] = __ldg(a.p.v_scale + cell);
+                    // this thread's keys' scales
+                    float scale[2][kBN / C::kConvert];
+#pragma unroll
+                    for (int e = 0; e < kBN / C::kConvert; ++e) {
+                        scale[0][e] = scale[1][e] = 0.0f;
+                        const int key = key0 + t + e * C::kConvert;
+                        if (seen(key)) {
+                            const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
+                            if (page < a.p.n_pages) {
+                                const uint64_t cell = ((uint64_t(page) * Hkv + uint32_t(g.h)) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1));
+                                scale[0][e] = __ldg(a.p.k_scale + cell); scale[1][e] = __ldg(a.p.v_scale + cell);
+                            }
                         }
                     }
 #pragma unroll
@@ -391,9 +412,9 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         if (it >= C::kStages && !(ok = WAIT(kv_empty(s), uint32_t(it / C::kStages - 1) & 1))) break;
                         const uint8_t* from = smem + C::kOffStaging + ss * C::kCodes;
                         uint8_t* to = smem + C::kOffRing + s * C::kTile;
-#pragma unroll
-                        for (int e = 0; e < kChunks; ++e) {
-                            const int c = t128 % kChunks, r = t128 / kChunks + e * (128 / kChunks);
+#pragma unroll 4
+                        for (int e = 0; e < kChunks * (kBN / C::kConvert); ++e) {
+                            const int c = t % kChunks, r = t / kChunks + e * (C::kConvert / kChunks);
                             uint4 x = *reinterpret_cast<const uint4*>(from + r * D + c * 16);
                             if (!seen(key0 + r)) x = make_uint4(0, 0, 0, 0);
                             const uint4 lo = make_uint4(widen<BF, CACHE>(x.x & 0xffffu), widen<BF, CACHE>(x.x >> 16), widen<BF, CACHE>(x.y & 0xffffu), widen<BF, CACHE>(x.y >> 16));
@@ -404,7 +425,8 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                             else { *reinterpret_cast<uint4*>(row + p1) = hi; *reinterpret_cast<uint4*>(row + p0) = lo; }   // the other order: no bank twice
                         }
                         float* sc = reinterpret_cast<float*>(smem + C::kOffScales) + ((it / 2) % 4 * 2 + kv) * kBN;
-                        sc[t128] = kv ? scale[1] * C::kLift : scale[0] * a.scale_log2;
+#pragma unroll
+                        for (int e = 0; e < kBN / C::kConvert; ++e) sc[t + e * C::kConvert] = kv ? scale[1][e] * C::kLift : scale[0][e] * a.scale_log2;
                         fence_async_proxy();
                         bar_arrive(kv_full(s));
                         bar_arrive(st_empty(ss));
@@ -413,12 +435,17 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 }
             }
         }
-    } else if (warp < 8) {
-        // ---- softmax of one row tile, a row per thread ----
-        const int w = warp / 4, r = tid % 128;
+    } else if (warp < C::kSoftmaxWarps) {
+        // ---- softmax of one row tile: kHalves threads per row, kCols columns each ----
+        constexpr int kCols = kBN / C::kHalves;
+        const int w = warp / (4 * C::kHalves), half = warp / 4 % C::kHalves, r = tid % 128;
         const uint32_t lanes = uint32_t(warp % 4 * 32) << 16;
-        const uint32_t tS = tmem + C::kColS + w * 128 + lanes, tO = tmem + C::kColO + w * D + lanes;
-        uint32_t it = 0, n_done = 0, joins = 0;             // tiles of the block (ring items / 2), tiles of this row tile, joins
+        const uint32_t tS = tmem + C::kColS + w * 128 + half * kCols + lanes, tP = tmem + C::kColS + w * 128 + C::kColP + half * kCols / 2 + lanes;
+        const uint32_t tO = tmem + C::kColO + w * D + half * (D / C::kHalves) + lanes;
+        const uint32_t pair = pair_bar(w * 4 + warp % 4);                     // the two warps that share 32 rows
+        float* mine = reinterpret_cast<float*>(smem + C::kOffExchange) + (w * 2 + half) * kBM + r;
+        const float* theirs = reinterpret_cast<float*>(smem + C::kOffExchange) + (w * 2 + (half ^ 1)) * kBM + r;
+        uint32_t it = 0, n_done = 0, joins = 0, pairs = 0;   // tiles of the block (ring items / 2), tiles of this row tile, joins, exchanges
         bool ok = true;
         while (ok && next()) {
             const int n = g.t1 - g.t0;
@@ -431,74 +458,77 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             float m = kLow, l = 0.0f;
             if (work) {
                 for (int j = 0; j < n; ++j) {
-                    const int key0 = g.tile_key(g.t0 + j);
-                    const uint32_t ring_k = 2 * (it + j);
-                    if (!(ok = WAIT(s_full(w), uint32_t(n_done) & 1))) break;
+                    const int key0 = g.tile_key(g.t0 + j), first = key0 + half * kCols;
+                    const uint32_t iv = 2 * (it + j) + 1;                    // ring item of the tile's values
+                    if (!(ok = WAIT(s_full(w), n_done & 1))) break;
                     tc_after();
                     const bool masked = key0 + kBN - 1 > place_a || (a.window && key0 < place_b - int(a.window) + 1 && key0 + kBN > int(a.sinks));
-                    const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + ((it + j) % 4 * 2) * kBN;
-                    if constexpr (kQuant) { if (!(ok = WAIT(kv_full(int((ring_k + 1) % C::kStages)), uint32_t((ring_k + 1) / C::kStages) & 1))) break; }
-                    // the columns [c0, c0 + 32) that this row sees, a bit each
+                    const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + ((it + j) % 4 * 2) * kBN + half * kCols;
+                    if constexpr (kQuant) { if (!(ok = WAIT(kv_full(int(iv % C::kStages)), (iv / C::kStages) & 1))) break; }     // both scales are there
+                    // the columns [c0, c0 + 32) of this thread that the row sees, a bit each
                     auto visible = [&](int c0) {
-                        const int end = min(max(place - key0 - c0 + 1, 0), 32);                       // columns before `end` are not ahead of the row
+                        const int end = min(max(place - first - c0 + 1, 0), 32);                       // columns before `end` are not ahead of the row
                         uint32_t bits = end == 32 ? ~0u : (1u << end) - 1;
                         if (a.window) {
-                            const int from = min(max(place - key0 - c0 + 1 - int(a.window), 0), 32);  // columns before `from` have left the window, unless they are sinks
-                            const int sunk = min(max(int(a.sinks) - key0 - c0, 0), 32);
+                            const int from = min(max(place - first - c0 + 1 - int(a.window), 0), 32);  // columns before `from` have left the window, unless they are sinks
+                            const int sunk = min(max(int(a.sinks) - first - c0, 0), 32);
                             bits &= (from == 32 ? 0u : ~0u << from) | (sunk == 32 ? ~0u : (1u << sunk) - 1);
                         }
                         return bits;
                     };
-                    // 32 columns of S from c0 on, with key scales (which hold the softmax scale) where the cache has them
                     const float f = kQuant ? 1.0f : a.scale_log2;
                     const uint32_t kHidden = f < 0.0f ? 0x7f800000u : 0xff800000u;                    // x f = -infinity
-                    auto prepare = [&](uint32_t* x, int c0) {
+                    // 32 columns: times the key scales (which hold the softmax scale) where the cache has them, hidden ones put away
+                    auto prepare = [&](uint32_t* v, int c0) {
                         if constexpr (kQuant) {
 #pragma unroll
                             for (int e = 0; e < 32; e += 4) {
                                 const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(ks + c0 + e);
-                                scale2(x + e, k4.x); scale2(x + e + 2, k4.y);
+                                scale2(v + e, k4.x); scale2(v + e + 2, k4.y);
                             }
                         }
-                        if (masked) {
+                        if (masked) {                            // (the same for the whole warp)
                             const uint32_t bits = visible(c0);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = bits & (1u << e) ? x[e] : kHidden;
+                            for (int e = 0; e < 32; ++e) v[e] = bits & (1u << e) ? v[e] : kHidden;
                         }
                     };
-                    // the whole row is in registers for its maximum; its first 32 columns are read again later (tensor memory is cheaper than
-                    // 32 more registers)
-                    uint32_t x0[32], x[96];
+                    uint32_t x0[32], x[kCols - 32];
                     tm_ld32(tS, x0);
 #pragma unroll
-                    for (int c0 = 0; c0 < 96; c0 += 32) tm_ld32(tS + 32 + c0, x + c0);
+                    for (int c0 = 32; c0 < kCols; c0 += 32) tm_ld32(tS + c0, x + c0 - 32);
                     tm_wait_ld32(x0);
 #pragma unroll
-                    for (int c0 = 0; c0 < 96; c0 += 32) tie32(x + c0);
+                    for (int c0 = 32; c0 < kCols; c0 += 32) tie32(x + c0 - 32);
                     prepare(x0, 0);
 #pragma unroll
-                    for (int c0 = 0; c0 < 96; c0 += 32) prepare(x + c0, 32 + c0);
+                    for (int c0 = 32; c0 < kCols; c0 += 32) prepare(x + c0 - 32, c0);
                     auto X = [&](int e) { return __uint_as_float(e < 32 ? x0[e] : x[e - 32]); };
-                    float top = m;
-                    if (row_on) {
-                        float t0 = X(0), t1 = X(1), t2 = X(2), t3 = X(3);
-                        if (f >= 0.0f) {
+                    float top, t0 = X(0), t1 = X(1), t2 = X(2), t3 = X(3);
+                    if (f >= 0.0f) {
 #pragma unroll
-                            for (int e = 4; e < kBN; e += 4) { t0 = fmaxf(t0, X(e)); t1 = fmaxf(t1, X(e + 1)); t2 = fmaxf(t2, X(e + 2)); t3 = fmaxf(t3, X(e + 3)); }
-                            top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * f;
-                        } else {
+                        for (int e = 0; e < kCols; e += 8) { t0 = max3(t0, X(e), X(e + 1)); t1 = max3(t1, X(e + 2), X(e + 3)); t2 = max3(t2, X(e + 4), X(e + 5)); t3 = max3(t3, X(e + 6), X(e + 7)); }
+                        top = fmaxf(max3(t0, t1, t2), t3) * f;
+                    } else {
 #pragma unroll
-                            for (int e = 4; e < kBN; e += 4) { t0 = fminf(t0, X(e)); t1 = fminf(t1, X(e + 1)); t2 = fminf(t2, X(e + 2)); t3 = fminf(t3, X(e + 3)); }
-                            top = fminf(fminf(t0, t1), fminf(t2, t3)) * f;
-                        }
+                        for (int e = 4; e < kCols; e += 4) { t0 = fminf(t0, X(e)); t1 = fminf(t1, X(e + 1)); t2 = fminf(t2, X(e + 2)); t3 = fminf(t3, X(e + 3)); }
+                        top = fminf(fminf(t0, t1), fminf(t2, t3)) * f;
                     }
+                    if constexpr (C::kHalves == 2) {
+                        *mine = top;
+                        bar_arrive(pair);
+                        if (!(ok = WAIT(pair, pairs & 1))) break;
+                        ++pairs;
+                        top = fmaxf(top, *theirs);
+                    }
+                    if (!row_on) top = m;
                     if (__any_sync(0xffffffffu, top > m + C::kLag)) {
                         const float mn = fmaxf(m, top), shrink = ex2(m - mn);
-                        if (j > 0) {                            // O so far shrinks too, once the last product into it is done
-                            if (!(ok = WAIT(o_done(w), uint32_t(n_done - 1) & 1))) break;
+                        if (j > 0) {                            // O so far shrinks too, once the last product into it is done; each thread takes its share of the columns
+                            if (!(ok = WAIT(o_done(w), (n_done - 1) & 1))) break;
                             tc_after();
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 16) {
+                            for (int c0 = 0; c0 < D / C::kHalves; c0 += 16) {
                                 uint32_t v[16];
                                 tm_ld16(tO + c0, v);
                                 tm_wait_ld16(v);
@@ -508,6 +538,21 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                             }
                         }
                         l *= shrink; m = mn;
+                    }
+                    if constexpr (!kQuant) {
+                        // values that no row of the unit sees are zeroed in shared memory: a weight of 0 does not silence a NaN
+                        const bool edge = key0 + kBN > g.hi || (a.window && key0 < g.lo && key0 + kBN > int(a.sinks));
+                        if (edge && w == 0) {
+                            if (!(ok = WAIT(kv_full(int(iv % C::kStages)), (iv / C::kStages) & 1))) break;
+                            const int key = key0 + r;
+                            if (!(key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)))) {
+                                for (int d = 0; d < C::kSlabs; ++d)
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e)
+                                        *reinterpret_cast<uint4*>(smem + C::kOffRing + int(iv % C::kStages) * C::kTile + d * (kBN * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_async_proxy();
+                        }
                     }
                     const uint64_t f2 = pack2(f, f), m2 = pack2(-m, -m);
                     uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
@@ -521,39 +566,33 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                             const uint64_t y = pack2(y0, y1);
                             if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
                             if constexpr (kQuant) {
-                                unpack2(mul2(y, *reinterpret_cast<const uint64_t*>(ks + kBN + c0 + e)), y0, y1);
+                                const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(ks + kBN + c0 + e / 4 * 4);
+                                unpack2(mul2(y, e % 4 ? v4.y : v4.x), y0, y1);
                                 if (masked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
                             }
                             p[e / 2] = A::pack(y0, y1);
                         }
-                        tm_st16(tS + 64 + c0 / 2, p);           // P lies over columns of S that are in registers
+                        tm_st16(tP + c0 / 2, p);
                     };
-                    weights(x, 32);
-                    tm_ld32(tS, x0);
-                    weights(x + 32, 64);
-                    weights(x + 64, 96);
-                    tm_wait_ld32(x0);
-                    prepare(x0, 0);
-                    weights(x0, 0);
+                    if constexpr (C::kHalves == 1) {
+                        // the first 32 columns were dropped after the maximum and are read again (tensor memory is cheaper than 32 more registers)
+                        weights(x, 32);
+                        tm_ld32(tS, x0);
+                        weights(x + 32, 64);
+                        tm_wait_st();
+                        tc_before();
+                        bar_arrive(p_half(w));
+                        weights(x + 64, 96);
+                        tm_wait_ld32(x0);
+                        prepare(x0, 0);
+                        weights(x0, 0);
+                    } else {
+                        weights(x0, 0);
+                        weights(x, 32);
+                    }
                     float s0, s1;
                     unpack2(add2(sum_a, sum_b), s0, s1);
                     l += s0 + s1;
-                    if constexpr (!kQuant) {
-                        // values that no row of the unit sees are zeroed in shared memory: a weight of 0 does not silence a NaN
-                        const bool edge = key0 + kBN > g.hi || (a.window && key0 < g.lo && key0 + kBN > int(a.sinks));
-                        if (edge && w == 0) {
-                            const uint32_t iv = ring_k + 1;
-                            if (!(ok = WAIT(kv_full(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
-                            const int key = key0 + r;
-                            if (!(key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)))) {
-                                for (int d = 0; d < C::kSlabs; ++d)
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e)
-                                        *reinterpret_cast<uint4*>(smem + C::kOffRing + int(iv % C::kStages) * C::kTile + d * (kBN * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
-                            }
-                            fence_async_proxy();
-                        }
-                    }
                     tm_wait_st();
                     tc_before();
                     bar_arrive(p_full(w));
@@ -563,17 +602,24 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             if (!ok) break;
             it += n;
             if (work) {
+                if constexpr (C::kHalves == 2) {
+                    mine[4 * kBM] = l;                          // the row's sum is that of both halves
+                    bar_arrive(pair);
+                    if (!(ok = WAIT(pair, pairs & 1))) break;
+                    ++pairs;
+                    l = half ? theirs[4 * kBM] + l : l + theirs[4 * kBM];
+                }
                 if (!(ok = WAIT(o_done(w), uint32_t(n_done - 1) & 1))) break;
                 tc_after();
             }
             const bool whole = g.t0 == 0 && g.t1 == g.tiles;
             const long long x0 = begin + g.from;
             const uint32_t slot = 2 * blockIdx.x + (x0 == begin ? 0 : 1);
-            uint8_t* dst = a.out + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.out_stride + (uint64_t(g.h) * G + r % G) * D) * 2;
+            uint8_t* dst = a.out + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.out_stride + (uint64_t(g.h) * G + r % G) * D + half * (D / C::kHalves)) * 2;
             if (work) {
                 const float inv = l > 0.0f ? (1.0f / C::kLift) / l : l;
-#pragma unroll 1
-                for (int c0 = 0; c0 < D; c0 += 32) {
+#pragma unroll
+                for (int c0 = 0; c0 < D / C::kHalves; c0 += 32) {
                     uint32_t v[32];
                     tm_ld32(tO + c0, v);
                     tm_wait_ld32(v);
@@ -588,13 +634,13 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                             }
                         }
                     } else if (row_on) {
-                        float4* part = reinterpret_cast<float4*>(a.s.part_o) + (uint64_t(slot) * 2 + w) * (D / 4) * kBM + r;      // [slot][row tile][D / 4][128] float4
+                        float4* part = reinterpret_cast<float4*>(a.s.part_o) + ((uint64_t(slot) * 2 + w) * (D / 4) + half * (D / 4 / C::kHalves)) * kBM + r;      // [slot][row tile][D / 4][128] float4
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             part[(c0 / 4 + e) * kBM] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
                     }
                 }
-                if (!whole && row_on) a.s.part_ml[(slot * 2 + w) * kBM + r] = make_float2(m, l);
+                if (!whole && row_on && half == 0) a.s.part_ml[(slot * 2 + w) * kBM + r] = make_float2(m, l);
                 tc_before();
             }
             if (!whole) {
@@ -614,26 +660,28 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 if (words[2]) {
                     __threadfence();
                     if (row_on && work) {
-                        float mm = kLow;
-                        for (uint32_t b = blk0; b <= blk1; ++b) mm = fmaxf(mm, __ldcg(a.s.part_ml + ((b == blk0 ? first_slot : 2 * b) * 2 + w) * kBM + r).x);
-                        float ll = 0.0f;
-                        for (uint32_t b = blk0; b <= blk1; ++b) { const float2 ml = __ldcg(a.s.part_ml + ((b == blk0 ? first_slot : 2 * b) * 2 + w) * kBM + r); ll += ml.y * ex2(ml.x - mm); }
-                        const float inv = ll > 0.0f ? (1.0f / C::kLift) / ll : ll;
-#pragma unroll 1
-                        for (int d4 = 0; d4 < D / 4; d4 += 2) {
-                            float o[8];
+                        float4 acc[D / 4 / C::kHalves];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-                            for (uint32_t b = blk0; b <= blk1; ++b) {
-                                const uint32_t s = (b == blk0 ? first_slot : 2 * b) * 2 + w;
-                                const float e0 = ex2(__ldcg(a.s.part_ml + s * kBM + r).x - mm);
-                                const float4* part = reinterpret_cast<const float4*>(a.s.part_o) + uint64_t(s) * (D / 4) * kBM + r;
-                                const float4 p = __ldcg(part + d4 * kBM), q = __ldcg(part + (d4 + 1) * kBM);
-                                o[0] += p.x * e0; o[1] += p.y * e0; o[2] += p.z * e0; o[3] += p.w * e0;
-                                o[4] += q.x * e0; o[5] += q.y * e0; o[6] += q.z * e0; o[7] += q.w * e0;
+                        for (int e = 0; e < D / 4 / C::kHalves; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        float mm = kLow, ll = 0.0f;
+                        for (uint32_t b = blk0; b <= blk1; ++b) {
+                            const uint32_t s = (b == blk0 ? first_slot : 2 * b) * 2 + w;
+                            const float2 ml = __ldcg(a.s.part_ml + s * kBM + r);
+                            const float4* part = reinterpret_cast<const float4*>(a.s.part_o) + (uint64_t(s) * (D / 4) + half * (D / 4 / C::kHalves)) * kBM + r;
+                            const float mn = fmaxf(mm, ml.x), f0 = ex2(mm - mn), f1 = ex2(ml.x - mn);
+                            mm = mn; ll = ll * f0 + ml.y * f1;
+#pragma unroll
+                            for (int e = 0; e < D / 4 / C::kHalves; ++e) {           // the loads of a part do not depend on one another
+                                const float4 v = __ldcg(part + e * kBM);
+                                acc[e].x = acc[e].x * f0 + v.x * f1; acc[e].y = acc[e].y * f0 + v.y * f1;
+                                acc[e].z = acc[e].z * f0 + v.z * f1; acc[e].w = acc[e].w * f0 + v.w * f1;
                             }
-                            *reinterpret_cast<uint4*>(dst + d4 * 8) = make_uint4(A::pack(o[0] * inv, o[1] * inv), A::pack(o[2] * inv, o[3] * inv), A::pack(o[4] * inv, o[5] * inv), A::pack(o[6] * inv, o[7] * inv));
                         }
+                        const float inv = ll > 0.0f ? (1.0f / C::kLift) / ll : ll;
+#pragma unroll
+                        for (int e = 0; e < D / 4 / C::kHalves; e += 2)
+                            *reinterpret_cast<uint4*>(dst + e * 8) = make_uint4(A::pack(acc[e].x * inv, acc[e].y * inv), A::pack(acc[e].z * inv, acc[e].w * inv),
+                                                                                A::pack(acc[e + 1].x * inv, acc[e + 1].y * inv), A::pack(acc[e + 1].z * inv, acc[e + 1].w * inv));
                     }
                     if (tid == 0) a.s.ticket[first_slot] = 0;
                 }
