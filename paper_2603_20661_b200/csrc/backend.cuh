@@ -48,15 +48,15 @@ struct ShapeArgs {
     uint32_t* err;
 };
 
-constexpr uint32_t kDecodeSlots = 2 * 148 * 4;      // partial results of the row kernel: two per block of its largest grid
-constexpr uint32_t kDecodeRows = 16;
+constexpr uint32_t kDecodeSlots = 2 * 148 * 2;      // partial results of the row kernel: two per block of its largest grid
+constexpr uint32_t kDecodeRows = 32;                 // most rows of its units
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 
 cudaError_t launch_cache_append(const SeqBatch& b, const Pages& p, const void* k, uint64_t k_stride, const void* v, uint64_t v_stride,
                                 uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
 cudaError_t launch_cache_read(const SeqBatch& b, const Pages& p, const int32_t* row_start, uint64_t n_rows, void* k_out, void* v_out,
                               uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
-cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
+cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_attend_tile(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s);
 uint32_t shape_slice(uint32_t n_rows, uint32_t vocab);

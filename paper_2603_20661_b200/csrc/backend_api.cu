@@ -221,14 +221,15 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
     a.window = window < batch->max_kv_len ? window : 0;          // one that hides nothing is none
     a.sinks = sinks < batch->max_kv_len ? sinks : batch->max_kv_len;
     a.err = b->err;
-    // Sequences go by their rows per kv head (new tokens * group): up to 16, one tile of the row kernel, are bound by the cache's bytes; above
-    // that the tile kernel's 128-row tiles.  Both run only where the host's counts allow both kinds.
+    // Sequences go by their rows per kv head (new tokens * group): up to 32 are bound by the cache's bytes and go to the row kernel, above that
+    // the tile kernel's 128-row tiles.  Both run only where the host's counts allow both kinds; the short sequences are then taken to have one new token.
     a.few_rows = kDecodeRows;
-    const bool many = uint64_t(batch->max_q_len) * a.group > a.few_rows;
+    const uint64_t most = uint64_t(batch->max_q_len) * a.group;
+    const bool many = most > a.few_rows;
     const bool few = !many || uint64_t(batch->n_tokens) != uint64_t(batch->n_seqs) * batch->max_q_len;
     cudaError_t e = cudaSuccess;
     if (many) e = launch_attend_tile(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
-    if (e == cudaSuccess && few) e = launch_attend_rows(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+    if (e == cudaSuccess && few) e = launch_attend_rows(a, many ? a.group : uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
     return launched(b, e, "wwws_attend");
 }
 

@@ -1,21 +1,25 @@
 // Attention of few rows per kv head over the paged cache (single tokens, a few drafted tokens).
 //
 // out_r = sum_j 2^(x_rj - m_r) v_j / sum_j 2^(x_rj - m_r),  x = scale * log2(e) * q_r . k_j,  m_r = max_j x_rj, computed in one pass over
-// the keys with a running maximum and sum.  The query heads that share a kv head, times the sequence's new tokens, are the rows of one
-// 16-row tile, so a key is read once for all of them.  Bound by HBM: a key and its value are head_dim * 2 (or 1) * 2 bytes for
-// 4 * head_dim * rows operations, two orders of magnitude below the tensor peak, so the warp-level mma.sync does: what matters
-// is how many bytes are in flight.
+// the keys with a running maximum and sum.  The query heads that share a kv head, times the sequence's new tokens, are the rows of one unit, so a
+// key is read once for all of them.  Bound by HBM: a key and its value are head_dim * 2 (or 1) * 2 bytes for 4 * head_dim * rows operations, two
+// orders of magnitude below the tensor peak, so the warp-level mma.sync does: what matters is how many bytes are in flight and how few instructions
+// each costs.
+//   - Keys are the 16 rows of the operand, query rows its 8 columns (S^T = K Q^T, O^T = V^T P^T): no half-empty 16-row tile of queries, and
+//     kGroups = 1, 2 or 4 groups of 8 rows share the fragments of a key.
 //   - Work is cut by keys, not by sequences: all (sequence, row tile, kv head) units laid end to end in tiles of kTK keys, and block i takes
 //     the i-th equal share (the lengths are read on the device: no plan, no host copy of them).  A unit cut by a share boundary leaves a
 //     partial result (m, sum, weighted values) in the workspace; the last of its blocks to arrive joins them in block order,
 //     so the result does not depend on who arrives last.
 //   - Within a block the warps take every fourth tile of a segment, each with its own ring of cp.async stages (no block barrier
 //     inside a segment), and join through shared memory at its end.
-//   - A quantised tile is widened in registers on its way into the tensor operand; its scales multiply the score (keys) and the
-//     softmax weight (values), so the codes themselves, which 16-bit floats hold exactly, are the operands.
-// Fragments: mma.m16n8k16 leaves the order of the k index free as long as both operands agree.  For q.k a thread takes 16 consecutive bytes of
+//   - A quantised tile is widened in registers on its way into the operand; its scales multiply the score (keys) and the softmax weight
+//     (values), so the codes themselves, which f16 holds exactly, are the operands, whatever the activation type: bf16 queries become f16 by a
+//     power of two per row (exact down to 2^-28 of the row's largest), and weights times value scales are kept relative to the largest value
+//     scale so far.  Weights in f16 carry a factor 2^15, which cancels in the quotient and keeps small ones out of the subnormals.
+// Fragments: mma.m16n8k16 leaves the order of the k index free as long as both operands agree.  For K Q^T a thread takes 16 consecutive bytes of
 // its key's row (8 or 16 elements = 2 or 4 k-steps) and the query fragments follow that order; for 8-bit values, where no transposing load
-// fits, a thread takes head_dim / 8 consecutive columns of four keys' rows and n-tile i is column i of each thread's.
+// fits, a thread takes head_dim / 8 consecutive columns of four keys' rows and row tile i of V^T is columns 2i and 2i + 1 of each thread's.
 #include "backend.cuh"
 
 namespace wwws {
@@ -27,14 +31,14 @@ constexpr float kLow = -3.0e38f;            // below every score: 2^(x - kLow) i
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-template <bool BF> __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+template <bool BF> __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b)[2])
 {
     if constexpr (BF)
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
     else
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on)     // 16 bytes, or zeros
@@ -44,6 +48,18 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on)    
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool on)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(on ? 4 : 0) : "memory");
+}
+
+// Four codes to two pairs of f16: int8 by 0x6400 | (code ^ 0x80), which is 1024 + 128 + code, less 1152; e4m3 by the hardware's conversion.
+template <int CACHE> __device__ __forceinline__ void widen4(uint32_t four, uint32_t& lo, uint32_t& hi)
+{
+    if constexpr (CACHE == WWWS_CACHE_INT8) {
+        const uint32_t u = four ^ 0x80808080u;
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(__byte_perm(u, 0x64646464u, 0x4140)), "r"(0x64806480u));
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(__byte_perm(u, 0x64646464u, 0x4342)), "r"(0x64806480u));
+    } else {
+        asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}" : "=r"(lo), "=r"(hi) : "r"(four));
+    }
 }
 
 template <int CACHE, int D> struct Shape {
@@ -74,14 +90,16 @@ template <int TK> __device__ __forceinline__ Span span_of(int q_len, int kv, uin
     return s;
 }
 
-template <bool BF, int CACHE, int D>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendArgs a)
+template <bool BF, int CACHE, int D, int kGroups>
+__global__ void __launch_bounds__(kThreads, kGroups == 4 ? 1 : kBlocksPerSM) k_attend_rows(AttendArgs a)
 {
-    using A = Act<BF>;
-    using S = Shape<CACHE, D>;
-    constexpr int TK = S::kTK, NT = TK / 8, KT = TK / 16;
     constexpr bool kQuant = CACHE != WWWS_CACHE_16;
-    constexpr float kLift = kQuant && !BF ? 64.0f : 1.0f;    // keeps f16 weights times small value scales out of the subnormals (a scale of f16 values is at most 516, so the product stays finite)
+    constexpr bool kB = BF && !kQuant;                       // the operands' type
+    using A = Act<BF>;
+    using W = Act<kB>;
+    using S = Shape<CACHE, D>;
+    constexpr int TK = S::kTK, KT = TK / 16, kRows = 8 * kGroups;
+    constexpr float kLift = kB ? 0.0f : 15.0f;               // log2 of the weights' common factor
     extern __shared__ __align__(128) uint8_t smem[];
     unsigned long long* prefix = reinterpret_cast<unsigned long long*>(smem + S::kSmem);   // [n_seqs + 1] tiles of all earlier sequences, per kv head
     __shared__ unsigned long long warp_sum[kWarps];
@@ -96,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
         if (base + tid < a.b.n_seqs) {
             int q0, q_len, kv;
             if (sequence(a.b, base + tid, q0, q_len, kv, a.err) && q_len && uint32_t(q_len) * G <= a.few_rows)
-                x = (unsigned long long)((uint32_t(q_len) * G + kDecodeRows - 1) / kDecodeRows) * span_of<TK>(q_len, kv, a.window, a.sinks).tiles;
+                x = (unsigned long long)((uint32_t(q_len) * G + kRows - 1) / kRows) * span_of<TK>(q_len, kv, a.window, a.sinks).tiles;
         }
         const unsigned long long own = x;
 #pragma unroll
@@ -118,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
     const uint32_t ring = uint32_t(__cvta_generic_to_shared(smem)) + warp * S::kRing;
     const uint8_t* ring_g = smem + warp * S::kRing;
     float* comb_o = reinterpret_cast<float*>(smem);                                   // [kWarps][16][D], over the drained rings
-    float2* comb_ml = reinterpret_cast<float2*>(comb_o + kWarps * kDecodeRows * D);   // [kWarps][16]
+    float2* comb_ml = reinterpret_cast<float2*>(comb_o + kWarps * kRows * D);   // [kWarps][16]
 
     for (unsigned long long x = begin; x < end;) {
         // the segment: unit (sequence i, row tile r, kv head h), its tiles [t0, t1)
@@ -131,33 +149,54 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
         const uint32_t unit = uint32_t(rel / uint32_t(sp.tiles));
         const int t0 = int(rel - (unsigned long long)unit * uint32_t(sp.tiles));
         const int t1 = int(min((unsigned long long)sp.tiles, t0 + (end - x)));
-        const uint32_t h = unit % Hkv, row0 = unit / Hkv * kDecodeRows;
-        const int n_rows = min(int(kDecodeRows), q_len * int(G) - int(row0));
+        const uint32_t h = unit % Hkv, row0 = unit / Hkv * kRows;
+        const int n_rows = min(int(kRows), q_len * int(G) - int(row0));
         const int place0 = kv - q_len;                                   // place of the sequence's first new token
         const int first_place = place0 + int(row0 / G), last_place = place0 + int((row0 + n_rows - 1) / G);
         const int lo_key = a.window ? max(0, first_place - int(a.window) + 1) : 0, hi_key = min(kv, last_place + 1);
 
-        // query fragments, in the order in which the keys' chunks are taken
-        uint32_t qa[D / 16][4];
-        {
-            const int ra = n, rb = n + 8;
-            auto at = [&](int r) { return reinterpret_cast<const uint4*>(a.q + (uint64_t(q0 + int((row0 + r) / G)) * a.q_stride + (uint64_t(h) * G + (row0 + r) % G) * D) * 2); };
-            constexpr int kPer = kQuant ? 2 : 1;         // 8-element pieces of a thread's chunk
+        // Query fragments (columns are rows n + 8 g), in the order in which the keys' chunks are taken.  Quantised: f16 times 2^e of the row, whose
+        // largest element then lies in [2^14, 2^15); rm is what turns a product into x.
+        uint32_t qb[kGroups][D / 16][2];
+        float rm[kGroups][2];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int r = n + 8 * g;
+            const uint4* from = reinterpret_cast<const uint4*>(a.q + (uint64_t(q0 + int((row0 + min(r, n_rows - 1)) / G)) * a.q_stride + (uint64_t(h) * G + (row0 + min(r, n_rows - 1)) % G) * D) * 2);
 #pragma unroll
             for (int s = 0; s < D / 32; ++s) {
-                const int piece = kQuant ? (4 * (s / 2) + c) * kPer + s % 2 : 4 * s + c;
-                const uint4 z = make_uint4(0, 0, 0, 0);
-                const uint4 u = ra < n_rows ? __ldg(at(ra) + piece) : z, w = rb < n_rows ? __ldg(at(rb) + piece) : z;
-                qa[2 * s][0] = u.x; qa[2 * s][1] = w.x; qa[2 * s][2] = u.y; qa[2 * s][3] = w.y;
-                qa[2 * s + 1][0] = u.z; qa[2 * s + 1][1] = w.z; qa[2 * s + 1][2] = u.w; qa[2 * s + 1][3] = w.w;
+                const uint4 u = __ldg(from + (kQuant ? (4 * (s / 2) + c) * 2 + s % 2 : 4 * s + c));
+                qb[g][2 * s][0] = u.x; qb[g][2 * s][1] = u.y; qb[g][2 * s + 1][0] = u.z; qb[g][2 * s + 1][1] = u.w;
             }
-        }
-        const int pa = place0 + int((row0 + min(n, n_rows - 1)) / G), pb = place0 + int((row0 + min(n + 8, n_rows - 1)) / G);
-
-        float o[D / 8][4];
+            float mine = a.scale_log2;
+            if constexpr (kQuant && BF) {
+                uint32_t top = 0;
 #pragma unroll
-        for (int d = 0; d < D / 8; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.0f;
-        float ma = kLow, mb = kLow, la = 0.0f, lb = 0.0f;
+                for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) top = max(top, max(qb[g][s][e] << 16 & 0x7fffffffu, qb[g][s][e] & 0x7fff0000u));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1)); top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const uint32_t ex = top >> 23;                // 0: all zero or subnormal, 255: a NaN or an infinity
+                const uint32_t me = ex == 0 || ex == 255 ? 127 : min(max(127 + 127 + 14 - int(ex), 1), 253);
+                const float mul = __uint_as_float(me << 23);
+                mine *= __uint_as_float((254 - me) << 23);
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) qb[g][s][e] = W::pack(A::lo(qb[g][s][e]) * mul, A::hi(qb[g][s][e]) * mul);
+            }
+            rm[g][0] = __shfl_sync(0xffffffffu, mine, 8 * c); rm[g][1] = __shfl_sync(0xffffffffu, mine, 8 * c + 4);
+        }
+        // this thread's rows are the columns 2 c and 2 c + 1 of each group
+        auto place_of = [&](int g, int e) { return place0 + int((row0 + min(8 * g + 2 * c + e, n_rows - 1)) / G); };
+
+        float o[kGroups][D / 16][4], m[kGroups][2], l[kGroups][2], unit_v = 0.0f, unit_inv = 0.0f;      // largest value scale so far, its inverse
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            m[g][0] = m[g][1] = kLow; l[g][0] = l[g][1] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) o[g][d][0] = o[g][d][1] = o[g][d][2] = o[g][d][3] = 0.0f;
+        }
 
         const int32_t* table = a.b.page_table + uint64_t(i) * a.b.table_stride;
         const int page_mask = (1 << a.p.page_shift) - 1;
@@ -224,104 +263,152 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
             const uint8_t* vt = kt + S::kTile;
             const int key0 = key_of(t);
 
-            float s[NT][4];
+            // S^T: keys n, n + 8 of each 16, columns 2 c, 2 c + 1 of each group
+            float s[kGroups][KT][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+            for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-            for (int u = 0; u < S::kChunks / 4; ++u)
+                for (int k = 0; k < KT; ++k) s[g][k][0] = s[g][k][1] = s[g][k][2] = s[g][k][3] = 0.0f;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(kt + S::k_at(nt * 8 + n, 4 * u + c));
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int u = 0; u < S::kChunks / 4; ++u) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(kt + S::k_at(k * 16 + n, 4 * u + c)), y = *reinterpret_cast<const uint4*>(kt + S::k_at(k * 16 + n + 8, 4 * u + c));
                     if constexpr (!kQuant) {
-                        mma<BF>(s[nt], qa[2 * u], w.x, w.y);
-                        mma<BF>(s[nt], qa[2 * u + 1], w.z, w.w);
-                    } else {
-                        const uint32_t ws[4] = { w.x, w.y, w.z, w.w };
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) mma<BF>(s[nt], qa[4 * u + e], widen<BF, CACHE>(ws[e] & 0xffffu), widen<BF, CACHE>(ws[e] >> 16));
+                        for (int g = 0; g < kGroups; ++g) {
+                            mma<kB>(s[g][k], x.x, y.x, x.y, y.y, qb[g][2 * u]);
+                            mma<kB>(s[g][k], x.z, y.z, x.w, y.w, qb[g][2 * u + 1]);
+                        }
+                    } else {
+                        const uint32_t xs[4] = { x.x, x.y, x.z, x.w }, ys[4] = { y.x, y.y, y.z, y.w };
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t x0, x1, y0, y1;
+                            widen4<CACHE>(xs[e], x0, x1); widen4<CACHE>(ys[e], y0, y1);
+#pragma unroll
+                            for (int g = 0; g < kGroups; ++g) mma<kB>(s[g][k], x0, y0, x1, y1, qb[g][4 * u + e]);
+                        }
                     }
                 }
             const float* scales = reinterpret_cast<const float*>(vt + S::kTile);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float f0 = a.scale_log2, f1 = f0;
-                if constexpr (kQuant) { const float2 k2 = *reinterpret_cast<const float2*>(scales + nt * 8 + 2 * c); f0 = f0 * k2.x; f1 = f1 * k2.y; }
-                s[nt][0] *= f0; s[nt][1] *= f1; s[nt][2] *= f0; s[nt][3] *= f1;
-            }
-            // hidden keys, where the tile has any
             const bool masked = key0 + TK - 1 > first_place || (a.window && key0 < last_place - int(a.window) + 1 && key0 + TK > int(a.sinks));
-            if (masked) {
+            // value scales relative to the largest so far
+            float vs[KT][2];
+            if constexpr (kQuant) {
+                float top = 0.0f;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int k = 0; k < KT; ++k) { vs[k][0] = scales[TK + k * 16 + n]; vs[k][1] = scales[TK + k * 16 + n + 8]; top = fmaxf(top, fmaxf(vs[k][0], vs[k][1])); }
+                if (__any_sync(0xffffffffu, top > unit_v)) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = key0 + nt * 8 + 2 * c + (e & 1), p = e < 2 ? pa : pb;
-                        if (key > p || (a.window && key <= p - int(a.window) && key >= int(a.sinks))) s[nt][e] = -INFINITY;
-                    }
-            }
-            float xa = fmaxf(s[0][0], s[0][1]), xb = fmaxf(s[0][2], s[0][3]);
+                    for (int e = 4; e < 32; e <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, e));
+                    const float f = __fdiv_rn(unit_v, top);
+                    unit_v = top; unit_inv = __fdiv_rn(1.0f, top);
 #pragma unroll
-            for (int nt = 1; nt < NT; ++nt) { xa = fmaxf(xa, fmaxf(s[nt][0], s[nt][1])); xb = fmaxf(xb, fmaxf(s[nt][2], s[nt][3])); }
+                    for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-            for (int m = 1; m < 4; m <<= 1) { xa = fmaxf(xa, __shfl_xor_sync(0xffffffffu, xa, m)); xb = fmaxf(xb, __shfl_xor_sync(0xffffffffu, xb, m)); }
-            if (__any_sync(0xffffffffu, xa > ma || xb > mb)) {       // the maximum moved: earlier sums shrink
-                xa = fmaxf(xa, ma); xb = fmaxf(xb, mb);
-                const float ca = ex2(ma - xa), cb = ex2(mb - xb);
-                ma = xa; mb = xb; la *= ca; lb *= cb;
-#pragma unroll
-                for (int d = 0; d < D / 8; ++d) { o[d][0] *= ca; o[d][1] *= ca; o[d][2] *= cb; o[d][3] *= cb; }
-            }
-            uint32_t pf[KT][4];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float p0 = ex2(s[nt][0] - ma), p1 = ex2(s[nt][1] - ma), p2 = ex2(s[nt][2] - mb), p3 = ex2(s[nt][3] - mb);
-                la += p0 + p1; lb += p2 + p3;
-                if constexpr (kQuant) {
-                    const float2 v2 = *reinterpret_cast<const float2*>(scales + TK + nt * 8 + 2 * c);
-                    const float f0 = v2.x * kLift, f1 = v2.y * kLift;
-                    p0 *= f0; p1 *= f1; p2 *= f0; p3 *= f1;
-                    if (masked) {               // a hidden value's scale may be NaN
-                        p0 = s[nt][0] == -INFINITY ? 0.0f : p0; p1 = s[nt][1] == -INFINITY ? 0.0f : p1;
-                        p2 = s[nt][2] == -INFINITY ? 0.0f : p2; p3 = s[nt][3] == -INFINITY ? 0.0f : p3;
-                    }
+                        for (int d = 0; d < D / 16; ++d) { o[g][d][0] *= f; o[g][d][1] *= f; o[g][d][2] *= f; o[g][d][3] *= f; }
                 }
-                pf[nt / 2][(nt & 1) * 2] = A::pack(p0, p1);
-                pf[nt / 2][(nt & 1) * 2 + 1] = A::pack(p2, p3);
+#pragma unroll
+                for (int k = 0; k < KT; ++k) { vs[k][0] *= unit_inv; vs[k][1] *= unit_inv; }
+            }
+            uint32_t pf[kGroups][KT][2];                     // P^T fragments
+            bool moved = false;
+            float top[kGroups][2];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    float f0 = 1.0f, f1 = 1.0f;
+                    if constexpr (kQuant) { f0 = scales[k * 16 + n]; f1 = scales[k * 16 + n + 8]; }
+                    s[g][k][0] *= rm[g][0] * f0; s[g][k][1] *= rm[g][1] * f0; s[g][k][2] *= rm[g][0] * f1; s[g][k][3] *= rm[g][1] * f1;
+                }
+                if (masked) {
+#pragma unroll
+                    for (int k = 0; k < KT; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = key0 + k * 16 + n + 8 * (e >> 1), p = place_of(g, e & 1);
+                            if (key > p || (a.window && key <= p - int(a.window) && key >= int(a.sinks))) s[g][k][e] = -INFINITY;
+                        }
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float t = fmaxf(s[g][0][e], s[g][0][e + 2]);
+#pragma unroll
+                    for (int k = 1; k < KT; ++k) t = fmaxf(t, fmaxf(s[g][k][e], s[g][k][e + 2]));
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+                    top[g][e] = t;
+                    moved = moved || t > m[g][e];
+                }
+            }
+            if (__any_sync(0xffffffffu, moved)) {            // a maximum moved: earlier sums shrink
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const float x0 = fmaxf(top[g][0], m[g][0]), x1 = fmaxf(top[g][1], m[g][1]), c0 = ex2(m[g][0] - x0), c1 = ex2(m[g][1] - x1);
+                    m[g][0] = x0; m[g][1] = x1; l[g][0] *= c0; l[g][1] *= c1;
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) { o[g][d][0] *= c0; o[g][d][1] *= c1; o[g][d][2] *= c0; o[g][d][3] *= c1; }
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const float m0 = m[g][0] - kLift, m1 = m[g][1] - kLift;
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    float p0 = ex2(s[g][k][0] - m0), p1 = ex2(s[g][k][1] - m1), p2 = ex2(s[g][k][2] - m0), p3 = ex2(s[g][k][3] - m1);
+                    l[g][0] += p0 + p2; l[g][1] += p1 + p3;
+                    if constexpr (kQuant) {
+                        p0 *= vs[k][0]; p1 *= vs[k][0]; p2 *= vs[k][1]; p3 *= vs[k][1];
+                        if (masked) {                        // a hidden value's scale may be NaN
+                            p0 = s[g][k][0] == -INFINITY ? 0.0f : p0; p1 = s[g][k][1] == -INFINITY ? 0.0f : p1;
+                            p2 = s[g][k][2] == -INFINITY ? 0.0f : p2; p3 = s[g][k][3] == -INFINITY ? 0.0f : p3;
+                        }
+                    }
+                    // 8 keys x 8 rows, transposed: row n, keys 2 c and 2 c + 1
+                    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pf[g][k][0]) : "r"(W::pack(p0, p1)));
+                    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pf[g][k][1]) : "r"(W::pack(p2, p3)));
+                }
             }
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
                 if constexpr (!kQuant) {
-                    const int key = 16 * k + (lane & 15);
+                    // blocks (keys 0-7, columns 0-7), (keys 0-7, columns 8-15), (keys 8-15, ...) of 16 keys x 16 columns, transposed
+                    const int key = 16 * k + (lane & 7) + (lane >> 4) * 8;
 #pragma unroll
                     for (int d = 0; d < D / 16; ++d) {
                         uint32_t r0, r1, r2, r3;
-                        const uint32_t at = uint32_t(__cvta_generic_to_shared(vt)) + S::v_at(key, 2 * d + (lane >> 4));
+                        const uint32_t at = uint32_t(__cvta_generic_to_shared(vt)) + S::v_at(key, 2 * d + ((lane >> 3) & 1));
                         asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(at) : "memory");
-                        mma<BF>(o[2 * d], pf[k], r0, r1);
-                        mma<BF>(o[2 * d + 1], pf[k], r2, r3);
+#pragma unroll
+                        for (int g = 0; g < kGroups; ++g) mma<kB>(o[g][d], r0, r1, r2, r3, pf[g][k]);
                     }
                 } else {
-                    constexpr int W = D / 32;        // words of a thread's columns of one key
-                    uint32_t v[4][W];
+                    constexpr int kWords = D / 32;           // words of a thread's columns of one key
+                    uint32_t v[4][kWords];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = 16 * k + 2 * c + (e & 1) + (e >> 1) * 8;
-                        if constexpr (W == 4) {
-                            const uint4 w = *reinterpret_cast<const uint4*>(vt + S::v_at(key, n));
-                            v[e][0] = w.x; v[e][1] = w.y; v[e][2] = w.z; v[e][3] = w.w;
+                        if constexpr (kWords == 4) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(vt + S::v_at(key, n));
+                            v[e][0] = x.x; v[e][1] = x.y; v[e][2] = x.z; v[e][3] = x.w;
                         } else {
-                            const uint2 w = *reinterpret_cast<const uint2*>(vt + S::v_at(key, n >> 1) + (n & 1) * 8);
-                            v[e][0] = w.x; v[e][1] = w.y;
+                            const uint2 x = *reinterpret_cast<const uint2*>(vt + S::v_at(key, n >> 1) + (n & 1) * 8);
+                            v[e][0] = x.x; v[e][1] = x.y;
                         }
                     }
 #pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        const uint32_t a0 = __byte_perm(v[0][w], v[1][w], 0x5140), a1 = __byte_perm(v[0][w], v[1][w], 0x7362);
-                        const uint32_t b0 = __byte_perm(v[2][w], v[3][w], 0x5140), b1 = __byte_perm(v[2][w], v[3][w], 0x7362);
-                        mma<BF>(o[4 * w + 0], pf[k], widen<BF, CACHE>(a0 & 0xffffu), widen<BF, CACHE>(b0 & 0xffffu));
-                        mma<BF>(o[4 * w + 1], pf[k], widen<BF, CACHE>(a0 >> 16), widen<BF, CACHE>(b0 >> 16));
-                        mma<BF>(o[4 * w + 2], pf[k], widen<BF, CACHE>(a1 & 0xffffu), widen<BF, CACHE>(b1 & 0xffffu));
-                        mma<BF>(o[4 * w + 3], pf[k], widen<BF, CACHE>(a1 >> 16), widen<BF, CACHE>(b1 >> 16));
+                    for (int i = 0; i < kWords; ++i) {
+                        // columns 4 i .. 4 i + 3 of keys (0, 1) and (8, 9), side by side
+                        uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
+                        widen4<CACHE>(__byte_perm(v[0][i], v[1][i], 0x5140), a0, a1); widen4<CACHE>(__byte_perm(v[0][i], v[1][i], 0x7362), a2, a3);
+                        widen4<CACHE>(__byte_perm(v[2][i], v[3][i], 0x5140), b0, b1); widen4<CACHE>(__byte_perm(v[2][i], v[3][i], 0x7362), b2, b3);
+#pragma unroll
+                        for (int g = 0; g < kGroups; ++g) {
+                            mma<kB>(o[g][2 * i], a0, a1, b0, b1, pf[g][k]);
+                            mma<kB>(o[g][2 * i + 1], a2, a3, b2, b3, pf[g][k]);
+                        }
                     }
                 }
             }
@@ -329,26 +416,32 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
             stage = stage + 1 == S::kStages ? 0 : stage + 1;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll
-        for (int m = 1; m < 4; m <<= 1) { la += __shfl_xor_sync(0xffffffffu, la, m); lb += __shfl_xor_sync(0xffffffffu, lb, m); }
         __syncthreads();                       // every warp is done with its ring
-        {
-            float* ow = comb_o + warp * kDecodeRows * D;
 #pragma unroll
-            for (int d = 0; d < D / 8; ++d) {
-                // columns of n-tile d: 8 d + column (values as given), column * D / 8 + d (8-bit values)
-                const int c0 = kQuant ? 2 * c * (D / 8) + d : 8 * d + 2 * c, c1 = kQuant ? c0 + D / 8 : c0 + 1;
-                ow[n * D + c0] = o[d][0]; ow[n * D + c1] = o[d][1];
-                ow[(n + 8) * D + c0] = o[d][2]; ow[(n + 8) * D + c1] = o[d][3];
+        for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float t = l[g][e];
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+                const int r = 8 * g + 2 * c + e;
+                if (n == 0) comb_ml[warp * kRows + r] = make_float2(m[g][e], t);
+                float* ow = comb_o + (warp * kRows + r) * D;
+                const float back = kQuant ? unit_v : 1.0f;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) {
+                    // columns of row tile d: 16 d + n and + 8 (values as given), n D / 8 + 2 d and + 1 (8-bit values)
+                    const int d0 = kQuant ? n * (D / 8) + 2 * d : 16 * d + n;
+                    ow[d0] = o[g][d][e] * back; ow[d0 + (kQuant ? 1 : 8)] = o[g][d][e + 2] * back;
+                }
             }
-            if (c == 0) { comb_ml[warp * kDecodeRows + n] = make_float2(ma, la); comb_ml[warp * kDecodeRows + n + 8] = make_float2(mb, lb); }
         }
         __syncthreads();
         const bool whole = t0 == 0 && t1 == sp.tiles;
         // a segment at the start of the block's share goes to the block's slot 0, another to slot 1
         const uint32_t slot = 2 * blockIdx.x + (x == begin ? 0 : 1);
         auto store = [&](int r, int d, float v0, float v1, float l) {
-            const float f = l > 0.0f ? (1.0f / kLift) / l : l;       // l = 0: nothing seen; l = NaN stays NaN
+            const float f = l > 0.0f ? 1.0f / l : l;       // l = 0: nothing seen; l = NaN stays NaN
             const uint32_t row = row0 + r;
             *reinterpret_cast<uint32_t*>(a.out + (uint64_t(q0 + int(row / G)) * a.out_stride + (uint64_t(h) * G + row % G) * D + d) * 2) = A::pack(v0 * f, v1 * f);
         };
@@ -356,12 +449,12 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
             const int r = e / (D / 2), d = e % (D / 2) * 2;
             float m = kLow, l = 0.0f, v0 = 0.0f, v1 = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) m = fmaxf(m, comb_ml[w * kDecodeRows + r].x);
+            for (int w = 0; w < kWarps; ++w) m = fmaxf(m, comb_ml[w * kRows + r].x);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float2 ml = comb_ml[w * kDecodeRows + r];
+                const float2 ml = comb_ml[w * kRows + r];
                 const float f = ex2(ml.x - m);
-                const float2 v = *reinterpret_cast<const float2*>(comb_o + (w * kDecodeRows + r) * D + d);
+                const float2 v = *reinterpret_cast<const float2*>(comb_o + (w * kRows + r) * D + d);
                 l += ml.y * f; v0 += v.x * f; v1 += v.y * f;
             }
             if (whole) store(r, d, v0, v1, l);
@@ -404,24 +497,27 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSM) k_attend_rows(AttendAr
 
 }  // namespace
 
-cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s)
+// `rows`: rows per kv head of the longest sequence that comes here.
+cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s)
 {
-    auto go = [&](auto bf, auto kind, auto dim) -> cudaError_t {
-        constexpr bool BF = decltype(bf)::value;
-        constexpr int CACHE = decltype(kind)::value, D = decltype(dim)::value;
+    auto go = [&](auto bf, auto kind, auto dim, auto groups) -> cudaError_t {
+        constexpr int D = decltype(dim)::value, CACHE = decltype(kind)::value, kGroups = decltype(groups)::value;
         using S = Shape<CACHE, D>;
-        static_assert(S::kSmem >= kWarps * int(kDecodeRows) * (D + 2) * 4, "the joined rows fit the rings");
-        auto kernel = k_attend_rows<BF, CACHE, D>;
+        static_assert(S::kSmem >= kWarps * 8 * kGroups * (D + 2) * 4, "the joined rows fit the rings");
+        auto kernel = k_attend_rows<decltype(bf)::value, CACHE, D, kGroups>;
         const uint32_t smem = S::kSmem + (a.b.n_seqs + 1) * 8;
         if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem + 2049 * 8); e != cudaSuccess) return e;
-        const uint64_t row_tiles = (uint64_t(a.b.max_q_len) * a.group + kDecodeRows - 1) / kDecodeRows;
+        const uint64_t row_tiles = (rows + 8 * kGroups - 1) / (8 * kGroups);
         const uint64_t tiles = uint64_t(a.b.n_seqs) * row_tiles * a.p.n_kv_heads * ((a.b.max_kv_len + S::kTK - 1) / S::kTK + 1);
-        const uint64_t blocks = (tiles + kWarps - 1) / kWarps;
-        kernel<<<uint32_t(blocks < 148 * kBlocksPerSM ? blocks : 148 * kBlocksPerSM), kThreads, smem, s>>>(a);
+        const uint64_t blocks = (tiles + kWarps - 1) / kWarps, most = 148 * (kGroups == 4 ? 1 : kBlocksPerSM);
+        kernel<<<uint32_t(blocks < most ? blocks : most), kThreads, smem, s>>>(a);
         return cudaGetLastError();
     };
     using std::integral_constant;
-    auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? go(bf, kind, integral_constant<int, 64>()) : go(bf, kind, integral_constant<int, 128>()); };
+    auto group = [&](auto bf, auto kind, auto dim) {
+        return rows <= 8 ? go(bf, kind, dim, integral_constant<int, 1>()) : rows <= 16 ? go(bf, kind, dim, integral_constant<int, 2>()) : go(bf, kind, dim, integral_constant<int, 4>());
+    };
+    auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? group(bf, kind, integral_constant<int, 64>()) : group(bf, kind, integral_constant<int, 128>()); };
     auto kind = [&](auto bf) {
         return cache == WWWS_CACHE_16 ? dim(bf, integral_constant<int, 0>()) : cache == WWWS_CACHE_INT8 ? dim(bf, integral_constant<int, 1>()) : dim(bf, integral_constant<int, 2>());
     };
