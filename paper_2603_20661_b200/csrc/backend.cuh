@@ -48,7 +48,7 @@ struct ShapeArgs {
     uint32_t* err;
 };
 
-constexpr uint32_t kDecodeSlots = 2 * 148 * 2;      // partial results of the row kernel: two per block of its largest grid
+constexpr uint32_t kDecodeSlots = 2 * 148 * 3;      // partial results of the row kernel: two per block of its largest grid
 constexpr uint32_t kDecodeRows = 32;                 // most rows of its units
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 

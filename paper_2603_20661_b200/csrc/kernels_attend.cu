@@ -26,7 +26,6 @@ namespace wwws {
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kBlocksPerSM = 2;
 constexpr float kLow = -3.0e38f;            // below every score: 2^(x - kLow) is never formed, 2^(-inf - kLow) is 0
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -45,6 +44,7 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on)    
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool on)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(on ? 4 : 0) : "memory");
@@ -62,7 +62,7 @@ template <int CACHE> __device__ __forceinline__ void widen4(uint32_t four, uint3
     }
 }
 
-template <int CACHE, int D> struct Shape {
+template <int CACHE, int D, int kGroups> struct Shape {
     static constexpr int kElem = CACHE == WWWS_CACHE_16 ? 2 : 1;
     static constexpr int kRow = D * kElem;              // bytes of a cached row
     static constexpr int kChunks = kRow / 16;
@@ -70,7 +70,9 @@ template <int CACHE, int D> struct Shape {
     static constexpr int kTile = kTK * kRow;
     static constexpr int kScales = CACHE == WWWS_CACHE_16 ? 0 : kTK * 8;
     static constexpr int kStage = 2 * kTile + kScales;
-    static constexpr int kStages = kRow == 64 ? 5 : 3;
+    // blocks of an SM: as many as registers allow; stages: what their shared memory allows
+    static constexpr int kBlocks = kRow <= 128 && kGroups == 1 ? 3 : 2;
+    static constexpr int kStages = kRow == 64 ? (kBlocks == 3 ? 4 : 5) : kBlocks == 3 ? 2 : 3;
     static constexpr int kRing = kStages * kStage;
     static constexpr int kSmem = kWarps * kRing;
     // where chunk c of key's row lies, so that the fragment loads below meet no bank twice
@@ -91,13 +93,13 @@ template <int TK> __device__ __forceinline__ Span span_of(int q_len, int kv, uin
 }
 
 template <bool BF, int CACHE, int D, int kGroups>
-__global__ void __launch_bounds__(kThreads, kGroups == 4 ? 1 : kBlocksPerSM) k_attend_rows(AttendArgs a)
+__global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k_attend_rows(AttendArgs a)
 {
     constexpr bool kQuant = CACHE != WWWS_CACHE_16;
     constexpr bool kB = BF && !kQuant;                       // the operands' type
     using A = Act<BF>;
     using W = Act<kB>;
-    using S = Shape<CACHE, D>;
+    using S = Shape<CACHE, D, kGroups>;
     constexpr int TK = S::kTK, KT = TK / 16, kRows = 8 * kGroups;
     constexpr float kLift = kB ? 0.0f : 15.0f;               // log2 of the weights' common factor
     extern __shared__ __align__(128) uint8_t smem[];
@@ -220,12 +222,24 @@ __global__ void __launch_bounds__(kThreads, kGroups == 4 ? 1 : kBlocksPerSM) k_a
                     if (ok && pg[g] >= a.p.n_pages) { report(a.err, bePage); ok = false; }
                     const int64_t cell = ok ? (((int64_t(pg[g]) * Hkv + h) << a.p.page_shift) + (kg & page_mask)) : 0;
                     constexpr int kPer = 16 * S::kChunks / 32;
+                    const uint8_t* ksrc = a.p.k + cell * S::kRow + lane * 16;
+                    const uint8_t* vsrc = a.p.v + cell * S::kRow + lane * 16;
+                    if (ok && kg + 16 <= hi_key && (kg >= lo_key || kg + 16 <= int(a.sinks))) {      // 16 keys that some row sees
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e) {
+                            const int ci = lane + 32 * e, kk = 16 * g + ci / S::kChunks, ch = ci % S::kChunks;
+                            cp16(dst + S::k_at(kk, ch), ksrc + e * 512);
+                            cp16(dst + S::kTile + S::v_at(kk, ch), vsrc + e * 512);
+                        }
+                        if constexpr (kQuant) cp4(dst + 2 * S::kTile + (lane / 16 * TK + 16 * g + lane % 16) * 4, (lane < 16 ? a.p.k_scale : a.p.v_scale) + cell + lane % 16, true);
+                        continue;
+                    }
 #pragma unroll
                     for (int e = 0; e < kPer; ++e) {
                         const int ci = lane + 32 * e, kk = ci / S::kChunks, ch = ci % S::kChunks, key = kg + kk;
                         const bool on = ok && key < hi_key && (key >= lo_key || key < int(a.sinks));
-                        cp16(dst + S::k_at(16 * g + kk, ch), a.p.k + cell * S::kRow + (on ? ci * 16 : 0), on);
-                        cp16(dst + S::kTile + S::v_at(16 * g + kk, ch), a.p.v + cell * S::kRow + (on ? ci * 16 : 0), on);
+                        cp16(dst + S::k_at(16 * g + kk, ch), on ? ksrc + e * 512 : a.p.k, on);
+                        cp16(dst + S::kTile + S::v_at(16 * g + kk, ch), on ? vsrc + e * 512 : a.p.v, on);
                     }
                     if constexpr (kQuant) {
                         const int kk = lane % 16, key = kg + kk;
@@ -477,13 +491,24 @@ __global__ void __launch_bounds__(kThreads, kGroups == 4 ? 1 : kBlocksPerSM) k_a
                 for (int e = tid; e < n_rows * (D / 2); e += kThreads) {
                     const int r = e / (D / 2), d = e % (D / 2) * 2;
                     float m = kLow, l = 0.0f, v0 = 0.0f, v1 = 0.0f;
-                    for (uint32_t k = blk0; k <= blk1; ++k) {
-                        const uint32_t s = k == blk0 ? first_slot : 2 * k;
-                        const float2 ml = __ldcg(a.s.part_ml + s * kDecodeRows + r);
-                        const float2 v = __ldcg(reinterpret_cast<const float2*>(a.s.part_o + (uint64_t(s) * kDecodeRows + r) * D + d));
-                        const float mn = fmaxf(m, ml.x), f0 = ex2(m - mn), f1 = ex2(ml.x - mn);
-                        l = l * f0 + ml.y * f1; v0 = v0 * f0 + v.x * f1; v1 = v1 * f0 + v.y * f1;
-                        m = mn;
+                    constexpr uint32_t kAtOnce = 8;             // parts whose loads are in flight together
+                    for (uint32_t k0 = blk0; k0 <= blk1; k0 += kAtOnce) {
+                        float2 ml[kAtOnce], v[kAtOnce];
+#pragma unroll
+                        for (uint32_t k = 0; k < kAtOnce; ++k) {
+                            ml[k] = make_float2(kLow, 0.0f); v[k] = make_float2(0.0f, 0.0f);
+                            if (k0 + k <= blk1) {
+                                const uint32_t s = k0 + k == blk0 ? first_slot : 2 * (k0 + k);
+                                ml[k] = __ldcg(a.s.part_ml + s * kDecodeRows + r);
+                                v[k] = __ldcg(reinterpret_cast<const float2*>(a.s.part_o + (uint64_t(s) * kDecodeRows + r) * D + d));
+                            }
+                        }
+#pragma unroll
+                        for (uint32_t k = 0; k < kAtOnce; ++k) {
+                            const float mn = fmaxf(m, ml[k].x), f0 = ex2(m - mn), f1 = ex2(ml[k].x - mn);
+                            l = l * f0 + ml[k].y * f1; v0 = v0 * f0 + v[k].x * f1; v1 = v1 * f0 + v[k].y * f1;
+                            m = mn;
+                        }
                     }
                     store(r, d, v0, v1, l);
                 }
@@ -502,14 +527,14 @@ cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head
 {
     auto go = [&](auto bf, auto kind, auto dim, auto groups) -> cudaError_t {
         constexpr int D = decltype(dim)::value, CACHE = decltype(kind)::value, kGroups = decltype(groups)::value;
-        using S = Shape<CACHE, D>;
+        using S = Shape<CACHE, D, kGroups>;
         static_assert(S::kSmem >= kWarps * 8 * kGroups * (D + 2) * 4, "the joined rows fit the rings");
         auto kernel = k_attend_rows<decltype(bf)::value, CACHE, D, kGroups>;
         const uint32_t smem = S::kSmem + (a.b.n_seqs + 1) * 8;
         if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem + 2049 * 8); e != cudaSuccess) return e;
         const uint64_t row_tiles = (rows + 8 * kGroups - 1) / (8 * kGroups);
         const uint64_t tiles = uint64_t(a.b.n_seqs) * row_tiles * a.p.n_kv_heads * ((a.b.max_kv_len + S::kTK - 1) / S::kTK + 1);
-        const uint64_t blocks = (tiles + kWarps - 1) / kWarps, most = 148 * (kGroups == 4 ? 1 : kBlocksPerSM);
+        const uint64_t blocks = (tiles + kWarps - 1) / kWarps, most = 148 * S::kBlocks;
         kernel<<<uint32_t(blocks < most ? blocks : most), kThreads, smem, s>>>(a);
         return cudaGetLastError();
     };
