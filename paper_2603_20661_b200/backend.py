@@ -103,6 +103,7 @@ class Backend:
         self.cache = cache
         self.n_heads, self.n_kv_heads, self.head_dim, self.page_tokens = n_heads, n_kv_heads, head_dim, page_tokens
         self.n_pages, self.max_pages = n_pages, max_pages
+        self._scale = head_dim ** -0.5 if head_dim else 1.0
         self._elem = {"16": self.dtype, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}[cache]
         cfg = BackendConfig(n_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_tokens, max_pages, max_rows,
                             self._codes[self.dtype], CACHES[cache])
@@ -113,6 +114,7 @@ class Backend:
             self._stream = stream if stream is not None else torch.cuda.current_stream(self.device)
             with torch.cuda.stream(self._stream):
                 self._ws = torch.empty(nbytes.value, dtype=torch.uint8, device=self.device)
+            self._index, self._raw, self._raw_current = self.device.index, self._stream.cuda_stream, torch._C._cuda_getCurrentRawStream
             h = C.c_void_p()
             self._check(self._lib.wwws_create_backend(C.byref(cfg), self._ws.data_ptr(), nbytes.value, self._stream.cuda_stream, C.byref(h)))
         self._h = h
@@ -132,20 +134,23 @@ class Backend:
         except Exception:
             pass
 
-    def _mine(self, *tensors):
-        """True if the backend's stream is the current one; else the tensors are marked as used on the backend's."""
-        if self._torch.cuda.current_stream(self.device) == self._stream:
-            return True
+    def _aside(self):
+        """Whether another stream than the backend's is current (asked once per call: it costs as much as a small kernel)."""
+        return self._raw_current(self._index) != self._raw
+
+    def _used(self, *tensors):
+        """Mark tensors of the current stream as used on the backend's."""
         for t in tensors:
             if t is not None:
                 t.record_stream(self._stream)
-        return False
 
-    def _empty(self, shape, dtype):
-        if self._torch.cuda.current_stream(self.device) == self._stream:
+    def _empty(self, shape, dtype, aside):
+        if not aside:
             return self._torch.empty(shape, dtype=dtype, device=self.device)
         with self._torch.cuda.stream(self._stream):
-            return self._torch.empty(shape, dtype=dtype, device=self.device)
+            t = self._torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(self._torch.cuda.current_stream(self.device))
+        return t
 
     def _array(self, t, dtype, name, dims=1):
         if t.dtype != dtype or t.dim() != dims or not t.is_contiguous() or t.device != self.device:
@@ -164,8 +169,9 @@ class Backend:
     def new_cache(self):
         """A page pool of the configuration (uninitialised), bound."""
         shape = (self.n_pages, self.n_kv_heads, self.page_tokens)
-        k, v = (self._empty(shape + (self.head_dim,), self._elem) for _ in range(2))
-        ks, vs = (None, None) if self.cache == "16" else (self._empty(shape, self._torch.float32) for _ in range(2))
+        aside = self._aside()
+        k, v = (self._empty(shape + (self.head_dim,), self._elem, aside) for _ in range(2))
+        ks, vs = (None, None) if self.cache == "16" else (self._empty(shape, self._torch.float32, aside) for _ in range(2))
         return self.bind_cache(k, v, ks, vs)
 
     def bind_cache(self, k, v, k_scale=None, v_scale=None):
@@ -222,47 +228,56 @@ class Backend:
         ks, vs = self._rows(k, self.n_kv_heads, "k"), self._rows(v, self.n_kv_heads, "v")
         if k.shape[0] != batch.extra or v.shape[0] != batch.extra:
             raise ValueError(f"k and v must hold the batch's {batch.extra} tokens")
-        self._mine(k, v, *cache.tensors, *batch.tensors)
+        if self._aside():
+            self._used(k, v, *cache.tensors, *batch.tensors)
         self._check(self._lib.wwws_cache_append(self._h, batch.at, cache.at, k.data_ptr(), ks, v.data_ptr(), vs))
 
     def read(self, cache, batch, row_start, n_rows):
         """Whole sequences back: (k, v), each [n_rows, n_kv_heads, head_dim]; sequence i's tokens from row row_start[i] on."""
         self._array(row_start, self._torch.int32, "row_start")
-        k, v = (self._empty((int(n_rows), self.n_kv_heads, self.head_dim), self.dtype) for _ in range(2))
-        self._mine(row_start, k, v, *cache.tensors, *batch.tensors)
-        self._check(self._lib.wwws_cache_read(self._h, batch.at, cache.at, row_start.data_ptr(), int(n_rows), k.data_ptr(), v.data_ptr()))
+        if row_start.shape[0] != batch.c.n_seqs + 1:
+            raise ValueError(f"row_start: expected {batch.c.n_seqs + 1} entries, got {row_start.shape[0]}")
+        aside = self._aside()
+        kv = self._empty((2, n_rows, self.n_kv_heads, self.head_dim), self.dtype, aside)
+        if aside:
+            self._used(row_start, *cache.tensors, *batch.tensors)
+        k, v = kv.unbind(0)
+        self._check(self._lib.wwws_cache_read(self._h, batch.at, cache.at, row_start.data_ptr(), n_rows, k.data_ptr(), v.data_ptr()))
         return k, v
 
     def attend(self, cache, batch, q, out=None, scale=None, window=0, sinks=0):
         """Attention of the new tokens ([n_tokens, n_heads, head_dim]) over the cache; scale defaults to head_dim ** -0.5."""
         qs = self._rows(q, self.n_heads, "q")
+        aside = self._aside()
         if out is None:
-            out = self._empty((q.shape[0], self.n_heads, self.head_dim), self.dtype)
-        os = self._rows(out, self.n_heads, "out")
+            out, os = self._empty(q.shape, self.dtype, aside), self.n_heads * self.head_dim
+        else:
+            os = self._rows(out, self.n_heads, "out")
         if q.shape[0] != batch.extra or out.shape[0] != batch.extra:
             raise ValueError(f"q and out must hold the batch's {batch.extra} tokens")
-        self._mine(q, out, *cache.tensors, *batch.tensors)
-        self._check(self._lib.wwws_attend(self._h, batch.at, cache.at, q.data_ptr(), qs, out.data_ptr(), os,
-                                          self.head_dim ** -0.5 if scale is None else scale, window, sinks))
+        if aside:
+            self._used(q, out, *cache.tensors, *batch.tensors)
+        self._check(self._lib.wwws_attend(self._h, batch.at, cache.at, q.data_ptr(), qs, out.data_ptr(), os, self._scale if scale is None else scale, window, sinks))
         return out
 
     def shape_logits(self, logits, shaping, out=None, tokens=True):
         """(shaped logits, token per row): penalties, biases and masks on logits [rows, vocab] (bf16, f16 or f32)."""
-        torch = self._torch
-        if logits.dim() != 2 or logits.dtype not in self._codes or logits.device != self.device or logits.stride(1) != 1 and logits.shape[1] > 1:
+        dtype = self._codes.get(logits.dtype)
+        if logits.dim() != 2 or dtype is None or logits.device != self.device or logits.stride(1) != 1 and logits.shape[1] > 1:
             raise ValueError(f"logits: expected [rows, vocab] of bf16, f16 or f32 with packed rows on {self.device}")
         rows, vocab = logits.shape
         if shaping.extra is not None and shaping.extra != rows:
             raise ValueError(f"the shaping names {shaping.extra} rows, logits has {rows}")
+        aside = self._aside()
         if out is None:
-            out = self._empty((rows, vocab), logits.dtype)
+            out = self._empty((rows, vocab), logits.dtype, aside)
         elif out.shape != logits.shape or out.dtype != logits.dtype or out.stride(1) != 1 and vocab > 1 or out.device != self.device:
             raise ValueError("out: expected the shape and type of logits")
-        token = self._empty((rows,), torch.int32) if tokens else None
-        self._mine(logits, out, token, *shaping.tensors)
-        self._check(self._lib.wwws_shape_logits(self._h, shaping.at, rows, vocab, self._codes[logits.dtype], logits.data_ptr(),
-                                                logits.stride(0) if rows > 1 else vocab, out.data_ptr(), out.stride(0) if rows > 1 else vocab,
-                                                token.data_ptr() if tokens else None))
+        token = self._empty((rows,), self._torch.int32, aside) if tokens else None
+        if aside:
+            self._used(logits, out, token, *shaping.tensors)
+        self._check(self._lib.wwws_shape_logits(self._h, shaping.at, rows, vocab, dtype, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab,
+                                                out.data_ptr(), out.stride(0) if rows > 1 else vocab, token.data_ptr() if tokens else None))
         return out, token
 
     def sync(self):

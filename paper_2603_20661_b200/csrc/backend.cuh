@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/wwws_backend.h"
 
 namespace wwws {
@@ -36,6 +38,7 @@ struct AttendArgs {
     uint32_t group;      // query heads per kv head
     float scale_log2;    // softmax scale * log2(e)
     uint32_t window, sinks;
+    uint32_t pad;        // row kernel: 0, or the tiles that every unit counts (see kernels_attend.cu)
     uint32_t few_rows;   // sequences with at most this many rows per kv head (new tokens * group) go to the row kernel, others to the tile kernel
     uint32_t* err;
 };
@@ -43,7 +46,7 @@ struct AttendArgs {
 struct ShapeArgs {
     wwws_shaping s;
     const uint8_t* in; uint8_t* out; uint64_t in_stride, out_stride;
-    uint32_t n_rows, vocab, slice, n_slices;
+    uint32_t n_rows, vocab, n_slices;
     int32_t* token; unsigned long long* best; uint32_t* ticket;     // best, ticket: [n_rows], zero between calls
     uint32_t* err;
 };
@@ -52,6 +55,19 @@ constexpr uint32_t kDecodeSlots = 2 * 148 * 3;      // partial results of the ro
 constexpr uint32_t kDecodeRows = 32;                 // most rows of its units
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 
+// Raises a kernel's limit of dynamic shared memory, the first time on each device.
+template <auto kKernel> cudaError_t allow_smem(int bytes)
+{
+    static std::atomic<uint64_t> done{ 0 };          // a bit per device
+    int device = 0;
+    if (cudaError_t e = cudaGetDevice(&device); e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    if (cudaError_t e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); e != cudaSuccess) return e;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
 cudaError_t launch_cache_append(const SeqBatch& b, const Pages& p, const void* k, uint64_t k_stride, const void* v, uint64_t v_stride,
                                 uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
 cudaError_t launch_cache_read(const SeqBatch& b, const Pages& p, const int32_t* row_start, uint64_t n_rows, void* k_out, void* v_out,
@@ -59,7 +75,6 @@ cudaError_t launch_cache_read(const SeqBatch& b, const Pages& p, const int32_t* 
 cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_attend_tile(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s);
-uint32_t shape_slice(uint32_t n_rows, uint32_t vocab);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void report(uint32_t* err, uint32_t bit) { atomicOr(err, bit); }

@@ -253,7 +253,7 @@ wwws_status wwws_shape_logits(wwws_backend* b, const wwws_shaping* s, uint32_t n
     ShapeArgs a{};
     a.s = *s;
     a.in = static_cast<const uint8_t*>(logits); a.out = static_cast<uint8_t*>(out); a.in_stride = stride; a.out_stride = out_stride;
-    a.n_rows = n_rows; a.vocab = vocab; a.slice = shape_slice(n_rows, vocab); a.n_slices = (vocab + a.slice - 1) / a.slice;
+    a.n_rows = n_rows; a.vocab = vocab;
     a.token = token; a.best = b->best; a.ticket = b->row_ticket; a.err = b->err;
     return launched(b, launch_shape_logits(a, int(dtype), b->stream), "wwws_shape_logits");
 }

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
         if (base + tid < a.b.n_seqs) {
             int q0, q_len, kv;
             if (sequence(a.b, base + tid, q0, q_len, kv, a.err) && q_len && uint32_t(q_len) * G <= a.few_rows)
-                x = (unsigned long long)((uint32_t(q_len) * G + kRows - 1) / kRows) * span_of<TK>(q_len, kv, a.window, a.sinks).tiles;
+                x = (unsigned long long)((uint32_t(q_len) * G + kRows - 1) / kRows) * (a.pad ? a.pad : span_of<TK>(q_len, kv, a.window, a.sinks).tiles);
         }
         const unsigned long long own = x;
 #pragma unroll
@@ -133,6 +133,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
     const unsigned long long total = carry * Hkv;
     unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
     if (share < kWarps) share = kWarps;
+    if (a.pad) share = (share + a.pad - 1) / a.pad * a.pad;
     const unsigned long long begin = blockIdx.x * share, end = min(total, begin + share);
 
     const uint32_t ring = uint32_t(__cvta_generic_to_shared(smem)) + warp * S::kRing;
@@ -148,9 +149,9 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
         const int q0 = a.b.q_start[i], q_len = a.b.q_start[i + 1] - q0, kv = a.b.kv_len[i];
         const Span sp = span_of<TK>(q_len, kv, a.window, a.sinks);
         const unsigned long long rel = x - prefix[i] * Hkv;
-        const uint32_t unit = uint32_t(rel / uint32_t(sp.tiles));
-        const int t0 = int(rel - (unsigned long long)unit * uint32_t(sp.tiles));
-        const int t1 = int(min((unsigned long long)sp.tiles, t0 + (end - x)));
+        const uint32_t counted = a.pad ? a.pad : uint32_t(sp.tiles), unit = uint32_t(rel / counted);
+        const int t0 = int(rel - (unsigned long long)unit * counted);
+        const int t1 = a.pad ? sp.tiles : int(min((unsigned long long)sp.tiles, t0 + (end - x)));
         const uint32_t h = unit % Hkv, row0 = unit / Hkv * kRows;
         const int n_rows = min(int(kRows), q_len * int(G) - int(row0));
         const int place0 = kv - q_len;                                   // place of the sequence's first new token
@@ -516,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
             }
         }
         __syncthreads();                       // the joined rows are read before the rings fill again
-        x += t1 - t0;
+        x += a.pad ? a.pad : t1 - t0;
     }
 }
 
@@ -529,13 +530,20 @@ cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head
         constexpr int D = decltype(dim)::value, CACHE = decltype(kind)::value, kGroups = decltype(groups)::value;
         using S = Shape<CACHE, D, kGroups>;
         static_assert(S::kSmem >= kWarps * 8 * kGroups * (D + 2) * 4, "the joined rows fit the rings");
-        auto kernel = k_attend_rows<decltype(bf)::value, CACHE, D, kGroups>;
+        constexpr auto kernel = k_attend_rows<decltype(bf)::value, CACHE, D, kGroups>;
         const uint32_t smem = S::kSmem + (a.b.n_seqs + 1) * 8;
-        if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem + 2049 * 8); e != cudaSuccess) return e;
+        if (cudaError_t e = allow_smem<kernel>(S::kSmem + 2049 * 8); e != cudaSuccess) return e;
         const uint64_t row_tiles = (rows + 8 * kGroups - 1) / (8 * kGroups);
-        const uint64_t tiles = uint64_t(a.b.n_seqs) * row_tiles * a.p.n_kv_heads * ((a.b.max_kv_len + S::kTK - 1) / S::kTK + 1);
-        const uint64_t blocks = (tiles + kWarps - 1) / kWarps, most = 148 * S::kBlocks;
-        kernel<<<uint32_t(blocks < most ? blocks : most), kThreads, smem, s>>>(a);
+        const uint64_t units = uint64_t(a.b.n_seqs) * row_tiles * a.p.n_kv_heads, most = 148 * S::kBlocks;
+        uint64_t tiles = (a.b.max_kv_len + S::kTK - 1) / S::kTK;             // of a unit, at most
+        const uint64_t seen = (a.sinks + S::kTK - 1) / S::kTK + (uint64_t(a.window) + a.b.max_q_len) / S::kTK + 2;
+        if (a.window && seen < tiles) tiles = seen;
+        // Units of at most 16 tiles are not cut: each counts the same number of tiles and shares end between units, which saves the parts and their
+        // joining (one request of 300 tokens: TIMES us) and costs some balance, little against it at this size.
+        AttendArgs args = a;
+        args.pad = tiles <= 16 ? uint32_t(tiles ? tiles : 1) : 0;
+        const uint64_t blocks = args.pad ? units : (units * (tiles + 1) + kWarps - 1) / kWarps;
+        kernel<<<uint32_t(blocks < most ? blocks : most), kThreads, smem, s>>>(args);
         return cudaGetLastError();
     };
     using std::integral_constant;

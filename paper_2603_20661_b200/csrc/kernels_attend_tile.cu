@@ -737,8 +737,8 @@ cudaError_t launch_attend_tile(const AttendArgs& a, uint32_t head_dim, int dtype
         using C = Cfg<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
         static_assert(C::kSmem <= 232448 - 512, "shared memory of a block");
         static_assert(C::kOffBars >= 2048 * 8, "the prefix fits over the rings");
-        auto kernel = k_attend_tile<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
-        if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem); e != cudaSuccess) return e;
+        constexpr auto kernel = k_attend_tile<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
+        if (cudaError_t e = allow_smem<kernel>(C::kSmem); e != cudaSuccess) return e;
         // no more blocks than tiles the bounds allow
         const uint64_t step = 2 * (128 / a.group), units = a.b.n_tokens / step + a.b.n_seqs;
         const uint64_t tiles = units * a.p.n_kv_heads * ((a.b.max_kv_len + kBN - 1) / kBN);
