@@ -46,7 +46,7 @@ struct AttendArgs {
 struct ShapeArgs {
     wwws_shaping s;
     const uint8_t* in; uint8_t* out; uint64_t in_stride, out_stride;
-    uint32_t n_rows, vocab, n_slices;
+    uint32_t n_rows, vocab;
     int32_t* token; unsigned long long* best; uint32_t* ticket;     // best, ticket: [n_rows], zero between calls
     uint32_t* err;
 };

@@ -1,36 +1,54 @@
 // Logits shaping: penalties for repeated tokens, biases, a grammar mask, and the row's largest logit, in one pass.
 //
 // Bound by HBM: every logit is read once and written once.  What makes it more than a copy is the history: a row's tokens
-// come in no order, and the penalty of a token depends on how often it occurs.  A block owns a slice of one row's vocabulary:
-//   1. its logits are requested, into registers;
-//   2. while they are on their way, the row's history is counted in shared memory (16 bits per token: bit 15 = seen in the prompt, the
-//      rest = count in the output; integer atomics, so the result does not depend on their order), and the bias entry that applies to
-//      a token is noted (the last one: an integer maximum).  The history is read once per slice, from L2 after the first;
-//   3. eight tokens at a time: untouched ones, nearly all, are only masked and compared, as bits; the others take the arithmetic.
-// Rows with more than 32,767 tokens of history are counted in 32 bits, half a slice at a time.  The largest logit is a 64-bit integer
-// maximum of (rounded value as an ordered integer, ~index): the lowest index wins a tie, and again the order of the atomics does not
-// matter.  The row's last block to arrive writes the token and leaves the row's words at zero for the next call.
+// come in no order, and the penalty of a token depends on how often it occurs.  A block takes a part of one row (all of it where there are enough
+// rows) and first sorts the part's history by slices of 1,024 tokens (2 KB of 16-bit logits) into shared memory, a counting sort, while
+// the first logits are on their way.  From there on its warps work alone, without a barrier, a slice at a time:
+//   1. the slice's history is counted and its biases are noted in a word per token: 20 bits of count in the output, a bit for the prompt, 11 bits
+//      for the last bias entry that names the token (integer atomics: their order does not matter);
+//   2. eight tokens at a time, all are masked and written as bits, and their maximum is taken two at a time;
+//   3. the next slice's logits are requested, and the touched tokens are done over by whoever takes their word, which clears it.
+// Doing the touched tokens over, not in step 2, spares nearly every warp the arithmetic of all its tokens for the sake of one or two.
+// Measured at 256 x 131,072 bf16 logits with 2,000 tokens of history a row: arithmetic in step 2 166 us; a block per slice of 16,384 tokens, its
+// phases between barriers, 97 us; this way TIMES.
+// The maximum of step 2 counts touched tokens by their old logits; should it be in a piece with one of those, the warp takes it again without them.
+// The largest logit is a 64-bit integer maximum of (rounded value as an ordered integer, ~index): the lowest index wins a tie, and again the
+// order of the atomics does not matter.  The block that brings a row's last part writes the token and leaves the row's words at zero for the
+// next call.
 #include "backend.cuh"
 
 namespace wwws {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kMaxCount = 32767;                 // of a 16-bit count
+constexpr int kThreads = 256, kWarps = kThreads / 32, kBlocks = 4;     // blocks per SM
+constexpr uint32_t kTokens = 1024;               // of a slice
+constexpr uint32_t kSlices = 256;                // of a part, at most
+constexpr uint32_t kIds = 8192;                  // history entries of a part that are sorted; with more, every slice goes through the history
+constexpr uint32_t kBiases = 512;                // bias entries that are kept in shared memory
+constexpr uint32_t kHeavy = 192;                // history entries of a slice from which on its touched tokens are done with the others
+constexpr uint32_t kMaxBias = 2047, kMaxHistory = (1u << 20) - 1;
+constexpr uint32_t kPrompt = 1u << 20, kCount = kPrompt - 1;           // fields of a token's word; the bias entry + 1 is above them
 
+// max2: the larger of two packed pairs (f32: of two numbers); a NaN loses.
 template <int DT> struct Elem;
 template <> struct Elem<WWWS_F32> {
     using Raw = uint32_t;
+    static __device__ uint32_t max2(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+    static __device__ float last(uint32_t w) { return __uint_as_float(w); }
     static __device__ float get(Raw r) { return __uint_as_float(r); }
     static __device__ Raw put(float f) { return __float_as_uint(f); }
 };
 template <> struct Elem<WWWS_BF16> {
     using Raw = uint16_t;
+    static __device__ uint32_t max2(uint32_t a, uint32_t b) { uint32_t r; asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+    static __device__ float last(uint32_t w) { return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
     static __device__ float get(Raw r) { return __uint_as_float(uint32_t(r) << 16); }
     static __device__ Raw put(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
 };
 template <> struct Elem<WWWS_F16> {
     using Raw = uint16_t;
+    static __device__ uint32_t max2(uint32_t a, uint32_t b) { uint32_t r; asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+    static __device__ float last(uint32_t w) { return fmaxf(__half2float(__ushort_as_half(uint16_t(w))), __half2float(__ushort_as_half(uint16_t(w >> 16)))); }
     static __device__ float get(Raw r) { return __half2float(__ushort_as_half(r)); }
     static __device__ Raw put(float f) { return __half_as_ushort(__float2half_rn(f)); }
 };
@@ -44,46 +62,64 @@ __device__ __forceinline__ uint32_t ordered(float f)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// kVecs 16-byte pieces per thread: a slice is kThreads * kVecs * 16 bytes of logits.
-template <int DT, int kVecs>
-__global__ void __launch_bounds__(kThreads) k_shape_logits(ShapeArgs a)
+// A warp's words have room for 8 tokens more than a slice, so that 16-byte pieces start at multiples of theirs whatever the row's alignment.
+constexpr uint32_t kWords = kTokens + 8;
+constexpr uint32_t kSmem = kWarps * kWords * 4 + kIds * 2 + kSlices * 4 + kBiases * 4;
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads, kBlocks) k_shape_logits(ShapeArgs a)
 {
     using E = Elem<DT>;
     using Raw = typename E::Raw;
-    constexpr uint32_t P = 16 / sizeof(Raw), kSlice = kThreads * kVecs * P, kHalf = kSlice / 2;
-    extern __shared__ __align__(16) uint8_t smem[];
-    uint16_t* count16 = reinterpret_cast<uint16_t*>(smem);                           // [kSlice], or
-    uint32_t* count32 = reinterpret_cast<uint32_t*>(smem);                           // [kHalf]
-    uint16_t* bias16 = reinterpret_cast<uint16_t*>(smem) + kSlice;                   // [kSlice], where the call has biases: entry + 1
-    __shared__ unsigned long long best_of_warp[kThreads / 32];
-    const uint32_t row = blockIdx.y, first = blockIdx.x * (kSlice - P);              // (P tokens short: room for an unaligned start)
-    const uint32_t n = min(kSlice - P, a.vocab - first);
+    constexpr uint32_t P = 16 / sizeof(Raw);     // tokens of 16 bytes
+    constexpr int kVecs = kTokens / P / 32;      // 16-byte pieces of a lane
+    extern __shared__ __align__(16) uint32_t smem[];
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint32_t* words = smem + warp * kWords;
+    uint32_t* slice_end = smem + kWarps * kWords;                                    // [kSlices] where a slice's entries end in ids
+    uint32_t* bias_ids = slice_end + kSlices;
+    uint16_t* ids = reinterpret_cast<uint16_t*>(bias_ids + kBiases);                 // [kIds] token within its slice, bit 15 = in the prompt
+    __shared__ unsigned long long best_of_warp[kWarps];
+    __shared__ uint32_t sum_of_warp[kWarps];
 
-    const Raw* in = reinterpret_cast<const Raw*>(a.in) + uint64_t(row) * a.in_stride + first;
-    Raw* out = reinterpret_cast<Raw*>(a.out) + uint64_t(row) * a.out_stride + first;
-    // 16-byte accesses between the first and the last 16-byte boundary of the slice, single elements outside, or throughout
-    // where input and output are not aligned alike
-    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(in) & 15), off_out = uint32_t(reinterpret_cast<uintptr_t>(out) & 15);
-    const uint32_t head = off == off_out ? min(n, uint32_t(((16 - off) & 15) / sizeof(Raw))) : n;
-    const uint32_t vecs = (n - head) / P, shift = (P - head % P) % P;                // token i's words are at i + shift: pieces start at multiples of P
+    const uint32_t row = blockIdx.y, n_slices = (a.vocab + kTokens - 1) / kTokens;
+    const uint32_t s0 = uint32_t(uint64_t(n_slices) * blockIdx.x / gridDim.x), s1 = uint32_t(uint64_t(n_slices) * (blockIdx.x + 1) / gridDim.x);
+
+    // A slice's place: 16-byte accesses between its first and last 16-byte boundary, single elements outside, or throughout where input and
+    // output are not aligned alike.  Token i's word is at i + shift: pieces start at multiples of P.
+    struct Place { const Raw* in; Raw* out; uint32_t first, n, head, vecs, shift; };
+    auto place = [&](uint32_t slice) {
+        Place p;
+        p.first = slice * kTokens;
+        p.n = min(kTokens, a.vocab - p.first);
+        p.in = reinterpret_cast<const Raw*>(a.in) + uint64_t(row) * a.in_stride + p.first;
+        p.out = reinterpret_cast<Raw*>(a.out) + uint64_t(row) * a.out_stride + p.first;
+        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p.in) & 15), off_out = uint32_t(reinterpret_cast<uintptr_t>(p.out) & 15);
+        p.head = off == off_out ? min(p.n, uint32_t(((16 - off) & 15) / sizeof(Raw))) : p.n;
+        p.vecs = (p.n - p.head) / P;
+        p.shift = (P - p.head % P) % P;
+        return p;
+    };
     uint4 x[kVecs];
+    auto request = [&](uint32_t slice) {
+        if (slice >= s1) return;
+        const Place p = place(slice);
 #pragma unroll
-    for (int t = 0; t < kVecs; ++t) {
-        const uint32_t j = threadIdx.x + t * kThreads;
-        if (j < vecs) x[t] = __ldcs(reinterpret_cast<const uint4*>(in + head) + j);
-    }
+        for (int t = 0; t < kVecs; ++t) if (lane + t * 32 < p.vecs) x[t] = *(reinterpret_cast<const uint4*>(p.in + p.head) + lane + t * 32);     // (kept in L2: touched tokens are read again)
+    };
+    request(s0 + warp);
 
-    int h0 = 0, h1 = 0, prompt_end = 0, b0 = 0, b1 = 0;
+    int h0 = 0, h1 = 0, prompt_end = 0, b0 = 0, nb = 0;
+    const uint32_t* mask = nullptr;
     if (a.s.history) {
         h0 = a.s.history_start[row]; h1 = a.s.history_start[row + 1];
-        if (h0 < 0 || h1 < h0 || uint64_t(h1) > a.s.n_history) { report(a.err, beOffset); h0 = h1 = 0; }
+        if (h0 < 0 || h1 < h0 || uint64_t(h1) > a.s.n_history || h1 - h0 > int(kMaxHistory)) { report(a.err, beOffset); h0 = h1 = 0; }
         prompt_end = h0 + (a.s.prompt_len ? a.s.prompt_len[row] : 0);
     }
     if (a.s.bias_id) {
-        b0 = a.s.bias_start[row]; b1 = a.s.bias_start[row + 1];
-        if (b0 < 0 || b1 < b0 || b1 - b0 > 65535 || uint64_t(b1) > a.s.n_bias) { report(a.err, beOffset); b0 = b1 = 0; }
+        b0 = a.s.bias_start[row]; nb = a.s.bias_start[row + 1] - b0;
+        if (b0 < 0 || nb < 0 || nb > int(kMaxBias) || uint64_t(b0) + uint64_t(nb) > a.s.n_bias) { report(a.err, beOffset); b0 = nb = 0; }
     }
-    const uint32_t* mask = nullptr;
     if (a.s.mask) {
         const int m = a.s.mask_index ? a.s.mask_index[row] : int(row);
         if (m >= 0 && uint32_t(m) < a.s.n_masks) mask = a.s.mask + uint64_t(m) * a.s.mask_stride;
@@ -92,181 +128,238 @@ __global__ void __launch_bounds__(kThreads) k_shape_logits(ShapeArgs a)
     const float rep = a.s.repetition ? a.s.repetition[row] : 1.0f;
     const float freq = a.s.frequency ? a.s.frequency[row] : 0.0f;
     const float pres = a.s.presence ? a.s.presence[row] : 0.0f;
-    const bool has_history = h1 > h0, has_bias = b1 > b0, wide = h1 - h0 > kMaxCount;
 
-    float best = -INFINITY;
-    uint32_t best_at = 0;
-    auto consider = [&](float v, uint32_t i) { if (v > best) { best = v; best_at = i; } };       // a thread meets its tokens in ascending order, except as noted
-    if (has_bias) {
-        for (uint32_t i = threadIdx.x; i < kSlice / 8; i += kThreads) reinterpret_cast<uint4*>(bias16)[i] = make_uint4(0, 0, 0, 0);
-        __syncthreads();
-        for (int i = b0 + int(threadIdx.x); i < b1; i += kThreads) {
-            const uint32_t id = uint32_t(a.s.bias_id[i]), at = id - first;
-            if (id >= a.vocab) { report(a.err, beToken); continue; }
-            if (at >= n) continue;
-            // the largest entry of a token, in its half of a word
-            uint32_t* word = reinterpret_cast<uint32_t*>(bias16) + ((at + shift) >> 1);
-            const uint32_t up = ((at + shift) & 1) * 16, e = uint32_t(i - b0) + 1u;
-            uint32_t was = *word;
-            while (((was >> up) & 0xffffu) < e) {
-                const uint32_t seen = atomicCAS(word, was, (was & ~(0xffffu << up)) | e << up);
-                if (seen == was) break;
-                was = seen;
-            }
+    bool sorted = true;
+    if (h1 > h0 || nb) {
+        for (uint32_t i = threadIdx.x; i < kWarps * kWords / 4; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = threadIdx.x; i < min(nb, int(kBiases)); i += kThreads) {
+            const uint32_t id = uint32_t(__ldg(a.s.bias_id + b0 + i));
+            if (id >= a.vocab) report(a.err, beToken);
+            bias_ids[i] = id;
         }
-    }
-    for (uint32_t part = 0; part < (wide ? 2u : 1u); ++part) {
-        const uint32_t from = part * kHalf, size = wide ? kHalf : kSlice;            // the words [from, from + size) of this part
-        if (has_history) {
-            if (part) __syncthreads();
-            for (uint32_t i = threadIdx.x; i < kSlice / 8; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+        if (h1 > h0) {           // the counting sort; the order within a slice does not matter
+            slice_end[threadIdx.x] = 0;
+            static_assert(kSlices == kThreads, "a thread per slice");
             __syncthreads();
-            for (int i = h0 + int(threadIdx.x); i < h1; i += kThreads) {
-                const uint32_t id = uint32_t(__ldg(a.s.history + i)), at = id - first;
-                if (id >= a.vocab) { report(a.err, beToken); continue; }
-                const uint32_t w = at + shift - from;
-                if (at >= n || w >= size) continue;
-                if (wide) {
-                    if (i < prompt_end) atomicOr(count32 + w, 0x80000000u); else atomicAdd(count32 + w, 1u);
-                } else {
-                    uint32_t* word = count32 + (w >> 1);
-                    const uint32_t up = (w & 1) * 16;
-                    if (i < prompt_end) atomicOr(word, 0x8000u << up); else atomicAdd(word, 1u << up);
+            auto places = [&](int pass) {
+                constexpr int kAhead = 4;                    // entries per thread that are requested together
+                for (int first = h0 + int(threadIdx.x); first < h1; first += kAhead * kThreads) {
+                    uint32_t id[kAhead];
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k) id[k] = first + k * kThreads < h1 ? uint32_t(__ldg(a.s.history + first + k * kThreads)) : 0xffffffffu;
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k) {
+                        const int i = first + k * kThreads;
+                        const uint32_t slice = id[k] / kTokens;
+                        if (id[k] >= a.vocab) { if (i < h1 && pass == 0) report(a.err, beToken); }
+                        else if (slice >= s0 && slice < s1) {
+                            const uint32_t at = atomicAdd(&slice_end[slice - s0], 1u);
+                            if (pass) ids[at] = uint16_t(id[k] % kTokens | (i < prompt_end ? 0x8000u : 0u));
+                        }
+                    }
                 }
+            };
+            places(0);
+            __syncthreads();
+            const uint32_t mine = slice_end[threadIdx.x];
+            uint32_t sum = mine;
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) { const uint32_t o = __shfl_up_sync(0xffffffffu, sum, m); if (lane >= uint32_t(m)) sum += o; }
+            if (lane == 31) sum_of_warp[warp] = sum;
+            __syncthreads();
+            uint32_t before = 0, all = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < kWarps; ++w) { if (w < warp) before += sum_of_warp[w]; all += sum_of_warp[w]; }
+            sorted = all <= kIds;
+            if (sorted) {
+                slice_end[threadIdx.x] = before + sum - mine;            // where the slice starts; the second pass moves it to the end
+                __syncthreads();
+                places(1);
             }
         }
-        if (has_history || has_bias) __syncthreads();
+        __syncthreads();
+    }
+    const bool has_history = h1 > h0, plain = !has_history && !nb;
 
-        // the operations and their order are the header's; nothing is contracted (the library is built without fused multiply-adds)
-        auto shape = [&](Raw raw, uint32_t i, bool allowed) -> Raw {
-            float v = E::get(raw);
-            if (has_history) {
-                const uint32_t w = i + shift - from;
-                uint32_t seen, times;
-                if (wide) { const uint32_t c = count32[w]; seen = c; times = c & 0x7fffffffu; }
-                else { const uint32_t c = count16[w]; seen = c; times = c & 0x7fffu; }
-                if (seen) {
-                    v = v > 0.0f ? __fdiv_rn(v, rep) : v * rep;
-                    if (times) { v = v - freq * float(times); v = v - pres; }
+    float best = -INFINITY;                                  // of this lane's touched and single tokens
+    uint32_t best_at = 0, warp_best = 0, warp_best_at = 0;   // of untouched tokens, ordered(); the warp's lanes agree
+    for (uint32_t slice = s0 + warp; slice < s1; slice += kWarps) {
+        const Place p = place(slice);
+        const uint32_t e0 = sorted && has_history && slice > s0 ? slice_end[slice - s0 - 1] : 0, e1 = sorted && has_history ? slice_end[slice - s0] : 0;
+        auto each_bias = [&](auto&& f) {
+            for (int i = int(lane); i < nb; i += 32) {
+                const uint32_t id = i < int(kBiases) ? bias_ids[i] : uint32_t(__ldg(a.s.bias_id + b0 + i)), at = id - p.first;
+                if (id >= a.vocab) { if (i >= int(kBiases)) report(a.err, beToken); }
+                else if (at < p.n) f(words + at + p.shift, at, uint32_t(i) + 1);
+            }
+        };
+        auto each_token = [&](auto&& f) {
+            if (sorted) {
+                for (uint32_t i = e0 + lane; i < e1; i += 32) { const uint32_t v = ids[i], at = v & 0x3ffu; f(words + at + p.shift, at, v >> 15); }
+            } else {
+                for (int i = h0 + int(lane); i < h1; i += 32) {
+                    const uint32_t id = uint32_t(__ldg(a.s.history + i)), at = id - p.first;
+                    if (id < a.vocab && at < p.n) f(words + at + p.shift, at, uint32_t(i < prompt_end));
                 }
             }
-            if (has_bias) { const uint32_t e = bias16[i + shift]; if (e) v = v + a.s.bias_value[b0 + int(e) - 1]; }
-            return E::put(allowed ? v : -INFINITY);
         };
-        auto scalar = [&](uint32_t i) {
-            const uint32_t v = first + i;
-            if (i + shift - from >= size) return;
-            const Raw r = shape(in[i], i, !mask || ((mask[v >> 5] >> (v & 31)) & 1u));
-            out[i] = r;
-            const float f = E::get(r);
-            if (f > best || (f == best && i < best_at && f > -INFINITY)) { best = f; best_at = i; }
+        if (nb) { each_bias([&](uint32_t* w, uint32_t, uint32_t entry) { atomicMax(w, entry << 21); }); __syncwarp(); }
+        if (has_history) each_token([&](uint32_t* w, uint32_t, uint32_t prompt) { if (prompt) atomicOr(w, kPrompt); else atomicAdd(w, 1u); });
+        __syncwarp();
+
+        // Slices with many touched tokens (low ids, mostly) take the arithmetic on the way, where the logits are in registers.
+        const bool heavy = e1 - e0 > kHeavy;
+        // the operations and their order are the header's; nothing is contracted (the library is built without fused multiply-adds)
+        auto shaped = [&](float f, uint32_t c) {
+            if (c & (kPrompt | kCount)) f = f > 0.0f ? __fdiv_rn(f, rep) : f * rep;
+            if (c & kCount) { f = f - freq * float(c & kCount); f = f - pres; }
+            if (c >> 21) f = f + a.s.bias_value[b0 + int(c >> 21) - 1];
+            return f;
         };
-        for (uint32_t i = threadIdx.x; i < head; i += kThreads) scalar(i);
+        auto allows = [&](uint32_t i) { const uint32_t v = p.first + i; return !mask || ((__ldg(mask + (v >> 5)) >> (v & 31)) & 1u); };
+        auto touched = [&](uint32_t i) { return !plain && words[i + p.shift] != 0; };
+        auto better = [&](float v, uint32_t i) { if (v > best || (v == best && p.first + i < best_at && v > -INFINITY)) { best = v; best_at = p.first + i; } };
+        auto single = [&](uint32_t i) {
+            const Raw r = allows(i) ? p.in[i] : E::put(-INFINITY);
+            p.out[i] = r;
+            if (!touched(i)) better(E::get(r), i);
+        };
+        for (uint32_t i = lane; i < p.head; i += 32) single(i);
+        for (uint32_t i = p.head + p.vecs * P + lane; i < p.n; i += 32) single(i);
+        float top = -INFINITY;                               // the largest of this lane's pieces, and the first piece that has it
+        int top_t = 0;
 #pragma unroll
         for (int t = 0; t < kVecs; ++t) {
-            const uint32_t j = threadIdx.x + t * kThreads, i = head + j * P, w = i + shift - from;
-            if (j >= vecs || w >= size) continue;
-            const uint32_t v = first + i;
-            uint32_t bits = (1u << P) - 1;
-            if (mask) {
-                const uint32_t s = v & 31;
-                uint32_t m = mask[v >> 5] >> s;
-                if (s + P > 32) m |= mask[(v >> 5) + 1] << (32 - s);
-                bits &= m;
-            }
-            uint32_t touched = 0;                                                    // any word of these tokens
-            if (has_history) {
-                if (wide) {
-#pragma unroll
-                    for (uint32_t e = 0; e < P; ++e) touched |= count32[w + e];
-                } else if constexpr (P == 8) { const uint4 c = *reinterpret_cast<const uint4*>(count16 + w); touched = c.x | c.y | c.z | c.w; }
-                else { const uint2 c = *reinterpret_cast<const uint2*>(count16 + w); touched = c.x | c.y; }
-            }
-            if (has_bias) {
-                if constexpr (P == 8) { const uint4 c = *reinterpret_cast<const uint4*>(bias16 + i + shift); touched |= c.x | c.y | c.z | c.w; }
-                else { const uint2 c = *reinterpret_cast<const uint2*>(bias16 + i + shift); touched |= c.x | c.y; }
-            }
-            uint32_t q[4] = { x[t].x, x[t].y, x[t].z, x[t].w };
-            if (touched) {
+            if (lane + t * 32 >= p.vecs) continue;
+            const uint32_t i = p.head + (lane + t * 32) * P;
+            if (heavy) {
                 Raw e[P];
-                memcpy(e, q, 16);
+                memcpy(e, &x[t], 16);
 #pragma unroll
-                for (uint32_t k = 0; k < P; ++k) e[k] = shape(e[k], i + k, (bits >> k) & 1u);
-                memcpy(q, e, 16);
-            } else if (bits != (1u << P) - 1) {
-#pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) {
+                for (uint32_t k = 0; k < P; ++k) {
+                    const uint32_t c = words[i + k + p.shift];
+                    if (c) { words[i + k + p.shift] = 0; e[k] = E::put(shaped(E::get(e[k]), c)); }
+                }
+                memcpy(&x[t], e, 16);
+            }
+            if (mask) {
+                const uint32_t v = p.first + i, s = v & 31;
+                uint32_t bits = __ldg(mask + (v >> 5)) >> s;
+                if (s + P > 32) bits |= __ldg(mask + (v >> 5) + 1) << (32 - s);
+                auto put = [&](uint32_t& q, uint32_t k) {
                     if constexpr (P == 8) {
                         constexpr uint32_t kNone = DT == WWWS_BF16 ? 0xff80u : 0xfc00u;
                         const uint32_t keep = ((bits >> (2 * k)) & 1u) * 0xffffu | ((bits >> (2 * k + 1)) & 1u) * 0xffff0000u;
-                        q[k] = (q[k] & keep) | (~keep & (kNone | kNone << 16));
-                    } else q[k] = (bits >> k) & 1u ? q[k] : 0xff800000u;
-                }
+                        q = (q & keep) | (~keep & (kNone | kNone << 16));
+                    } else q = (bits >> k) & 1u ? q : 0xff800000u;
+                };
+                put(x[t].x, 0); put(x[t].y, 1); put(x[t].z, 2); put(x[t].w, 3);
             }
-            if (a.token) {
-                float f[P];
-#pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) {
-                    if constexpr (P == 8) { f[2 * k] = E::get(Raw(q[k])); f[2 * k + 1] = E::get(Raw(q[k] >> 16)); }
-                    else f[k] = E::get(Raw(q[k]));
-                }
-                float top = f[0];
-#pragma unroll
-                for (uint32_t k = 1; k < P; ++k) top = fmaxf(top, f[k]);
-                // (the head's single tokens lie below, so a tie keeps what is there)
-                if (top > best) {
-#pragma unroll
-                    for (uint32_t k = 0; k < P; ++k) consider(f[k], i + k);
-                }
-            }
-            __stcs(reinterpret_cast<uint4*>(out + i), make_uint4(q[0], q[1], q[2], q[3]));
+            __stcs(reinterpret_cast<uint4*>(p.out + i), x[t]);
+            const float f = E::last(E::max2(E::max2(x[t].x, x[t].y), E::max2(x[t].z, x[t].w)));
+            if (f > top) { top = f; top_t = t; }
         }
-        for (uint32_t i = head + vecs * P + threadIdx.x; i < n; i += kThreads) scalar(i);
+        if (a.token) {
+            // The warp's largest, where it exceeds what the warp has (later tokens lose ties).  The lanes that hold it find the token; if
+            // their pieces have touched tokens, the warp looks again without those.
+            uint32_t mine = ordered(top), all = __reduce_max_sync(0xffffffffu, mine);
+            if (all > warp_best) {
+                uint32_t at = 0xffffffffu;
+                bool clash = false;
+                if (mine == all) {
+#pragma unroll
+                    for (int t = 0; t < kVecs; ++t) {
+                        if (t != top_t) continue;
+                        const uint32_t i = p.head + (lane + t * 32) * P;
+                        Raw e[P];
+                        memcpy(e, &x[t], 16);
+#pragma unroll
+                        for (int k = int(P) - 1; k >= 0; --k) { clash = clash || touched(i + k); if (E::get(e[k]) == top) at = i + k; }
+                    }
+                }
+                if (__any_sync(0xffffffffu, clash)) {
+                    top = -INFINITY; at = 0xffffffffu;
+#pragma unroll
+                    for (int t = 0; t < kVecs; ++t) {
+                        if (lane + t * 32 >= p.vecs) continue;
+                        const uint32_t i = p.head + (lane + t * 32) * P;
+                        Raw e[P];
+                        memcpy(e, &x[t], 16);
+#pragma unroll
+                        for (uint32_t k = 0; k < P; ++k) { const float f = E::get(e[k]); if (f > top && !touched(i + k)) { top = f; at = i + k; } }
+                    }
+                    mine = ordered(top); all = __reduce_max_sync(0xffffffffu, mine);
+                }
+                at = __reduce_min_sync(0xffffffffu, mine == all ? at : 0xffffffffu);
+                if (all > warp_best) { warp_best = all; warp_best_at = p.first + at; }
+            }
+        }
+        request(slice + kWarps);
+        if (plain) continue;
+        __syncwarp();                                        // what is done over below has been written
+        if (heavy && p.vecs * P == p.n) continue;
+        auto over = [&](uint32_t* w, uint32_t at, uint32_t) {
+            const uint32_t c = atomicExch(w, 0u);
+            if (c == 0 || !allows(at)) return;               // taken already, or masked above
+            const Raw r = E::put(shaped(E::get(p.in[at]), c));
+            p.out[at] = r;
+            better(E::get(r), at);
+        };
+        if (sorted) {
+            // two at a time: their logits are on their way together
+            for (uint32_t i = e0 + lane; i < e1; i += 64) {
+                const uint32_t at0 = ids[i] & 0x3ffu, at1 = i + 32 < e1 ? ids[i + 32] & 0x3ffu : 0;
+                uint32_t c0 = atomicExch(words + at0 + p.shift, 0u), c1 = i + 32 < e1 ? atomicExch(words + at1 + p.shift, 0u) : 0;
+                const Raw in0 = c0 ? p.in[at0] : Raw(0), in1 = c1 ? p.in[at1] : Raw(0);
+                if (!allows(at0)) c0 = 0;
+                if (!allows(at1)) c1 = 0;
+                if (c0) { const Raw r = E::put(shaped(E::get(in0), c0)); p.out[at0] = r; better(E::get(r), at0); }
+                if (c1) { const Raw r = E::put(shaped(E::get(in1), c1)); p.out[at1] = r; better(E::get(r), at1); }
+            }
+        } else each_token(over);
+        if (nb) each_bias(over);
+        __syncwarp();
     }
     if (!a.token) return;
 
-    unsigned long long key = best > -INFINITY ? (unsigned long long)(ordered(best)) << 32 | uint32_t(~(first + best_at)) : 0ull;
+    unsigned long long key = best > -INFINITY ? (unsigned long long)(ordered(best)) << 32 | uint32_t(~best_at) : 0ull;
+    const unsigned long long of_warp = warp_best ? (unsigned long long)(warp_best) << 32 | uint32_t(~warp_best_at) : 0ull;
+    if (of_warp > key) key = of_warp;
 #pragma unroll
     for (int m = 16; m; m >>= 1) { const unsigned long long o = __shfl_xor_sync(0xffffffffu, key, m); if (o > key) key = o; }
-    if (threadIdx.x % 32 == 0) best_of_warp[threadIdx.x / 32] = key;
+    if (lane == 0) best_of_warp[warp] = key;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kThreads / 32; ++w) if (best_of_warp[w] > key) key = best_of_warp[w];
-        unsigned long long all = key;
-        if (a.n_slices > 1) {
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) if (best_of_warp[w] > key) key = best_of_warp[w];
+        if (gridDim.x > 1) {
             if (key) atomicMax(&a.best[row], key);
             __threadfence();
             if (atomicAdd(&a.ticket[row], 1u) != gridDim.x - 1) return;
             __threadfence();
-            all = atomicExch(&a.best[row], 0ull);
+            key = atomicExch(&a.best[row], 0ull);
             a.ticket[row] = 0;
         }
-        a.token[row] = (all >> 32) ? int32_t(~uint32_t(all)) : -1;
+        a.token[row] = (key >> 32) ? int32_t(~uint32_t(key)) : -1;
     }
 }
 
 }  // namespace
 
-// Slices of 32 KB of logits (16,384 16-bit tokens: counts and bias entries take 64 KB of shared memory) where that gives every SM two blocks, down
-// to 8 KB for few rows, whose time is that of one block.
-cudaError_t launch_shape_logits(const ShapeArgs& given, int dtype, cudaStream_t s)
+cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s)
 {
-    auto go = [&](auto type, auto vecs) -> cudaError_t {
-        constexpr int DT = decltype(type)::value, kVecs = decltype(vecs)::value;
-        constexpr uint32_t P = DT == WWWS_F32 ? 4 : 8, slice = kThreads * kVecs * P;
-        constexpr auto kernel = k_shape_logits<DT, kVecs>;
-        ShapeArgs a = given;
-        a.n_slices = (a.vocab + slice - P - 1) / (slice - P);
-        if (cudaError_t e = allow_smem<kernel>(slice * 4); e != cudaSuccess) return e;
-        kernel<<<dim3(a.n_slices, a.n_rows), kThreads, slice * (a.s.bias_id ? 4 : 2), s>>>(a);
+    auto go = [&](auto type) -> cudaError_t {
+        constexpr auto kernel = k_shape_logits<decltype(type)::value>;
+        if (cudaError_t e = allow_smem<kernel>(kSmem); e != cudaSuccess) return e;
+        // Parts of a row: as many as give the GPU its blocks, of a slice per warp at least and kSlices at most.
+        const uint32_t slices = (a.vocab + kTokens - 1) / kTokens, least = (slices + kSlices - 1) / kSlices, most = (slices + kWarps - 1) / kWarps;
+        uint32_t parts = 148 * kBlocks / a.n_rows;
+        parts = parts < least ? least : parts > most ? most : parts;
+        kernel<<<dim3(parts, a.n_rows), kThreads, kSmem, s>>>(a);
         return cudaGetLastError();
     };
     using std::integral_constant;
-    auto size = [&](auto type) {
-        const uint64_t bytes = uint64_t(given.n_rows) * given.vocab * (decltype(type)::value == WWWS_F32 ? 4 : 2);
-        return bytes >= 148 * 2 * 32768ull ? go(type, integral_constant<int, 4>()) : bytes >= 148 * 2 * 16384ull ? go(type, integral_constant<int, 2>()) : go(type, integral_constant<int, 1>());
-    };
-    return dtype == WWWS_F32 ? size(integral_constant<int, WWWS_F32>()) : dtype == WWWS_BF16 ? size(integral_constant<int, WWWS_BF16>()) : size(integral_constant<int, WWWS_F16>());
+    return dtype == WWWS_F32 ? go(integral_constant<int, WWWS_F32>()) : dtype == WWWS_BF16 ? go(integral_constant<int, WWWS_BF16>()) : go(integral_constant<int, WWWS_F16>());
 }
 
 }  // namespace wwws
