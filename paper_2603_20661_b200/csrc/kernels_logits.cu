@@ -7,10 +7,11 @@
 //   1. the slice's history is counted and its biases are noted in a word per token: 20 bits of count in the output, a bit for the prompt, 11 bits
 //      for the last bias entry that names the token (integer atomics: their order does not matter);
 //   2. eight tokens at a time, all are masked and written as bits, and their maximum is taken two at a time;
-//   3. the next slice's logits are requested, and the touched tokens are done over by whoever takes their word, which clears it.
+//   3. the next slice's logits are requested, and the touched tokens are done over, a lane each, and their
+//      words cleared; where they are many (low ids, mostly) step 2 takes their arithmetic on the way.
 // Doing the touched tokens over, not in step 2, spares nearly every warp the arithmetic of all its tokens for the sake of one or two.
 // Measured at 256 x 131,072 bf16 logits with 2,000 tokens of history a row: arithmetic in step 2 166 us; a block per slice of 16,384 tokens, its
-// phases between barriers, 97 us; this way TIMES.
+// phases between barriers, 97 us; this way 66 us, 29 of them without a history.
 // The maximum of step 2 counts touched tokens by their old logits; should it be in a piece with one of those, the warp takes it again without them.
 // The largest logit is a 64-bit integer maximum of (rounded value as an ordered integer, ~index): the lowest index wins a tie, and again the
 // order of the atomics does not matter.  The block that brings a row's last part writes the token and leaves the row's words at zero for the
@@ -25,7 +26,7 @@ constexpr uint32_t kTokens = 1024;               // of a slice
 constexpr uint32_t kSlices = 256;                // of a part, at most
 constexpr uint32_t kIds = 8192;                  // history entries of a part that are sorted; with more, every slice goes through the history
 constexpr uint32_t kBiases = 512;                // bias entries that are kept in shared memory
-constexpr uint32_t kHeavy = 192;                // history entries of a slice from which on its touched tokens are done with the others
+constexpr uint32_t kHeavy = 128;                 // touched tokens of a slice above which they are done with the others
 constexpr uint32_t kMaxBias = 2047, kMaxHistory = (1u << 20) - 1;
 constexpr uint32_t kPrompt = 1u << 20, kCount = kPrompt - 1;           // fields of a token's word; the bias entry + 1 is above them
 
@@ -64,7 +65,7 @@ __device__ __forceinline__ uint32_t ordered(float f)
 
 // A warp's words have room for 8 tokens more than a slice, so that 16-byte pieces start at multiples of theirs whatever the row's alignment.
 constexpr uint32_t kWords = kTokens + 8;
-constexpr uint32_t kSmem = kWarps * kWords * 4 + kIds * 2 + kSlices * 4 + kBiases * 4;
+constexpr uint32_t kSmem = kWarps * kWords * 4 + kIds * 2 + kSlices * 4 + kBiases * 4 + kWarps * kHeavy * 2;
 
 template <int DT>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_shape_logits(ShapeArgs a)
@@ -79,6 +80,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_shape_logits(ShapeArgs a)
     uint32_t* slice_end = smem + kWarps * kWords;                                    // [kSlices] where a slice's entries end in ids
     uint32_t* bias_ids = slice_end + kSlices;
     uint16_t* ids = reinterpret_cast<uint16_t*>(bias_ids + kBiases);                 // [kIds] token within its slice, bit 15 = in the prompt
+    uint16_t* listed = ids + kIds + warp * kHeavy;                                   // [kHeavy] touched tokens of the slice
     __shared__ unsigned long long best_of_warp[kWarps];
     __shared__ uint32_t sum_of_warp[kWarps];
 
@@ -186,33 +188,54 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_shape_logits(ShapeArgs a)
     for (uint32_t slice = s0 + warp; slice < s1; slice += kWarps) {
         const Place p = place(slice);
         const uint32_t e0 = sorted && has_history && slice > s0 ? slice_end[slice - s0 - 1] : 0, e1 = sorted && has_history ? slice_end[slice - s0] : 0;
-        auto each_bias = [&](auto&& f) {
-            for (int i = int(lane); i < nb; i += 32) {
-                const uint32_t id = i < int(kBiases) ? bias_ids[i] : uint32_t(__ldg(a.s.bias_id + b0 + i)), at = id - p.first;
-                if (id >= a.vocab) { if (i >= int(kBiases)) report(a.err, beToken); }
-                else if (at < p.n) f(words + at + p.shift, at, uint32_t(i) + 1);
-            }
+        // bias entries and history into the words; the tokens whose word was empty are listed
+        uint32_t n_listed = 0;
+        auto list = [&](bool first, uint32_t at) {
+            const uint32_t who = __ballot_sync(0xffffffffu, first), k = n_listed + __popc(who & ((1u << lane) - 1));
+            if (first && k < kHeavy) listed[k] = uint16_t(at);
+            n_listed += __popc(who);
         };
-        auto each_token = [&](auto&& f) {
-            if (sorted) {
-                for (uint32_t i = e0 + lane; i < e1; i += 32) { const uint32_t v = ids[i], at = v & 0x3ffu; f(words + at + p.shift, at, v >> 15); }
-            } else {
-                for (int i = h0 + int(lane); i < h1; i += 32) {
-                    const uint32_t id = uint32_t(__ldg(a.s.history + i)), at = id - p.first;
-                    if (id < a.vocab && at < p.n) f(words + at + p.shift, at, uint32_t(i < prompt_end));
+        for (int i0 = 0; i0 < nb; i0 += 32) {
+            const int i = i0 + int(lane);
+            uint32_t at = 0xffffffffu;
+            if (i < nb) {
+                const uint32_t id = i < int(kBiases) ? bias_ids[i] : uint32_t(__ldg(a.s.bias_id + b0 + i));
+                if (id < a.vocab) at = id - p.first; else if (i >= int(kBiases)) report(a.err, beToken);
+            }
+            list(at < p.n && atomicMax(words + at + p.shift, uint32_t(i + 1) << 21) == 0, at);
+        }
+        if (nb) __syncwarp();
+        // entries [i0, end) of the history, four per lane at a time (the atomics' latency is most of it); get: an entry's place in the slice and
+        // whether it is in the prompt
+        auto count = [&](int i0, int end, auto&& get) {
+            for (; i0 < end; i0 += 128) {
+                uint32_t at[4], was[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int i = i0 + 32 * k + int(lane);
+                    bool prompt = false;
+                    at[k] = 0xffffffffu;
+                    if (i < end) get(i, at[k], prompt);
+                    was[k] = 1;
+                    if (at[k] < p.n) was[k] = prompt ? atomicOr(words + at[k] + p.shift, kPrompt) : atomicAdd(words + at[k] + p.shift, 1u);
                 }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) list(was[k] == 0, at[k]);
             }
         };
-        if (nb) { each_bias([&](uint32_t* w, uint32_t, uint32_t entry) { atomicMax(w, entry << 21); }); __syncwarp(); }
-        if (has_history) each_token([&](uint32_t* w, uint32_t, uint32_t prompt) { if (prompt) atomicOr(w, kPrompt); else atomicAdd(w, 1u); });
+        if (sorted) count(int(e0), int(e1), [&](int i, uint32_t& at, bool& prompt) { const uint32_t v = ids[i]; at = v & 0x3ffu; prompt = v >> 15; });
+        else count(h0, h1, [&](int i, uint32_t& at, bool& prompt) { const uint32_t id = uint32_t(__ldg(a.s.history + i)); at = id < a.vocab ? id - p.first : 0xffffffffu; prompt = i < prompt_end; });
         __syncwarp();
 
         // Slices with many touched tokens (low ids, mostly) take the arithmetic on the way, where the logits are in registers.
-        const bool heavy = e1 - e0 > kHeavy;
+        const bool heavy = n_listed > kHeavy;
         // the operations and their order are the header's; nothing is contracted (the library is built without fused multiply-adds)
         auto shaped = [&](float f, uint32_t c) {
-            if (c & (kPrompt | kCount)) f = f > 0.0f ? __fdiv_rn(f, rep) : f * rep;
-            if (c & kCount) { f = f - freq * float(c & kCount); f = f - pres; }
+            // (selected, not branched to: several tokens' divisions overlap)
+            const float g = f > 0.0f ? __fdiv_rn(f, rep) : f * rep;
+            f = c & (kPrompt | kCount) ? g : f;
+            const float h = f - freq * float(c & kCount);
+            f = c & kCount ? h - pres : f;
             if (c >> 21) f = f + a.s.bias_value[b0 + int(c >> 21) - 1];
             return f;
         };
@@ -220,28 +243,43 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_shape_logits(ShapeArgs a)
         auto touched = [&](uint32_t i) { return !plain && words[i + p.shift] != 0; };
         auto better = [&](float v, uint32_t i) { if (v > best || (v == best && p.first + i < best_at && v > -INFINITY)) { best = v; best_at = p.first + i; } };
         auto single = [&](uint32_t i) {
-            const Raw r = allows(i) ? p.in[i] : E::put(-INFINITY);
+            Raw r = p.in[i];
+            const uint32_t c = heavy ? words[i + p.shift] : 0;
+            if (c) { words[i + p.shift] = 0; r = E::put(shaped(E::get(r), c)); }
+            if (!allows(i)) r = E::put(-INFINITY);
             p.out[i] = r;
             if (!touched(i)) better(E::get(r), i);
         };
         for (uint32_t i = lane; i < p.head; i += 32) single(i);
         for (uint32_t i = p.head + p.vecs * P + lane; i < p.n; i += 32) single(i);
+        if (heavy) {
+            // in a loop that is not unrolled (its code would be most of the kernel's), by way of the output, which the lane itself reads back
+#pragma unroll 1
+            for (uint32_t j = lane; j < p.vecs; j += 32) {
+                const uint32_t i = p.head + j * P;
+                uint4 q = *(reinterpret_cast<const uint4*>(p.in + p.head) + j);
+                Raw e[P];
+                memcpy(e, &q, 16);
+#pragma unroll
+                for (uint32_t k = 0; k < P; ++k) {
+                    const uint32_t c = words[i + k + p.shift];
+                    const Raw r = E::put(shaped(E::get(e[k]), c));
+                    e[k] = c ? r : e[k];
+                }
+#pragma unroll
+                for (uint32_t k = 0; k < P; k += 4) *reinterpret_cast<uint4*>(words + i + k + p.shift) = make_uint4(0, 0, 0, 0);
+                memcpy(&q, e, 16);
+                *(reinterpret_cast<uint4*>(p.out + p.head) + j) = q;
+            }
+#pragma unroll
+            for (int t = 0; t < kVecs; ++t) if (lane + t * 32 < p.vecs) x[t] = *(reinterpret_cast<const uint4*>(p.out + p.head) + lane + t * 32);
+        }
         float top = -INFINITY;                               // the largest of this lane's pieces, and the first piece that has it
         int top_t = 0;
 #pragma unroll
         for (int t = 0; t < kVecs; ++t) {
             if (lane + t * 32 >= p.vecs) continue;
             const uint32_t i = p.head + (lane + t * 32) * P;
-            if (heavy) {
-                Raw e[P];
-                memcpy(e, &x[t], 16);
-#pragma unroll
-                for (uint32_t k = 0; k < P; ++k) {
-                    const uint32_t c = words[i + k + p.shift];
-                    if (c) { words[i + k + p.shift] = 0; e[k] = E::put(shaped(E::get(e[k]), c)); }
-                }
-                memcpy(&x[t], e, 16);
-            }
             if (mask) {
                 const uint32_t v = p.first + i, s = v & 31;
                 uint32_t bits = __ldg(mask + (v >> 5)) >> s;
@@ -297,27 +335,19 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_shape_logits(ShapeArgs a)
         request(slice + kWarps);
         if (plain) continue;
         __syncwarp();                                        // what is done over below has been written
-        if (heavy && p.vecs * P == p.n) continue;
-        auto over = [&](uint32_t* w, uint32_t at, uint32_t) {
-            const uint32_t c = atomicExch(w, 0u);
-            if (c == 0 || !allows(at)) return;               // taken already, or masked above
-            const Raw r = E::put(shaped(E::get(p.in[at]), c));
-            p.out[at] = r;
-            better(E::get(r), at);
-        };
-        if (sorted) {
+        if (!heavy) {
             // two at a time: their logits are on their way together
-            for (uint32_t i = e0 + lane; i < e1; i += 64) {
-                const uint32_t at0 = ids[i] & 0x3ffu, at1 = i + 32 < e1 ? ids[i + 32] & 0x3ffu : 0;
-                uint32_t c0 = atomicExch(words + at0 + p.shift, 0u), c1 = i + 32 < e1 ? atomicExch(words + at1 + p.shift, 0u) : 0;
-                const Raw in0 = c0 ? p.in[at0] : Raw(0), in1 = c1 ? p.in[at1] : Raw(0);
-                if (!allows(at0)) c0 = 0;
-                if (!allows(at1)) c1 = 0;
-                if (c0) { const Raw r = E::put(shaped(E::get(in0), c0)); p.out[at0] = r; better(E::get(r), at0); }
-                if (c1) { const Raw r = E::put(shaped(E::get(in1), c1)); p.out[at1] = r; better(E::get(r), at1); }
+            for (uint32_t i = lane; i < n_listed; i += 64) {
+                const bool two = i + 32 < n_listed;
+                const uint32_t at0 = listed[i], at1 = two ? listed[i + 32] : 0;
+                const Raw in0 = p.in[at0], in1 = two ? p.in[at1] : Raw(0);
+                const bool on0 = allows(at0), on1 = two && allows(at1);              // the others are masked above
+                if (on0) { const Raw r = E::put(shaped(E::get(in0), words[at0 + p.shift])); p.out[at0] = r; better(E::get(r), at0); }
+                if (on1) { const Raw r = E::put(shaped(E::get(in1), words[at1 + p.shift])); p.out[at1] = r; better(E::get(r), at1); }
+                words[at0 + p.shift] = 0;
+                if (two) words[at1 + p.shift] = 0;
             }
-        } else each_token(over);
-        if (nb) each_bias(over);
+        }
         __syncwarp();
     }
     if (!a.token) return;
