@@ -52,7 +52,8 @@ struct ShapeArgs {
 };
 
 constexpr uint32_t kDecodeSlots = 2 * 148 * 3;      // partial results of the row kernel: two per block of its largest grid
-constexpr uint32_t kDecodeRows = 32;                 // most rows of its units
+constexpr uint32_t kDecodeRows = 16;                 // most rows of its units
+constexpr uint32_t kFewRows = 32, kFewRowsQuant = 48;     // most rows per kv head of a sequence that goes to it (see wwws_attend)
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 
 // Raises a kernel's limit of dynamic shared memory, the first time on each device.

@@ -221,9 +221,11 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
     a.window = window < batch->max_kv_len ? window : 0;          // one that hides nothing is none
     a.sinks = sinks < batch->max_kv_len ? sinks : batch->max_kv_len;
     a.err = b->err;
-    // Sequences go by their rows per kv head (new tokens * group): up to 32 are bound by the cache's bytes and go to the row kernel, above that
-    // the tile kernel's 128-row tiles.  Both run only where the host's counts allow both kinds; the short sequences are then taken to have one new token.
-    a.few_rows = kDecodeRows;
+    // Sequences go by their rows per kv head (new tokens * group): few to the row kernel, which reads the cache once per 16 rows, more to the tile
+    // kernel.  24 requests of 3,000 tokens at head_dim 128, row kernel / tile kernel in us: 16-bit cache, 36 rows 96 / 67; e4m3, 30 rows 68 / 107,
+    // 36 and 48 rows 89 / 109, 60 rows 111 / 110; int8, 48 rows 96 / 124.  Both run only where the host's counts allow both kinds; the short
+    // sequences are then taken to have one new token.
+    a.few_rows = b->cfg.cache == WWWS_CACHE_16 ? kFewRows : kFewRowsQuant;
     const uint64_t most = uint64_t(batch->max_q_len) * a.group;
     const bool many = most > a.few_rows;
     const bool few = !many || uint64_t(batch->n_tokens) != uint64_t(batch->n_seqs) * batch->max_q_len;

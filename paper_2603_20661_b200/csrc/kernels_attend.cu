@@ -6,7 +6,8 @@
 // orders of magnitude below the tensor peak, so the warp-level mma.sync does: what matters is how many bytes are in flight and how few instructions
 // each costs.
 //   - Keys are the 16 rows of the operand, query rows its 8 columns (S^T = K Q^T, O^T = V^T P^T): no half-empty 16-row tile of queries, and
-//     kGroups = 1, 2 or 4 groups of 8 rows share the fragments of a key.
+//     kGroups = 1 or 2 groups of 8 rows share the fragments of a key.  (Up to 32 rows come here, as two units of 16: one unit of 32 took 82 us where
+//     these take 69, five drafted tokens of 24 requests, since it has registers for no more than half the warps' work in flight.)
 //   - Work is cut by keys, not by sequences: all (sequence, row tile, kv head) units laid end to end in tiles of kTK keys, and block i takes
 //     the i-th equal share (the lengths are read on the device: no plan, no host copy of them).  A unit cut by a share boundary leaves a
 //     partial result (m, sum, weighted values) in the workspace; the last of its blocks to arrive joins them in block order,
@@ -548,7 +549,7 @@ cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head
     };
     using std::integral_constant;
     auto group = [&](auto bf, auto kind, auto dim) {
-        return rows <= 8 ? go(bf, kind, dim, integral_constant<int, 1>()) : rows <= 16 ? go(bf, kind, dim, integral_constant<int, 2>()) : go(bf, kind, dim, integral_constant<int, 4>());
+        return rows <= 8 ? go(bf, kind, dim, integral_constant<int, 1>()) : go(bf, kind, dim, integral_constant<int, 2>());
     };
     auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? group(bf, kind, integral_constant<int, 64>()) : group(bf, kind, integral_constant<int, 128>()); };
     auto kind = [&](auto bf) {

@@ -3,19 +3,25 @@
 // A block works on 256 rows of one (sequence, kv head) at a time, as two tiles of 128: a row is a (new token, query head) pair,
 // the query heads of a kv head side by side, so every key tile serves all of them.  Per tile of 128 keys
 //     S = Q K^T            128 x 128 x head_dim into tensor memory, fp32
-//     P = 2^(x - m)        x = scale * log2(e) * S, one row per thread: running maximum and sum without any exchange between threads
+//     P = 2^(x - m)        x = scale * log2(e) * S, running maximum and sum per row, a row per thread (per two threads for a quantised cache)
 //     O = O + P V          P back into tensor memory over S, rounded to the activation type; O stays in tensor memory, fp32
-// One warp issues all matrix instructions in the order PV0 S0 PV1 S1: while the tensor cores work on one row tile, the four warps of the
+// One warp issues all matrix instructions in the order PV0 S0 PV1 S1: while the tensor cores work on one row tile, the softmax warps of the
 // other turn its S into P.  m is allowed to lag behind the true maximum by a factor 2^kLag, so that O is rescaled (a pass over
 // tensor memory) in the first few tiles only; the result is the same sum, since numerator and denominator share m.
-//   - Bound by the exponentials and the tensor cores about equally (head_dim 128: 2 x 16,384 exponentials at 16 a clock and
-//     4 x 128^3 multiply-adds, 2,048 clocks each per key tile).
+//   - Floor per key tile at head_dim 128: 4 x 128^3 multiply-adds, 2,048 clocks of the tensor cores, and 2 x 16,384 exponentials at 16 a clock,
+//     as many.  Measured: about 3,500 clocks, two prompts of 8,192 tokens (32 heads, 8 kv heads, 1.10e12 operations) in 1.17 ms,
+//     943 TFLOP/s, 57 % of the library's rate for a large product.  What is left is the chain of a row tile: scores, softmax (2,150
+//     clocks), P back, PV, the next scores; the two row tiles hide half of it from one another, and tensor memory (2 x 128 columns of S, 2 x
+//     head_dim of O) has no room for a third.  Tried and slower: 64-key tiles with two S each (1.26 ms: the cost per tile is mostly fixed),
+//     polynomials for a quarter of the exponentials (1.22 against 1.10 ms: their constants cost more moves than the unit saves).
+//   - The issuing warp stays converged and predicates each instruction on one lane: in a branch for one lane the descriptors went through
+//     vector registers, 90 clocks per instruction instead of 30.
 //   - Work is cut by key tiles, as in kernels_attend.cu: all (unit, tile) pairs laid end to end, an equal share for each of 148
 //     blocks, cut units joined by the last of their blocks.  The position of a share is found from closed sums (floor_sum), so
 //     causal triangles, windows and ragged lengths need no plan.
 //   - K and V tiles come by TMA page by page into the 128-byte-swizzled layout that the matrix instructions read; pages that no row
 //     sees are fetched from beyond the tensor's end, which fills zeros.
-//   - Quantised caches: codes land in a staging ring, four more warps widen them into the operand layout (exactly: 16-bit floats
+//   - Quantised caches: codes land in a staging ring, two more warps widen them into the operand layout (exactly: 16-bit floats
 //     hold the codes); scales multiply the scores (keys) and the weights (values) in fp32.
 #include <cuda.h>
 
