@@ -184,7 +184,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024 - (smem_at(raw) & 1023)) & 1023);
     const uint32_t base = smem_at(smem);
-    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready (its first half, all of it) / PV done per row tile, join, pairs of warps
+    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready (its first half, all of it) / PV done per row tile, join, pairs of warps, all instructions done
     const uint32_t bars = base + C::kOffBars;
     auto kv_full = [&](int s) { return bars + 8 * s; };
     auto kv_empty = [&](int s) { return bars + 8 * (C::kStages + s); };
@@ -198,7 +198,8 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     auto p_half = [&](int w) { return q_full + 64 + 8 * w; };
     const uint32_t join = q_full + 80;
     auto pair_bar = [&](int k) { return q_full + 88 + 8 * k; };
-    static_assert(8 * (kRest + 19) <= 400, "barriers fit");
+    const uint32_t drained = q_full + 152;
+    static_assert(8 * (kRest + 20) <= 400, "barriers fit");
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [4..] the share's start
     volatile uint32_t* dead = words + 1;
     int* start = reinterpret_cast<int*>(words + 4);                                 // [0] base, [1] sequence, [2] unit
@@ -246,6 +247,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         for (int w2 = 0; w2 < 2; ++w2) { bar_init(s_full(w2), 1); bar_init(p_full(w2), 128 * C::kHalves); bar_init(p_half(w2), 128); bar_init(o_done(w2), 1); }
         bar_init(join, 256 * C::kHalves);
         for (int k = 0; k < 8; ++k) bar_init(pair_bar(k), 64);
+        bar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();                                                                // the share is known, prefix is done with
@@ -320,13 +322,12 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 }
             }
         }
-        if (*dead) {      // leave no copy in flight behind
-            constexpr int N = kQuant ? C::kStaging : C::kStages;
-            for (uint32_t k = it > N ? it - N : 0; k < it; ++k) {
-                const long long t0 = clock64();
-                while (!bar_try(kQuant ? st_full(int(k % N)) : kv_full(int(k % N)), uint32_t(k / N) & 1) && clock64() - t0 < 100000000ll) {}
-            }
-        }
+        // leave no copy in flight behind: where all went well they have landed long ago; otherwise the waits end after 1e8 cycles
+        constexpr int N = kQuant ? C::kStaging : C::kStages;
+        const long long t0 = clock64();
+        auto landed = [&](uint32_t bar, uint32_t parity) { while (!bar_try(bar, parity) && clock64() - t0 < 100000000ll) {} };
+        for (uint32_t k = it > N ? it - N : 0; k < it; ++k) landed(kQuant ? st_full(int(k % N)) : kv_full(int(k % N)), uint32_t(k / N) & 1);
+        if (seg) landed(q_full, uint32_t(seg - 1) & 1);
     } else if (warp == C::kWarpMma) {
         // ---- matrix instructions: S of the first tile, then per tile PV and the next S, the two row tiles in turn ----
         constexpr uint32_t kDescS = mma_desc(BF, false, kBN), kDescO = mma_desc(BF, true, D);
@@ -386,6 +387,10 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             }
             ++seg;
         }
+        // nor any matrix instruction, or its arrival at a barrier
+        commit(drained);
+        const long long t0 = clock64();
+        while (!bar_try(drained, 0) && clock64() - t0 < 100000000ll) {}
     } else if (kQuant && warp >= C::kWarpConvert && warp < C::kWarpMma) {
         // ---- widening: codes of a staged tile to the operand layout, scales beside them ----
         if constexpr (kQuant) {
