@@ -46,7 +46,7 @@ typedef enum {
     WWWS_ERR_RANGE = 4,     /* a peer's version counter reached 2^24 */
     WWWS_ERR_CUDA = 5,      /* a CUDA runtime call failed */
     WWWS_ERR_INVARIANT = 6, /* total credit changed across a settlement */
-    WWWS_ERR_TIMEOUT = 7,   /* reserved */
+    WWWS_ERR_TIMEOUT = 7,   /* a wait inside a kernel ran out (wwws_backend.h) */
     WWWS_ERR_INDEX = 8      /* only from a library built with -DWWWS_CHECK_INDICES: an index that a kernel took from
                                device data (a partner id, a list offset, a candidate or executor id) was out of
                                range; the access was skipped and the results of that call are not to be trusted */

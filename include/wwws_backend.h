@@ -128,7 +128,8 @@ wwws_status wwws_shape_logits(wwws_backend* b, const wwws_shaping* shaping, uint
                               int32_t* token);
 
 /* Wait for the stream and report what the kernels found wrong since the last call: WWWS_ERR_INDEX (a page, token or
- * mask id out of range), WWWS_ERR_ARG (offsets or lengths outside the batch's bounds). */
+ * mask id out of range), WWWS_ERR_ARG (offsets or lengths outside the batch's bounds), WWWS_ERR_TIMEOUT (a wait inside
+ * wwws_attend ran out after about two seconds: its outputs are not to be trusted; the next call starts clean). */
 wwws_status wwws_backend_sync(wwws_backend* b);
 
 const char* wwws_backend_last_error(const wwws_backend* b);

@@ -29,7 +29,7 @@ struct Pages {
 struct AttendScratch {
     float* part_o;       // [slots][rows][head_dim]
     float2* part_ml;     // [slots][rows]
-    uint32_t* ticket;    // [slots], zero between calls
+    uint32_t* ticket;    // [kTickets], zero between calls
 };
 
 struct AttendArgs {
@@ -55,6 +55,8 @@ constexpr uint32_t kDecodeSlots = 2 * 148 * 3;      // partial results of the ro
 constexpr uint32_t kDecodeRows = 16;                 // most rows of its units
 constexpr uint32_t kFewRows = 32, kFewRowsQuant = 48;     // most rows per kv head of a sequence that goes to it (see wwws_attend)
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
+
+constexpr uint32_t kTickets = kDecodeSlots > kTileSlots ? kDecodeSlots : kTileSlots;
 
 // Raises a kernel's limit of dynamic shared memory, the first time on each device.
 template <auto kKernel> cudaError_t allow_smem(int bytes)

@@ -72,7 +72,7 @@ uint64_t carve(const wwws_backend_config& c, uint8_t* base, wwws_backend* b)
     uint8_t* best = take(8ull * c.max_rows);
     uint8_t* row_ticket = take(4ull * c.max_rows);
     constexpr uint64_t kRowSlots = uint64_t(kDecodeSlots) * kDecodeRows, kTileRows = uint64_t(kTileSlots) * 256, rows = kRowSlots > kTileRows ? kRowSlots : kTileRows;
-    uint8_t* ticket = c.n_heads ? take(4ull * (kDecodeSlots > kTileSlots ? kDecodeSlots : kTileSlots)) : nullptr;
+    uint8_t* ticket = c.n_heads ? take(sizeof(uint32_t) * kTickets) : nullptr;
     uint8_t* part_ml = c.n_heads ? take(8 * rows) : nullptr;
     uint8_t* part_o = c.n_heads ? take(4 * rows * c.head_dim) : nullptr;
     if (b) {
@@ -268,6 +268,8 @@ wwws_status wwws_backend_sync(wwws_backend* b)
     cudaError_t e = cudaMemcpyAsync(&bits, b->err, sizeof bits, cudaMemcpyDeviceToHost, b->stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(b->stream);
     if (e == cudaSuccess && bits) e = cudaMemsetAsync(b->err, 0, sizeof bits, b->stream);
+    // blocks that gave up did not take their tickets: those of the next call start at zero all the same
+    if (e == cudaSuccess && (bits & beTimeout) && b->scratch.ticket) e = cudaMemsetAsync(b->scratch.ticket, 0, kTickets * sizeof(uint32_t), b->stream);
     if (e != cudaSuccess) return launched(b, e, "wwws_backend_sync");
     if (bits == 0) return WWWS_OK;
     std::string text;
