@@ -205,11 +205,13 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
         const int32_t* table = a.b.page_table + uint64_t(i) * a.b.table_stride;
         const int page_mask = (1 << a.p.page_shift) - 1;
         auto key_of = [&](int t) { return (t < sp.n_sink ? t : sp.lo_tile + t - sp.n_sink) * TK; };
+        // whether a row of the unit sees any of 16 keys; a page of which none is seen may be someone else's by now and is not looked up
+        auto some = [&](int kg) { return kg < hi_key && (kg + 16 > lo_key || kg < int(a.sinks)); };
         auto pages_of = [&](int t, uint32_t (&pg)[KT]) {
 #pragma unroll
             for (int g = 0; g < KT; ++g) {
                 const int key = key_of(t) + 16 * g;
-                pg[g] = t < t1 && key < hi_key ? uint32_t(__ldg(table + (key >> a.p.page_shift))) : 0u;
+                pg[g] = t < t1 && some(key) ? uint32_t(__ldg(table + (key >> a.p.page_shift))) : 0u;
             }
         };
         // copies one tile of keys and values (zeros for keys that no row of the unit sees)
@@ -220,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
 #pragma unroll
                 for (int g = 0; g < KT; ++g) {
                     const int kg = key0 + 16 * g;
-                    bool ok = kg < hi_key;
+                    bool ok = some(kg);
                     if (ok && pg[g] >= a.p.n_pages) { report(a.err, bePage); ok = false; }
                     const int64_t cell = ok ? (((int64_t(pg[g]) * Hkv + h) << a.p.page_shift) + (kg & page_mask)) : 0;
                     constexpr int kPer = 16 * S::kChunks / 32;
