@@ -214,6 +214,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                 pg[g] = t < t1 && some(key) ? uint32_t(__ldg(table + (key >> a.p.page_shift))) : 0u;
             }
         };
+        bool bad = false;                                    // this warp has met a page outside the pool: such keys are looked for, and hidden
         // copies one tile of keys and values (zeros for keys that no row of the unit sees)
         auto issue = [&](int t, int stage, const uint32_t (&pg)[KT]) {
             if (t < t1) {
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                 for (int g = 0; g < KT; ++g) {
                     const int kg = key0 + 16 * g;
                     bool ok = some(kg);
-                    if (ok && pg[g] >= a.p.n_pages) { report(a.err, bePage); ok = false; }
+                    if (ok && pg[g] >= a.p.n_pages) { report(a.err, bePage); ok = false; bad = true; }
                     const int64_t cell = ok ? (((int64_t(pg[g]) * Hkv + h) << a.p.page_shift) + (kg & page_mask)) : 0;
                     constexpr int kPer = 16 * S::kChunks / 32;
                     const uint8_t* ksrc = a.p.k + cell * S::kRow + lane * 16;
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                     }
                 }
             const float* scales = reinterpret_cast<const float*>(vt + S::kTile);
-            const bool masked = key0 + TK - 1 > first_place || (a.window && key0 < last_place - int(a.window) + 1 && key0 + TK > int(a.sinks));
+            const bool masked = bad || key0 + TK - 1 > first_place || (a.window && key0 < last_place - int(a.window) + 1 && key0 + TK > int(a.sinks));
             // value scales relative to the largest so far
             float vs[KT][2];
             if constexpr (kQuant) {
@@ -349,6 +350,12 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                             const int key = key0 + k * 16 + n + 8 * (e >> 1), p = place_of(g, e & 1);
                             if (key > p || (a.window && key <= p - int(a.window) && key >= int(a.sinks))) s[g][k][e] = -INFINITY;
                         }
+                    if (bad) {
+#pragma unroll
+                        for (int k = 0; k < KT; ++k)
+                            if (const int kg = key0 + 16 * k; some(kg) && uint32_t(__ldg(table + (kg >> a.p.page_shift))) >= a.p.n_pages)
+                                s[g][k][0] = s[g][k][1] = s[g][k][2] = s[g][k][3] = -INFINITY;
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {

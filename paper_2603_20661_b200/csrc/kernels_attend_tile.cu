@@ -200,7 +200,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     auto pair_bar = [&](int k) { return q_full + 88 + 8 * k; };
     const uint32_t drained = q_full + 152;
     static_assert(8 * (kRest + 20) <= 400, "barriers fit");
-    uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [4..] the share's start
+    uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [3] a page outside the pool was met, [4..] the share's start
     volatile uint32_t* dead = words + 1;
     int* start = reinterpret_cast<int*>(words + 4);                                 // [0] base, [1] sequence, [2] unit
 
@@ -240,7 +240,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         int u = 0, uh = q.units;
         while (uh - u > 1) { const int mid = (u + uh) >> 1; if (prefix[i] + sp.sum(q, mid) <= per_head) u = mid; else uh = mid; }
         start[0] = int((prefix[i] + sp.sum(q, u)) * Hkv - begin); start[1] = int(i); start[2] = u;
-        words[1] = 0;
+        words[1] = words[3] = 0;
         for (int s = 0; s < C::kStages; ++s) { bar_init(kv_full(s), kQuant ? C::kConvert : 1); bar_init(kv_empty(s), 1); }
         for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), C::kConvert); }
         bar_init(q_full, 1); bar_init(q_empty, 1);
@@ -293,7 +293,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 if (lane < n_box && key < g.hi && (!a.window || key + int(page_tokens) > g.lo || key < int(a.sinks))) {
                     const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
                     if (page < a.p.n_pages) row = int((page * Hkv + uint32_t(g.h)) << a.p.page_shift);
-                    else report(a.err, bePage);
+                    else { report(a.err, bePage); words[3] = 1; }                // (seen by the softmax warps by way of the barriers below)
                 }
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
@@ -473,7 +473,15 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                     const uint32_t iv = 2 * (it + j) + 1;                    // ring item of the tile's values
                     if (!(ok = WAIT(s_full(w), n_done & 1))) break;
                     tc_after();
-                    const bool masked = key0 + kBN - 1 > place_a || (a.window && key0 < place_b - int(a.window) + 1 && key0 + kBN > int(a.sinks));
+                    uint32_t bad = 0;                                        // 16 keys each of this thread that lie in a page outside the pool: hidden
+                    if (*static_cast<volatile uint32_t*>(words + 3)) {
+#pragma unroll 1
+                        for (int e = 0; e < kCols / 16; ++e) {
+                            const int key = first + 16 * e;
+                            if (key < g.hi && uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift))) >= a.p.n_pages) bad |= 1u << e;
+                        }
+                    }
+                    const bool masked = bad || key0 + kBN - 1 > place_a || (a.window && key0 < place_b - int(a.window) + 1 && key0 + kBN > int(a.sinks));
                     const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + ((it + j) % 4 * 2) * kBN + half * kCols;
                     if constexpr (kQuant) { if (!(ok = WAIT(kv_full(int(iv % C::kStages)), (iv / C::kStages) & 1))) break; }     // both scales are there
                     // the columns [c0, c0 + 32) of this thread that the row sees, a bit each
@@ -485,7 +493,8 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                             const int sunk = min(max(int(a.sinks) - first - c0, 0), 32);
                             bits &= (from == 32 ? 0u : ~0u << from) | (sunk == 32 ? ~0u : (1u << sunk) - 1);
                         }
-                        return bits;
+                        const uint32_t out = bad >> (c0 / 16);
+                        return bits & ~((out & 1u) * 0xffffu | (out >> 1 & 1u) * 0xffff0000u);
                     };
                     const float f = kQuant ? 1.0f : a.scale_log2;
                     const uint32_t kHidden = f < 0.0f ? 0x7f800000u : 0xff800000u;                    // x f = -infinity
