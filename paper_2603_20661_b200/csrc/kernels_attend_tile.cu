@@ -58,8 +58,12 @@ template <bool BF, int CACHE, int D> struct Cfg {
     static constexpr int kWarpConvert = kSoftmaxWarps, kWarpMma = kWarpConvert + kConvert / 32, kWarpLoad = kWarpMma + 1;
     static constexpr int kThreads = (kWarpLoad + 1) * 32;
     static constexpr uint32_t kColP = kQuant ? 0 : 64;      // where P lies over S: the columns whose scores are in registers by then
-    static constexpr float kLag = !BF && kQuant ? 3.0f : 8.0f;              // f16 weights: 2^lag * lift * 516 (largest value scale) < 65,504
-    static constexpr float kLift = !BF && kQuant ? 8.0f : 1.0f;
+    // Weights in f16 over a quantised cache are kept relative to the power of two below the largest value scale of the segment so far, or small
+    // values would push them into f16's subnormals, and times kLift: 2^kLag * 2 * kLift = 2^15 < 65,504, and what is lost below 2^-24 is 2^-36
+    // of the row's largest weight.  bf16 has the range for the scales as they are.
+    static constexpr bool kRelative = !BF && kQuant;
+    static constexpr float kLag = kRelative ? 3.0f : 8.0f;
+    static constexpr float kLift = kRelative ? 2048.0f : 1.0f;
     static constexpr uint32_t kColS = 0, kColO = 256, kCols = 512;
 };
 
@@ -184,7 +188,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024 - (smem_at(raw) & 1023)) & 1023);
     const uint32_t base = smem_at(smem);
-    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready (its first half, all of it) / PV done per row tile, join, pairs of warps, all instructions done
+    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready (its first half, all of it) / PV done per row tile, join, pairs of warps, all instructions done, widening warps
     const uint32_t bars = base + C::kOffBars;
     auto kv_full = [&](int s) { return bars + 8 * s; };
     auto kv_empty = [&](int s) { return bars + 8 * (C::kStages + s); };
@@ -198,11 +202,13 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     auto p_half = [&](int w) { return q_full + 64 + 8 * w; };
     const uint32_t join = q_full + 80;
     auto pair_bar = [&](int k) { return q_full + 88 + 8 * k; };
-    const uint32_t drained = q_full + 152;
-    static_assert(8 * (kRest + 20) <= 400, "barriers fit");
+    const uint32_t drained = q_full + 152, widened = q_full + 160;
+    static_assert(8 * (kRest + 21) <= 400, "barriers fit");
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [3] a page outside the pool was met, [4..] the share's start
     volatile uint32_t* dead = words + 1;
     int* start = reinterpret_cast<int*>(words + 4);                                 // [0] base, [1] sequence, [2] unit
+    float* unit_of = reinterpret_cast<float*>(words + 8);                           // [4 tiles] what their value scales are relative to
+    uint32_t* largest = words + 12;                                                 // [2 tiles][2 widening warps]
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
     const uint32_t Hkv = a.p.n_kv_heads, G = a.group;
@@ -248,6 +254,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         bar_init(join, 256 * C::kHalves);
         for (int k = 0; k < 8; ++k) bar_init(pair_bar(k), 64);
         bar_init(drained, 1);
+        bar_init(widened, C::kConvert ? C::kConvert : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();                                                                // the share is known, prefix is done with
@@ -396,7 +403,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         if constexpr (kQuant) {
             const int t = tid - C::kWarpConvert * 32;
             constexpr int kChunks = D / 16;                     // 16 codes each
-            uint32_t it = 0;
+            uint32_t it = 0, unit = 0;                          // unit: a power of two, as bits
             bool ok = true;
             while (ok && next()) {
                 for (int tile = g.t0; ok && tile < g.t1; ++tile) {
@@ -415,6 +422,20 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                                 scale[0][e] = __ldg(a.p.k_scale + cell); scale[1][e] = __ldg(a.p.v_scale + cell);
                             }
                         }
+                    }
+                    float lift = C::kLift;
+                    if constexpr (C::kRelative) {
+                        uint32_t top = 0;
+#pragma unroll
+                        for (int e = 0; e < kBN / C::kConvert; ++e) { const uint32_t b = __float_as_uint(scale[1][e]) & 0x7fffffffu; if (b < 0x7f800000u) top = max(top, b); }
+                        top = __reduce_max_sync(0xffffffffu, top);
+                        const uint32_t n = it / 2 % 2;
+                        if (lane == 0) largest[2 * n + warp - C::kWarpConvert] = top;
+                        bar_arrive(widened);
+                        if (!(ok = WAIT(widened, n))) break;
+                        if (tile == g.t0) unit = 27u << 23;              // 2^-100: smaller values are zeros in f16 anyway, and its inverse can be lifted
+                        unit = min(max(unit, max(largest[2 * n], largest[2 * n + 1]) & 0x7f800000u), 253u << 23);
+                        lift *= __uint_as_float((254u << 23) - unit);
                     }
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
@@ -437,7 +458,8 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         }
                         float* sc = reinterpret_cast<float*>(smem + C::kOffScales) + ((it / 2) % 4 * 2 + kv) * kBN;
 #pragma unroll
-                        for (int e = 0; e < kBN / C::kConvert; ++e) sc[t + e * C::kConvert] = kv ? scale[1][e] * C::kLift : scale[0][e] * a.scale_log2;
+                        for (int e = 0; e < kBN / C::kConvert; ++e) sc[t + e * C::kConvert] = kv ? scale[1][e] * lift : scale[0][e] * a.scale_log2;
+                        if (C::kRelative && kv == 0 && t == 0) unit_of[it / 2 % 4] = __uint_as_float(unit);
                         fence_async_proxy();
                         bar_arrive(kv_full(s));
                         bar_arrive(st_empty(ss));
@@ -466,7 +488,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             const int place = (g.kv - g.q_len) + tok;
             // places of the row tile's first and last row
             const int place_a = (g.kv - g.q_len) + g.tok0(sp) + w * tq, place_b = (g.kv - g.q_len) + min(g.q_len - 1, g.tok0(sp) + w * tq + tq - 1);
-            float m = kLow, l = 0.0f;
+            float m = kLow, l = 0.0f, unit = 1.0f;                           // unit: what O is relative to
             if (work) {
                 for (int j = 0; j < n; ++j) {
                     const int key0 = g.tile_key(g.t0 + j), first = key0 + half * kCols;
@@ -542,8 +564,9 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         top = fmaxf(top, *theirs);
                     }
                     if (!row_on) top = m;
-                    if (__any_sync(0xffffffffu, top > m + C::kLag)) {
-                        const float mn = fmaxf(m, top), shrink = ex2(m - mn);
+                    const float unit_now = C::kRelative ? unit_of[(it + j) % 4] : 1.0f;
+                    if (__any_sync(0xffffffffu, top > m + C::kLag) || unit_now != unit) {
+                        const float mn = fmaxf(m, top), less = ex2(m - mn), shrink = C::kRelative ? less * __fdiv_rn(unit, unit_now) : less;
                         if (j > 0) {                            // O so far shrinks too, once the last product into it is done; each thread takes its share of the columns
                             if (!(ok = WAIT(o_done(w), (n_done - 1) & 1))) break;
                             tc_after();
@@ -557,7 +580,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                                 tm_st16(tO + c0, v);
                             }
                         }
-                        l *= shrink; m = mn;
+                        l *= less; m = mn; unit = unit_now;
                     }
                     if constexpr (!kQuant) {
                         // values that no row of the unit sees are zeroed in shared memory: a weight of 0 does not silence a NaN
@@ -637,7 +660,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             const uint32_t slot = 2 * blockIdx.x + (x0 == begin ? 0 : 1);
             uint8_t* dst = a.out + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.out_stride + (uint64_t(g.h) * G + r % G) * D + half * (D / C::kHalves)) * 2;
             if (work) {
-                const float inv = l > 0.0f ? (1.0f / C::kLift) / l : l;
+                const float inv = l > 0.0f ? (1.0f / C::kLift) / l * unit : l;
 #pragma unroll
                 for (int c0 = 0; c0 < D / C::kHalves; c0 += 32) {
                     uint32_t v[32];
@@ -657,7 +680,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         float4* part = reinterpret_cast<float4*>(a.s.part_o) + ((uint64_t(slot) * 2 + w) * (D / 4) + half * (D / 4 / C::kHalves)) * kBM + r;      // [slot][row tile][D / 4][128] float4
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            part[(c0 / 4 + e) * kBM] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+                            part[(c0 / 4 + e) * kBM] = make_float4(__uint_as_float(v[4 * e]) * unit, __uint_as_float(v[4 * e + 1]) * unit, __uint_as_float(v[4 * e + 2]) * unit, __uint_as_float(v[4 * e + 3]) * unit);
                     }
                 }
                 if (!whole && row_on && half == 0) a.s.part_ml[(slot * 2 + w) * kBM + r] = make_float2(m, l);
