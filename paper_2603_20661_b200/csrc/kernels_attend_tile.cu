@@ -64,6 +64,8 @@ template <bool BF, int CACHE, int D> struct Cfg {
     static constexpr bool kRelative = !BF && kQuant;
     static constexpr float kLag = kRelative ? 3.0f : 8.0f;
     static constexpr float kLift = kRelative ? 2048.0f : 1.0f;
+    // f16 weights over 16-bit values carry 2^kRaise from the exponential on, and so do their sums: again 2^15 at most, faint ones exact to 2^-32.
+    static constexpr float kRaise = !BF && !kQuant ? 7.0f : 0.0f;
     static constexpr uint32_t kColS = 0, kColO = 256, kCols = 512;
 };
 
@@ -597,7 +599,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                             fence_async_proxy();
                         }
                     }
-                    const uint64_t f2 = pack2(f, f), m2 = pack2(-m, -m);
+                    const uint64_t f2 = pack2(f, f), m2 = pack2(C::kRaise - m, C::kRaise - m);
                     uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
                     auto weights = [&](const uint32_t* v, int c0) {
                         uint32_t p[16];

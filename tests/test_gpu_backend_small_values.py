@@ -88,3 +88,32 @@ def test_largest_and_absent_values(cache, lens):
     got = case.attend(0, 0)
     case.backend.sync()
     assert (got == 0).all()
+
+
+@pytest.mark.parametrize("cache", ["16", "int8", "e4m3"])
+@pytest.mark.parametrize("lens", [[(1, 4000)], [(20, 4000)], [(70, 4000)]], ids=str)
+def test_many_keys_that_are_faint_alone(cache, lens):
+    """One key 17.5 nats ahead whose value is 0, 4,000 others with a value of 1: what is left is their sum, 1e-4, though each weighs 2^-25.2, less than half
+    of f16's smallest number."""
+    case = Case(lens, kv_heads=1, group=4, dim=64, page=32, dtype=torch.float16, cache=cache, seed=25)
+    way = torch.ones(64, device="cuda") / 8.0
+    case.q.copy_((way * 8.0).expand_as(case.q))
+    page, slot = case.table[0, 1].item(), 3                          # key 35
+    if cache == "16":
+        case.k.copy_(torch.where(torch.isnan(case.k), case.k, 0.0))
+        case.v.copy_(torch.where(torch.isnan(case.v), case.v, 1.0))
+        case.k[page, :, slot], case.v[page, :, slot] = (way * 17.5).half(), 0.0
+    else:
+        one = 1 if cache == "int8" else 0x38                         # code 1
+        case.k.view(torch.uint8).zero_()
+        case.v.view(torch.uint8).fill_(one)
+        for scale in (case.k_scale, case.v_scale):
+            scale.copy_(torch.where(torch.isnan(scale), scale, 1.0))
+        case.k.view(torch.uint8)[page, :, slot], case.k_scale[page, :, slot] = one, 17.5 / 8.0
+        case.v.view(torch.uint8)[page, :, slot] = 0
+    got = case.attend(0, 0)
+    case.backend.sync()
+    want, weight, scores = attend_exact(case, 0, 0, None)
+    assert 0.8e-4 < want.min().item() and want.max().item() < 1.2e-4
+    off = (got.double() - want).abs() - bound(case, want, weight, scores, 2.0 ** -32)
+    assert (off <= 0).all(), f"{off.max().item():.3g} too far"
