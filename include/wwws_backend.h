@@ -98,8 +98,8 @@ wwws_status wwws_cache_read(wwws_backend* b, const wwws_batch* batch, const wwws
  *   out = sum_j softmax_j(scale * q . k_j) v_j,   0 where nothing is seen.
  * q and out: [n_tokens][n_heads][head_dim] of the backend's dtype, 16-byte aligned, strides in elements (multiples of
  * 8).  Scores, softmax and sums are fp32; the softmax weights are rounded to the backend's dtype for the second
- * product.  Hidden keys never reach a result where every new token of the sequence hides them (after kv_len, before the
- * window).  Results do not depend on what else is in the batch's pages, and repeat bit for bit. */
+ * product.  A hidden key never reaches a row's result, whatever its key and value hold; a
+ * visible one that is infinite or not a number does (a value: in its own column).  Results do not depend on what else is in the batch's pages, and repeat bit for bit. */
 wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
                         uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window, uint32_t sinks);
 

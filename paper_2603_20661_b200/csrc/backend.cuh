@@ -93,6 +93,20 @@ __device__ __forceinline__ bool sequence(const SeqBatch& b, uint32_t i, int& q0,
     return ok;
 }
 
+// A weight of 0 does not silence a value that is infinite or not a number, so the attention kernels look for these among the 16-bit values that some rows of a
+// unit see and others do not, take them out of the product, and add them to the sums of the rows that see them.
+__device__ __forceinline__ void largest_halves(uint32_t& top, uint4 x)       // the larger magnitudes of both halves, as bits: an exponent of ones is above every number
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"((e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w) & 0x7fff7fffu));
+}
+template <bool BF> __device__ __forceinline__ bool unreal(uint32_t half) { return (half & 0x7fffu) >= (BF ? 0x7f80u : 0x7c00u); }
+template <bool BF> __device__ __forceinline__ bool unreal2(uint32_t both) { return unreal<BF>(both) || unreal<BF>(both >> 16); }
+template <bool BF> __device__ __forceinline__ uint32_t real2(uint32_t both)  // zeros in their place
+{
+    return (unreal<BF>(both) ? 0u : both & 0xffffu) | (unreal<BF>(both >> 16) ? 0u : both & 0xffff0000u);
+}
+
 // Two-element vectors of the activation type, and the float conversions the kernels need.
 template <bool BF> struct Act;
 template <> struct Act<true> {

@@ -396,6 +396,42 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pf[g][k][1]) : "r"(W::pack(p2, p3)));
                 }
             }
+            if constexpr (!kQuant) {
+                if (masked && first_place != last_place) {   // (rows of one token see the same keys; five drafted tokens of 24 requests: 74.4 -> 76.9 us)
+                    uint8_t* values = smem + (vt - smem);
+                    uint32_t top_half = 0;
+#pragma unroll
+                    for (int e = 0; e < S::kTile / 512; ++e) largest_halves(top_half, *reinterpret_cast<const uint4*>(values + e * 512 + lane * 16));
+                    if (__any_sync(0xffffffffu, unreal2<BF>(top_half))) {
+#pragma unroll 1
+                        for (int kk = 0; kk < TK; ++kk) {
+                            auto value = [&](int d) { return uint32_t(*reinterpret_cast<const uint16_t*>(values + S::v_at(kk, d / 8) + d % 8 * 2)); };
+                            auto sees = [&](int g, int e) {
+                                const int key = key0 + kk, p = place_of(g, e);
+                                return key <= p && (!a.window || key > p - int(a.window) || key < int(a.sinks));
+                            };
+#pragma unroll
+                            for (int d = 0; d < D / 16; ++d) {
+                                const uint32_t v0 = value(16 * d + n), v1 = value(16 * d + n + 8);
+#pragma unroll
+                                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        if (unreal<BF>(v0) && sees(g, e)) o[g][d][e] += A::lo(v0);
+                                        if (unreal<BF>(v1) && sees(g, e)) o[g][d][e + 2] += A::lo(v1);
+                                    }
+                            }
+                        }
+                        __syncwarp();
+#pragma unroll 1
+                        for (int e = 0; e < S::kTile / 512; ++e) {
+                            uint4* x = reinterpret_cast<uint4*>(values + e * 512 + lane * 16);
+                            *x = make_uint4(real2<BF>(x->x), real2<BF>(x->y), real2<BF>(x->z), real2<BF>(x->w));
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
                 if constexpr (!kQuant) {

@@ -54,7 +54,7 @@ template <bool BF, int CACHE, int D> struct Cfg {
     // Threads per row: one where the scores are used as they come; two for a quantised cache, whose scales have to be fetched for every column
     // (a thread per row, 24 int8 prompts: 0.79 ms, two 0.62; two prompts of 8,192 tokens in 16 bits: 1.03 ms with one, 1.10 with two).
     static constexpr int kHalves = kQuant ? 2 : 1;
-    static constexpr int kSoftmaxWarps = 8 * kHalves, kConvert = kQuant ? 64 : 0;   // kConvert: threads of the widening warps
+    static constexpr int kSoftmaxWarps = 8 * kHalves, kConvert = kQuant ? 64 : 32;    // kConvert: threads that widen codes, or look through 16-bit values
     static constexpr int kWarpConvert = kSoftmaxWarps, kWarpMma = kWarpConvert + kConvert / 32, kWarpLoad = kWarpMma + 1;
     static constexpr int kThreads = (kWarpLoad + 1) * 32;
     static constexpr uint32_t kColP = kQuant ? 0 : 64;      // where P lies over S: the columns whose scores are in registers by then
@@ -166,6 +166,12 @@ struct Walk {
     __device__ __forceinline__ int tok0(const Space& sp) const { return u * sp.step; }             // first token of the unit
     __device__ __forceinline__ bool two(const Space& sp) const { return u * sp.step + sp.step / 2 < q_len; }   // the second row tile has tokens
     __device__ __forceinline__ int tile_key(int t) const { return (t < n_sink ? t : lo_tile + t - n_sink) * kBN; }
+    // whether the key tile has keys that some rows of the unit do not see
+    __device__ __forceinline__ bool mixed(const AttendArgs& a, const Space& sp, int key0) const
+    {
+        const int first = kv - q_len + u * sp.step, last = kv - q_len + min(q_len, (u + 1) * sp.step) - 1;
+        return key0 + kBN - 1 > first || (a.window && key0 < last - int(a.window) + 1 && key0 + kBN > int(a.sinks));
+    }
 };
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -180,6 +186,40 @@ __device__ __forceinline__ void scale2(uint32_t* x, uint64_t by)
     x[0] = __float_as_uint(y0); x[1] = __float_as_uint(y1);
 }
 
+// The values of keys [key0, end) that are infinite or not numbers, added to the sums (tensor memory, at tO) of this warp's rows that see them; `place`: of this
+// thread's row.  The product had zeros in their place.  (Not inlined, and its loops not unrolled: it hardly ever runs.)
+template <bool BF, int D>
+__device__ __noinline__ void add_unreal(const int32_t* table, const uint8_t* v, uint32_t n_pages, uint32_t page_shift, uint32_t n_kv_heads, uint32_t h, int key0, int end,
+                                        int lo, int window, int sinks, int place, uint32_t tO)
+{
+#pragma unroll 1
+    for (int key = key0; key < end; ++key) {
+        if (window && key < lo && key >= sinks) continue;
+        const uint32_t page = uint32_t(__ldg(table + (key >> page_shift)));
+        if (page >= n_pages) continue;
+        const uint4* row = reinterpret_cast<const uint4*>(v + (((uint64_t(page) * n_kv_heads + h) << page_shift) + (key & ((1 << page_shift) - 1))) * (D * 2));
+        const bool sees = key <= place && (!window || key > place - window || key < sinks);
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+            const uint4 x0 = __ldg(row + 2 * c), x1 = __ldg(row + 2 * c + 1);
+            uint32_t top = 0;
+            largest_halves(top, x0); largest_halves(top, x1);
+            if (!unreal2<BF>(top)) continue;                  // (the same for the whole warp)
+            const uint32_t x[8] = { x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w };
+            uint32_t o[16];
+            tm_ld16(tO + 16 * c, o);
+            tm_wait_ld16(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t half = x[e / 2] >> (e % 2 * 16) & 0xffffu;
+                if (sees && unreal<BF>(half)) o[e] = __float_as_uint(__uint_as_float(o[e]) + Act<BF>::lo(half));
+            }
+            tm_st16(tO + 16 * c, o);
+            tm_wait_st();
+        }
+    }
+}
+
 template <bool BF, int CACHE, int D>
 __global__ void __launch_bounds__(Cfg<BF, CACHE, D>::kThreads, 1)
 k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
@@ -190,7 +230,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024 - (smem_at(raw) & 1023)) & 1023);
     const uint32_t base = smem_at(smem);
-    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready (its first half, all of it) / PV done per row tile, join, pairs of warps, all instructions done, widening warps
+    // barriers: full and empty per stage, the same for staging, queries full and free, S ready / P ready (its first half, all of it) / PV done per row tile, join, pairs of warps, all instructions done, widening warps, values looked through
     const uint32_t bars = base + C::kOffBars;
     auto kv_full = [&](int s) { return bars + 8 * s; };
     auto kv_empty = [&](int s) { return bars + 8 * (C::kStages + s); };
@@ -205,8 +245,9 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
     const uint32_t join = q_full + 80;
     auto pair_bar = [&](int k) { return q_full + 88 + 8 * k; };
     const uint32_t drained = q_full + 152, widened = q_full + 160;
-    static_assert(8 * (kRest + 21) <= 400, "barriers fit");
-    uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [3] a page outside the pool was met, [4..] the share's start
+    auto v_ready = [&](int s) { return q_full + 168 + 8 * (s / 2); };                // 16-bit values, which lie in the odd stages: looked through
+    static_assert(8 * (kRest + 21 + C::kStages / 2) <= 400 && (kQuant || C::kStages % 2 == 0), "barriers fit");
+    uint32_t* words = reinterpret_cast<uint32_t*>(smem + C::kOffBars + 400);        // [0] tensor memory, [1] dead, [2] last to arrive, [3] bit 0: a page outside the pool was met, bit 1: a value that is no number was taken out, [4..] the share's start
     volatile uint32_t* dead = words + 1;
     int* start = reinterpret_cast<int*>(words + 4);                                 // [0] base, [1] sequence, [2] unit
     float* unit_of = reinterpret_cast<float*>(words + 8);                           // [4 tiles] what their value scales are relative to
@@ -256,7 +297,8 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         bar_init(join, 256 * C::kHalves);
         for (int k = 0; k < 8; ++k) bar_init(pair_bar(k), 64);
         bar_init(drained, 1);
-        bar_init(widened, C::kConvert ? C::kConvert : 1);
+        bar_init(widened, C::kConvert);
+        for (int s = 1; s < C::kStages; s += 2) bar_init(v_ready(s), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();                                                                // the share is known, prefix is done with
@@ -302,7 +344,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 if (lane < n_box && key < g.hi && (!a.window || key + int(page_tokens) > g.lo || key < int(a.sinks))) {
                     const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
                     if (page < a.p.n_pages) row = int((page * Hkv + uint32_t(g.h)) << a.p.page_shift);
-                    else { report(a.err, bePage); words[3] = 1; }                // (seen by the softmax warps by way of the barriers below)
+                    else { report(a.err, bePage); atomicOr(words + 3, 1u); }     // (seen by the softmax warps by way of the barriers below)
                 }
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
@@ -370,7 +412,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
             commit(kv_empty(int(it % C::kStages)));
             for (int j = 0; ok && j < n; ++j) {
                 const uint32_t iv = it + 1, ik = it + 2;
-                if (!(ok = WAIT(kv_full(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
+                if (!(ok = WAIT(kQuant ? kv_full(int(iv % C::kStages)) : v_ready(int(iv % C::kStages)), uint32_t(iv / C::kStages) & 1))) break;
                 for (int w = 0; ok && w < nw; ++w) {
                     if constexpr (!kQuant) {                    // the first half of P is worked on while the second is made
                         if (!(ok = WAIT(p_half(w), uint32_t(tiles_of[w]) & 1))) break;
@@ -400,7 +442,7 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
         commit(drained);
         const long long t0 = clock64();
         while (!bar_try(drained, 0) && clock64() - t0 < 100000000ll) {}
-    } else if (kQuant && warp >= C::kWarpConvert && warp < C::kWarpMma) {
+    } else if (warp >= C::kWarpConvert && warp < C::kWarpMma) {
         // ---- widening: codes of a staged tile to the operand layout, scales beside them ----
         if constexpr (kQuant) {
             const int t = tid - C::kWarpConvert * 32;
@@ -467,6 +509,45 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         bar_arrive(st_empty(ss));
                         ++it;
                     }
+                }
+            }
+        } else {
+            // ---- 16-bit values: those that no row of the unit sees become zeros (a weight of 0 does not silence a NaN), and so do, where some rows see
+            // them and others do not, those that are no numbers: the softmax warps add them to the rows that see them when the segment's sums are done.
+            // (A warp of its own: in the softmax warps the same cost 512 tokens behind 5,489 2 % and two prompts of 8,192 tokens 3 to 7 %; here they lose
+            // nothing.  A second such warp costs the former 4 %.)
+            const int t = tid - C::kWarpConvert * 32;
+            uint32_t it = 1;                                    // ring item of the values
+            bool ok = true;
+            while (ok && next()) {
+                for (int tile = g.t0; tile < g.t1; ++tile, it += 2) {
+                    const int key0 = g.tile_key(tile), s = int(it % C::kStages);
+                    if (!(ok = WAIT(kv_full(s), uint32_t(it / C::kStages) & 1))) break;
+                    if (g.mixed(a, sp, key0)) {
+#pragma unroll 1
+                        for (int r = t; r < kBN; r += C::kConvert) {
+                            const int key = key0 + r;
+                            const bool seen = key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks));
+                            uint8_t* row = smem + C::kOffRing + s * C::kTile + r * 128;
+                            auto piece = [&](int e) { return reinterpret_cast<uint4*>(row + e / 8 * (kBN * 128) + ((e ^ r) & 7) * 16); };     // (neighbours meet no bank twice)
+                            uint32_t top = 0;
+                            if (seen) {
+#pragma unroll
+                                for (int e = 0; e < 8 * C::kSlabs; ++e) largest_halves(top, *piece(e));
+                            }
+                            if (!seen || unreal2<BF>(top)) {
+#pragma unroll 1
+                                for (int e = 0; e < 8 * C::kSlabs; ++e) {
+                                    const uint4 x = *piece(e);
+                                    *piece(e) = seen ? make_uint4(real2<BF>(x.x), real2<BF>(x.y), real2<BF>(x.z), real2<BF>(x.w)) : make_uint4(0, 0, 0, 0);
+                                }
+                                if (seen) atomicOr(words + 3, 2u);
+                            }
+                        }
+                        fence_async_proxy();
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(v_ready(s));
                 }
             }
         }
@@ -584,21 +665,6 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                         }
                         l *= less; m = mn; unit = unit_now;
                     }
-                    if constexpr (!kQuant) {
-                        // values that no row of the unit sees are zeroed in shared memory: a weight of 0 does not silence a NaN
-                        const bool edge = key0 + kBN > g.hi || (a.window && key0 < g.lo && key0 + kBN > int(a.sinks));
-                        if (edge && w == 0) {
-                            if (!(ok = WAIT(kv_full(int(iv % C::kStages)), (iv / C::kStages) & 1))) break;
-                            const int key = key0 + r;
-                            if (!(key < g.hi && (!a.window || key >= g.lo || key < int(a.sinks)))) {
-                                for (int d = 0; d < C::kSlabs; ++d)
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e)
-                                        *reinterpret_cast<uint4*>(smem + C::kOffRing + int(iv % C::kStages) * C::kTile + d * (kBN * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
-                            }
-                            fence_async_proxy();
-                        }
-                    }
                     const uint64_t f2 = pack2(f, f), m2 = pack2(C::kRaise - m, C::kRaise - m);
                     uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
                     auto weights = [&](const uint32_t* v, int c0) {
@@ -656,6 +722,15 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 }
                 if (!(ok = WAIT(o_done(w), uint32_t(n_done - 1) & 1))) break;
                 tc_after();
+                if constexpr (!kQuant) {
+                    if (*static_cast<volatile uint32_t*>(words + 3) & 2) {
+#pragma unroll 1
+                        for (int j = 0; j < n; ++j)
+                            if (const int key0 = g.tile_key(g.t0 + j); g.mixed(a, sp, key0))
+                                add_unreal<BF, D>(a.b.page_table + uint64_t(g.seq) * a.b.table_stride, a.p.v, a.p.n_pages, a.p.page_shift, Hkv, uint32_t(g.h), key0, min(key0 + kBN, g.hi),
+                                                  g.lo, int(a.window), int(a.sinks), row_on ? place : -1, tO);
+                    }
+                }
             }
             const bool whole = g.t0 == 0 && g.t1 == g.tiles;
             const long long x0 = begin + g.from;
