@@ -588,8 +588,9 @@ cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head
         // joining (one request of 300 tokens: 10.3 us a call cut, 8.2 uncut) and costs some balance, little against it at this size.
         AttendArgs args = a;
         args.pad = tiles <= 16 ? uint32_t(tiles ? tiles : 1) : 0;
+        // (one at least: where max_q_len is 0 it reports the sequences that have tokens)
         const uint64_t blocks = args.pad ? units : (units * (tiles + 1) + kWarps - 1) / kWarps;
-        kernel<<<uint32_t(blocks < most ? blocks : most), kThreads, smem, s>>>(args);
+        kernel<<<uint32_t(blocks < 1 ? 1 : blocks < most ? blocks : most), kThreads, smem, s>>>(args);
         return cudaGetLastError();
     };
     using std::integral_constant;
