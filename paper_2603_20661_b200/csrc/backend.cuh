@@ -82,14 +82,15 @@ cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s);
 #ifdef __CUDACC__
 __device__ __forceinline__ void report(uint32_t* err, uint32_t bit) { atomicOr(err, bit); }
 
-// The place of sequence i in the batch; false (and reported) when its offsets or lengths break the batch's bounds, and
+// The place of sequence i of the batch's new tokens; false (and reported) when its offsets or lengths break the batch's bounds, and
 // the sequence is then skipped.
 __device__ __forceinline__ bool sequence(const SeqBatch& b, uint32_t i, int& q0, int& q_len, int& kv, uint32_t* err)
 {
     q0 = b.q_start[i]; q_len = b.q_start[i + 1] - q0; kv = b.kv_len[i];
     const bool ok = q0 >= 0 && q_len >= 0 && uint32_t(q_len) <= b.max_q_len && uint32_t(q0) + uint32_t(q_len) <= b.n_tokens &&
                     kv >= 0 && uint32_t(kv) <= b.max_kv_len;
-    if (!ok) report(err, beOffset);
+    // tokens before the first sequence or behind the last are nobody's: reported, since no block will come by them
+    if (!ok || (i == 0 && q0 != 0) || (i + 1 == b.n_seqs && uint32_t(q0) + uint32_t(q_len) != b.n_tokens)) report(err, beOffset);
     return ok;
 }
 

@@ -23,3 +23,22 @@ def test_no_new_token_allowed_but_some_given():
     assert torch.isfinite(case.attend()).all()
     case.backend.sync()
 
+
+
+@pytest.mark.parametrize("lens", [((1, 40), (1, 30)), ((40, 40), (40, 70)), ((40, 40), (1, 70))], ids=["decode", "prompts", "mixed"])
+@pytest.mark.parametrize("kind", ["behind", "before"])
+def test_tokens_that_no_sequence_holds_are_reported(lens, kind):
+    from paper_2603_20661_b200.binding import WwwsError
+    case = small(lens)
+    good = case.attend()
+    case.backend.sync()
+    start = case.q_start.tolist()
+    start = [start[0], start[1], start[2] - 1] if kind == "behind" else [1] + start[1:]
+    batch = case.backend.batch(torch.tensor(start, dtype=torch.int32, device="cuda"), case.kv_len, case.table, n_tokens=case.tokens, max_q_len=max(q for q, _ in lens),
+                               max_kv_len=max(kv for _, kv in lens))
+    case.backend.attend(case.cache, batch, case.q)
+    with pytest.raises(WwwsError) as e:
+        case.backend.sync()
+    assert e.value.status == 1 and "offsets" in str(e.value)
+    assert torch.equal(case.attend(), good)
+    case.backend.sync()
