@@ -253,6 +253,8 @@ class Backend:
             out, os = self._empty(q.shape, self.dtype, aside), self.n_heads * self.head_dim
         else:
             os = self._rows(out, self.n_heads, "out")
+        if window < 0 or sinks < 0:
+            raise ValueError(f"window and sinks must be 0 or more, got {window} and {sinks}")
         if q.shape[0] != batch.extra or out.shape[0] != batch.extra:
             raise ValueError(f"q and out must hold the batch's {batch.extra} tokens")
         if aside:

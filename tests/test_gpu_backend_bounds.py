@@ -42,3 +42,11 @@ def test_tokens_that_no_sequence_holds_are_reported(lens, kind):
     assert e.value.status == 1 and "offsets" in str(e.value)
     assert torch.equal(case.attend(), good)
     case.backend.sync()
+
+
+def test_windows_and_sinks_below_zero_are_refused():
+    """They would wrap to bounds that hide nothing, or show everything."""
+    case = small()
+    for more in (dict(window=-1), dict(sinks=-1), dict(window=8, sinks=-4)):
+        with pytest.raises(ValueError):
+            case.attend(**more)
