@@ -78,11 +78,11 @@ def _lib():
 
 
 class _Record:
-    """A C record, its address, and the tensors whose memory it names."""
-    __slots__ = ("c", "at", "tensors", "extra")
+    """A C record, its address, the tensors whose memory it names, and what of a backend's configuration their sizes follow."""
+    __slots__ = ("c", "at", "tensors", "of", "extra")
 
-    def __init__(self, c, tensors, extra=None):
-        self.c, self.at, self.tensors, self.extra = c, C.addressof(c), tensors, extra
+    def __init__(self, c, tensors, of, extra=None):
+        self.c, self.at, self.tensors, self.of, self.extra = c, C.addressof(c), tensors, of, extra
 
 
 class Backend:
@@ -107,6 +107,9 @@ class Backend:
         self._elem = {"16": self.dtype, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}[cache]
         cfg = BackendConfig(n_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_tokens, max_pages, max_rows,
                             self._codes[self.dtype], CACHES[cache])
+        # records made by another backend fit where these are equal
+        self._caches = ("cache", self.device, self._elem, n_pages, n_kv_heads, page_tokens, head_dim)
+        self._batches, self._shapings = ("batch", self.device, max_pages), ("shaping", self.device)
         self._h = None
         nbytes = C.c_uint64()
         self._check(self._lib.wwws_backend_workspace_bytes(C.byref(cfg), C.byref(nbytes)))
@@ -152,6 +155,11 @@ class Backend:
         t.record_stream(self._torch.cuda.current_stream(self.device))
         return t
 
+    @staticmethod
+    def _fits(record, of):
+        if record.of is not of and record.of != of:
+            raise ValueError(f"a {of[0]} of this backend's configuration is needed, got a {record.of[0]}" + (" of another's" if record.of[0] == of[0] else ""))
+
     def _array(self, t, dtype, name, dims=1):
         if t.dtype != dtype or t.dim() != dims or not t.is_contiguous() or t.device != self.device:
             raise ValueError(f"{name}: expected a contiguous {dims}-d {dtype} tensor on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -185,7 +193,7 @@ class Backend:
                 if t is None or tuple(self._array(t, self._torch.float32, name, 3).shape) != shape:
                     raise ValueError(f"{name}: expected float32 {shape}")
         ptr = [t.data_ptr() if t is not None else None for t in (k, v, k_scale, v_scale)]
-        return _Record(KvPages(*ptr), (k, v, k_scale, v_scale))
+        return _Record(KvPages(*ptr), (k, v, k_scale, v_scale), self._caches)
 
     def batch(self, q_start, kv_len, page_table, n_tokens, max_q_len, max_kv_len):
         """One step's sequences (device int32 tensors) and their host bounds."""
@@ -196,7 +204,7 @@ class Backend:
         if tuple(self._array(page_table, i32, "page_table", 2).shape) != (n, self.max_pages):
             raise ValueError(f"page_table: expected {(n, self.max_pages)}, got {tuple(page_table.shape)}")
         tensors = (q_start, kv_len, page_table)
-        return _Record(SeqBatch(*(t.data_ptr() for t in tensors), n, int(n_tokens), int(max_q_len), int(max_kv_len)), tensors, int(n_tokens))
+        return _Record(SeqBatch(*(t.data_ptr() for t in tensors), n, int(n_tokens), int(max_q_len), int(max_kv_len)), tensors, self._batches, int(n_tokens))
 
     def shaping(self, history=None, history_start=None, prompt_len=None, repetition=None, presence=None, frequency=None,
                 bias_id=None, bias_value=None, bias_start=None, mask=None, mask_index=None):
@@ -220,11 +228,13 @@ class Backend:
         c = ShapingRecord(*(t.data_ptr() if t is not None and t.numel() else None for t in tensors),
                           history.shape[0] if history is not None else 0, bias_id.shape[0] if bias_id is not None else 0,
                           mask.shape[0] if mask is not None else 0, mask.shape[1] if mask is not None else 0)
-        return _Record(c, tuple(tensors), rows.pop() if rows else None)
+        return _Record(c, tuple(tensors), self._shapings, rows.pop() if rows else None)
 
     # ---- the operators ----------------------------------------------------------------------
     def append(self, cache, batch, k, v):
         """Write the new tokens' keys and values ([n_tokens, n_kv_heads, head_dim]) to their pages."""
+        self._fits(cache, self._caches)
+        self._fits(batch, self._batches)
         ks, vs = self._rows(k, self.n_kv_heads, "k"), self._rows(v, self.n_kv_heads, "v")
         if k.shape[0] != batch.extra or v.shape[0] != batch.extra:
             raise ValueError(f"k and v must hold the batch's {batch.extra} tokens")
@@ -234,6 +244,8 @@ class Backend:
 
     def read(self, cache, batch, row_start, n_rows):
         """Whole sequences back: (k, v), each [n_rows, n_kv_heads, head_dim]; sequence i's tokens from row row_start[i] on."""
+        self._fits(cache, self._caches)
+        self._fits(batch, self._batches)
         self._array(row_start, self._torch.int32, "row_start")
         if row_start.shape[0] != batch.c.n_seqs + 1:
             raise ValueError(f"row_start: expected {batch.c.n_seqs + 1} entries, got {row_start.shape[0]}")
@@ -247,6 +259,8 @@ class Backend:
 
     def attend(self, cache, batch, q, out=None, scale=None, window=0, sinks=0):
         """Attention of the new tokens ([n_tokens, n_heads, head_dim]) over the cache; scale defaults to head_dim ** -0.5."""
+        self._fits(cache, self._caches)
+        self._fits(batch, self._batches)
         qs = self._rows(q, self.n_heads, "q")
         aside = self._aside()
         if out is None:
@@ -264,6 +278,7 @@ class Backend:
 
     def shape_logits(self, logits, shaping, out=None, tokens=True):
         """(shaped logits, token per row): penalties, biases and masks on logits [rows, vocab] (bf16, f16 or f32)."""
+        self._fits(shaping, self._shapings)
         dtype = self._codes.get(logits.dtype)
         if logits.dim() != 2 or dtype is None or logits.device != self.device or logits.stride(1) != 1 and logits.shape[1] > 1:
             raise ValueError(f"logits: expected [rows, vocab] of bf16, f16 or f32 with packed rows on {self.device}")

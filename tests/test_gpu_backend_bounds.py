@@ -50,3 +50,20 @@ def test_windows_and_sinks_below_zero_are_refused():
     for more in (dict(window=-1), dict(sinks=-1), dict(window=8, sinks=-4)):
         with pytest.raises(ValueError):
             case.attend(**more)
+
+
+def test_records_of_another_configuration_are_refused():
+    """A pool of fewer pages, a table of fewer columns or another kind of record would be read past its end.  Those of an equal backend are welcome."""
+    case, same, longer, other = small(), small(), small([(1, 400), (1, 30)]), small(cache="int8")
+    b = case.backend
+    for cache, batch in ((longer.cache, case.batch), (other.cache, case.batch), (case.cache, longer.batch), (case.batch, case.cache), (b.shaping(), case.batch)):
+        with pytest.raises(ValueError):
+            b.attend(cache, batch, case.q)
+        with pytest.raises(ValueError):
+            b.append(cache, batch, case.q[:, :1], case.q[:, :1])
+        with pytest.raises(ValueError):
+            b.read(cache, batch, torch.zeros(3, dtype=torch.int32, device="cuda"), 0)
+    with pytest.raises(ValueError):
+        b.shape_logits(torch.zeros(2, 8, device="cuda"), case.batch)
+    assert torch.equal(b.attend(same.cache, same.batch, same.q), case.attend())
+    b.sync()
