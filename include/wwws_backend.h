@@ -109,7 +109,8 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
  *   c times in its output           x = x - frequency[r] * c;  if c > 0: x = x - presence[r]
  *   v in its bias list              x = x + bias_value (the last entry of a repeated id holds; at most 2,047 entries a row)
  *   bit v of its mask is 0          x = -infinity
- * The history of row r, at most 2^20 - 1 tokens, is history[history_start[r] .. history_start[r + 1]): prompt_len[r] prompt tokens (none if NULL), then its output.  Masks are [n_masks][mask_stride] words of 32 tokens, lowest bit first; mask_index[r] < 0: no
+ * The history of row r, at most 2^20 - 1 tokens, is history[history_start[r] .. history_start[r + 1]): prompt_len[r]
+ * prompt tokens (none if NULL; all of it if prompt_len[r] is more), then its output.  Masks are [n_masks][mask_stride] words of 32 tokens, lowest bit first; mask_index[r] < 0: no
  * mask for the row; mask_index NULL: row r has mask r. */
 typedef struct {
     const int32_t* history; const int32_t* history_start; const int32_t* prompt_len; /* [..], [n_rows + 1], [n_rows] */

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_shape_logits(ShapeArgs a)
     if (a.s.history) {
         h0 = a.s.history_start[row]; h1 = a.s.history_start[row + 1];
         if (h0 < 0 || h1 < h0 || uint64_t(h1) > a.s.n_history || h1 - h0 > int(kMaxHistory)) { report(a.err, beOffset); h0 = h1 = 0; }
-        prompt_end = h0 + (a.s.prompt_len ? a.s.prompt_len[row] : 0);
+        prompt_end = h0 + (a.s.prompt_len ? min(max(a.s.prompt_len[row], 0), h1 - h0) : 0);
     }
     if (a.s.bias_id) {
         b0 = a.s.bias_start[row]; nb = a.s.bias_start[row + 1] - b0;

@@ -61,3 +61,14 @@ def test_most_history_that_a_row_may_have():
     s["prompt_len"] = torch.tensor([0], dtype=torch.int32)
     got, _ = run(backend(1), x.cuda(), s)
     assert torch.equal(got, plain(x, s, F32))
+
+
+@pytest.mark.parametrize("prompt", [2 ** 31 - 1, 2 ** 31 - 40, 50, -2 ** 31])
+def test_prompts_longer_than_their_history(prompt):
+    """A prompt length past the end of a row's history says that all of it is prompt, wherever the row's history starts; one below zero, none."""
+    s, x = inputs(3, 500, 40, 0, 9, 500)
+    s["prompt_len"][:] = prompt
+    got, token = run(backend(3), x.cuda(), s)
+    s["prompt_len"] = torch.full((3,), 40 if prompt > 0 else 0, dtype=torch.int32)
+    want = plain(x, s, F32)
+    assert torch.equal(got, want) and torch.equal(token, token_of(want))
