@@ -224,8 +224,11 @@ class Backend:
                 if t is not None and name in ("history_start", "prompt_len", "repetition", "presence", "frequency", "bias_start", "mask_index")}
         if len(rows) > 1:
             raise ValueError(f"the per-row arrays name different numbers of rows: {sorted(rows)}")
-        # an empty array is no array
-        c = ShapingRecord(*(t.data_ptr() if t is not None and t.numel() else None for t in tensors),
+        # An array that was given but is empty has no memory to point to; the kernels have to know of it all the same, to tell who asks for what it
+        # does not hold, and never read it (its length is 0).
+        # (A history or bias list without offsets, though, is none.)
+        nowhere, alone = self._ws.data_ptr(), {"history": history_start is None, "bias_id": bias_start is None}
+        c = ShapingRecord(*(None if t is None else t.data_ptr() if t.numel() else None if alone.get(name) else nowhere for name, t in zip(SHAPING_ARRAYS, tensors)),
                           history.shape[0] if history is not None else 0, bias_id.shape[0] if bias_id is not None else 0,
                           mask.shape[0] if mask is not None else 0, mask.shape[1] if mask is not None else 0)
         return _Record(c, tuple(tensors), self._shapings, rows.pop() if rows else None)

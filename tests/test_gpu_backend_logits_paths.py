@@ -72,3 +72,20 @@ def test_prompts_longer_than_their_history(prompt):
     s["prompt_len"] = torch.full((3,), 40 if prompt > 0 else 0, dtype=torch.int32)
     want = plain(x, s, F32)
     assert torch.equal(got, want) and torch.equal(token, token_of(want))
+
+
+def test_an_empty_set_of_masks():
+    """No masks in this step: rows that ask for one are reported, rows that do not are left alone."""
+    from paper_2603_20661_b200.binding import WwwsError
+    x = torch.randn(2, 100)
+    none = {"mask": torch.zeros(0, 4, dtype=torch.int32), "mask_index": torch.tensor([-1, -1], dtype=torch.int32)}
+    b = backend(2)
+    got, token = run(b, x.cuda(), none)
+    assert torch.equal(got, x) and torch.equal(token, token_of(x))
+    none["mask_index"][1] = 0
+    with pytest.raises(WwwsError) as e:
+        run(b, x.cuda(), none)
+    assert e.value.status == 8 and "mask" in str(e.value)
+    with pytest.raises(WwwsError) as e:
+        run(b, x.cuda(), {"mask": none["mask"]})                       # a mask per row is asked for
+    assert e.value.status == 1
