@@ -780,28 +780,36 @@ k_attend_tile(AttendArgs a, const __grid_constant__ CUtensorMap q_map, const __g
                 if (words[2]) {
                     __threadfence();
                     if (row_on && work) {
-                        float4 acc[D / 4 / C::kHalves];
-#pragma unroll
-                        for (int e = 0; e < D / 4 / C::kHalves; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        // what the parts' weights add up to, then 32 columns at a time, whose loads do not depend on one another
+                        auto slot_of = [&](uint32_t b) { return (b == blk0 ? first_slot : 2 * b) * 2 + w; };
                         float mm = kLow, ll = 0.0f;
                         for (uint32_t b = blk0; b <= blk1; ++b) {
-                            const uint32_t s = (b == blk0 ? first_slot : 2 * b) * 2 + w;
-                            const float2 ml = __ldcg(a.s.part_ml + s * kBM + r);
-                            const float4* part = reinterpret_cast<const float4*>(a.s.part_o) + (uint64_t(s) * (D / 4) + half * (D / 4 / C::kHalves)) * kBM + r;
-                            const float mn = fmaxf(mm, ml.x), f0 = ex2(mm - mn), f1 = ex2(ml.x - mn);
-                            mm = mn; ll = ll * f0 + ml.y * f1;
-#pragma unroll
-                            for (int e = 0; e < D / 4 / C::kHalves; ++e) {           // the loads of a part do not depend on one another
-                                const float4 v = __ldcg(part + e * kBM);
-                                acc[e].x = acc[e].x * f0 + v.x * f1; acc[e].y = acc[e].y * f0 + v.y * f1;
-                                acc[e].z = acc[e].z * f0 + v.z * f1; acc[e].w = acc[e].w * f0 + v.w * f1;
-                            }
+                            const float2 ml = __ldcg(a.s.part_ml + slot_of(b) * kBM + r);
+                            const float mn = fmaxf(mm, ml.x);
+                            ll = ll * ex2(mm - mn) + ml.y * ex2(ml.x - mn); mm = mn;
                         }
                         const float inv = ll > 0.0f ? (1.0f / C::kLift) / ll : ll;
+#pragma unroll 1
+                        for (int c = 0; c < D / 4 / C::kHalves; c += 8) {
+                            float4 acc[8];
 #pragma unroll
-                        for (int e = 0; e < D / 4 / C::kHalves; e += 2)
-                            *reinterpret_cast<uint4*>(dst + e * 8) = make_uint4(A::pack(acc[e].x * inv, acc[e].y * inv), A::pack(acc[e].z * inv, acc[e].w * inv),
-                                                                                A::pack(acc[e + 1].x * inv, acc[e + 1].y * inv), A::pack(acc[e + 1].z * inv, acc[e + 1].w * inv));
+                            for (int e = 0; e < 8; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+                            for (uint32_t b = blk0; b <= blk1; ++b) {
+                                const uint32_t s = slot_of(b);
+                                const float f = ex2(__ldcg(a.s.part_ml + s * kBM + r).x - mm);
+                                const float4* part = reinterpret_cast<const float4*>(a.s.part_o) + (uint64_t(s) * (D / 4) + half * (D / 4 / C::kHalves) + c) * kBM + r;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const float4 v = __ldcg(part + e * kBM);
+                                    acc[e].x += v.x * f; acc[e].y += v.y * f; acc[e].z += v.z * f; acc[e].w += v.w * f;
+                                }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; e += 2)
+                                *reinterpret_cast<uint4*>(dst + (c + e) * 8) = make_uint4(A::pack(acc[e].x * inv, acc[e].y * inv), A::pack(acc[e].z * inv, acc[e].w * inv),
+                                                                                          A::pack(acc[e + 1].x * inv, acc[e + 1].y * inv), A::pack(acc[e + 1].z * inv, acc[e + 1].w * inv));
+                        }
                     }
                     if (tid == 0) a.s.ticket[first_slot] = 0;
                 }
