@@ -17,7 +17,7 @@
 //   - The issuing warp stays converged and predicates each instruction on one lane: in a branch for one lane the descriptors went through
 //     vector registers, 90 clocks per instruction instead of 30.
 //   - Work is cut by key tiles, as in kernels_attend.cu: all (unit, tile) pairs laid end to end, an equal share for each of 148
-//     blocks, cut units joined by the last of their blocks.  The position of a share is found from closed sums (floor_sum), so
+//     blocks, cut units joined by the last of their blocks.  The position of a share is found from closed sums, so
 //     causal triangles, windows and ragged lengths need no plan.
 //   - K and V tiles come by TMA page by page into the 128-byte-swizzled layout that the matrix instructions read; pages that no row
 //     sees are fetched from beyond the tensor's end, which fills zeros.
@@ -73,17 +73,17 @@ template <bool BF, int CACHE, int D> struct Cfg {
 // A unit counts kUnitCost tiles more than it has: what loading its queries and storing its result costs, in tiles.
 constexpr int kUnitCost = 2;
 
-__device__ __forceinline__ long long floor_sum(long long n, long long m, long long a, long long b)    // sum_{i<n} floor((a i + b) / m), a, b >= 0
+// sum_{i<n} floor((a i + b) / kBN) = (sum_{i<n} (a i + b) - sum_{i<n} (a i + b) mod kBN) / kBN, a > 0, b >= 0.  kBN is a power of two, so with g = gcd(a, kBN) the
+// remainders repeat after p = kBN / g of them, and p neighbouring ones are b mod g, b mod g + g, b mod g + 2 g, ... in some order: whole periods have a
+// closed sum, and fewer than p (a is even: 64 at most) are left to add.
+__device__ __forceinline__ long long floors(long long n, int a, long long b)
 {
-    long long s = 0;
-    while (true) {        // Euclid's steps on (a, m), as in the published algorithm for lattice points under a line
-        if (a >= m) { s += (n - 1) * n / 2 * (a / m); a %= m; }
-        if (b >= m) { s += n * (b / m); b %= m; }
-        const long long y = a * n + b;
-        if (y < m) return s;
-        n = y / m; b = y % m;
-        const long long t = m; m = a; a = t;
-    }
+    if (n <= 0) return 0;
+    const int g = min(a & -a, kBN), p = kBN / g;
+    long long rest = n / p * (p * (int(b) & (g - 1)) + p * (p - 1) / 2 * g);
+    int x = int(b) & (kBN - 1);
+    for (int i = int(n) & (p - 1); i; --i) { rest += x; x = (x + a) & (kBN - 1); }
+    return (n * (n - 1) / 2 * a + n * b - rest) / kBN;
 }
 
 struct Seq {
@@ -113,11 +113,11 @@ struct Space {
         int first = 0;
         if (s.place0 + step <= 0) first = min(last, (-s.place0) / step);           // units that see nothing: one tile each
         total += first;
-        total += floor_sum(last - first, kBN, step, (long long)s.place0 + (long long)(first + 1) * step + kBN - 1);
+        total += floors(last - first, step, (long long)s.place0 + (long long)(first + 1) * step + kBN - 1);
         if (window) {                                                              // less floor((place0 + u step - window + 1) / 128) - sink tiles, where positive
             const long long b = (long long)s.place0 - window + 1 - (long long)sink_tiles * kBN;
             long long u0 = b >= 0 ? 0 : (-b + step - 1) / step;
-            if (u0 < last) total -= floor_sum(last - u0, kBN, step, b + u0 * step);
+            if (u0 < last) total -= floors(last - u0, step, b + u0 * step);
         }
         return total;
     }
