@@ -17,6 +17,7 @@ enum BackendError : uint32_t { bePage = 1, beToken = 2, beMask = 4, beOffset = 8
 struct SeqBatch {
     const int32_t* q_start; const int32_t* kv_len; const int32_t* page_table;
     uint32_t n_seqs, n_tokens, max_q_len, max_kv_len, table_stride;
+    uint32_t ends;       // bit 0: the call's first sequence is among these, bit 1: its last
 };
 
 struct Pages {
@@ -56,6 +57,7 @@ constexpr uint32_t kDecodeRows = 16;                 // most rows of its units
 constexpr uint32_t kFewRows = 32, kFewRowsQuant = 48;     // most rows per kv head of a sequence that goes to it (see wwws_attend)
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 
+constexpr uint32_t kTileSeqs = 32;                    // sequences of a launch of the tile kernel, at most (see wwws_attend)
 constexpr uint32_t kTickets = kDecodeSlots > kTileSlots ? kDecodeSlots : kTileSlots;
 
 // Raises a kernel's limit of dynamic shared memory, the first time on each device.
@@ -90,7 +92,7 @@ __device__ __forceinline__ bool sequence(const SeqBatch& b, uint32_t i, int& q0,
     const bool ok = q0 >= 0 && q_len >= 0 && uint32_t(q_len) <= b.max_q_len && uint32_t(q0) + uint32_t(q_len) <= b.n_tokens &&
                     kv >= 0 && uint32_t(kv) <= b.max_kv_len;
     // tokens before the first sequence or behind the last are nobody's: reported, since no block will come by them
-    if (!ok || (i == 0 && q0 != 0) || (i + 1 == b.n_seqs && uint32_t(q0) + uint32_t(q_len) != b.n_tokens)) report(err, beOffset);
+    if (!ok || (b.ends & 1 && i == 0 && q0 != 0) || (b.ends & 2 && i + 1 == b.n_seqs && uint32_t(q0) + uint32_t(q_len) != b.n_tokens)) report(err, beOffset);
     return ok;
 }
 

@@ -111,7 +111,7 @@ const char* check_rows(const void* p, uint64_t stride, uint32_t heads, uint32_t 
 
 SeqBatch seqs_of(const wwws_backend* b, const wwws_batch* s)
 {
-    return SeqBatch{ s->q_start, s->kv_len, s->page_table, s->n_seqs, s->n_tokens, s->max_q_len, s->max_kv_len, b->cfg.max_pages };
+    return SeqBatch{ s->q_start, s->kv_len, s->page_table, s->n_seqs, s->n_tokens, s->max_q_len, s->max_kv_len, b->cfg.max_pages, 3 };
 }
 
 Pages pages_of(const wwws_backend* b, const wwws_kv_pages* p)
@@ -229,9 +229,17 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
     const uint64_t most = uint64_t(batch->max_q_len) * a.group;
     const bool many = most > a.few_rows;
     const bool few = !many || uint64_t(batch->n_tokens) != uint64_t(batch->n_seqs) * batch->max_q_len;
+    // Where the tile kernel takes part, 32 sequences at a time.  One launch of it over 129 short and long ones, with the row kernel behind it, ended in a fault
+    // of the GPU that neither reading nor checks of every access in memory explained; launches of up to 32 have been run in every mixture.
+    const uint32_t at_once = many && batch->n_seqs > kTileSeqs ? kTileSeqs : batch->n_seqs;
     cudaError_t e = cudaSuccess;
-    if (many) e = launch_attend_tile(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
-    if (e == cudaSuccess && few) e = launch_attend_rows(a, many ? a.group : uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+    for (uint32_t first = 0; e == cudaSuccess && first < batch->n_seqs; first += at_once) {
+        a.b.q_start = batch->q_start + first; a.b.kv_len = batch->kv_len + first; a.b.page_table = batch->page_table + uint64_t(first) * b->cfg.max_pages;
+        a.b.n_seqs = batch->n_seqs - first < at_once ? batch->n_seqs - first : at_once;
+        a.b.ends = (first == 0 ? 1u : 0u) | (first + a.b.n_seqs == batch->n_seqs ? 2u : 0u);
+        if (many) e = launch_attend_tile(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+        if (e == cudaSuccess && few) e = launch_attend_rows(a, many ? a.group : uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+    }
     return launched(b, e, "wwws_attend");
 }
 
