@@ -4,8 +4,8 @@ The simulator dispatches a batch of requests over a network of providers; this e
 the most of them and runs their token counts through a small decoder with random weights, the way a serving backend does:
 prompts in chunks, then one token per request and step, all sequences together over one paged cache per layer
 (`Backend.append`, `Backend.attend`), the next token from logits under a repetition penalty (`Backend.shape_logits`, a
-temperature of zero).  Finished duels are judged under a mask that leaves three verdict tokens.  The measured rate is
-what `cap_true_tok_s` stands for in the simulator.
+temperature of zero).  Finished duels are judged under a mask that leaves three verdict tokens.  The measured rate stands
+where `cap_true_tok_s` does in the simulator; here most of it is this script's lists and copies, not the operators.
 
     python examples/answer_requests.py [--cache int8] [--requests 24]
 """
@@ -167,7 +167,7 @@ def main(argv=None):
     seconds = time.perf_counter() - t
     total = sum(len(p) for p in prompts) + sum(n_new)
     verdicts = serving.verdicts(torch.stack([logits[i] for i in sorted(logits)])[: max(1, min(duels, len(logits)))], [11, 12, 13])
-    print(f"provider {peer}: {len(prompts)} requests, {total} tokens in {seconds:.2f} s = {total / seconds:.0f} tokens/s (its cap_true_tok_s); "
+    print(f"provider {peer}: {len(prompts)} requests, {total} tokens in {seconds:.2f} s = {total / seconds:.0f} tokens/s (what cap_true_tok_s stands for); "
           f"verdicts {[('first', 'second', 'draw')[v] for v in verdicts[:4]]}")
     return serving
 

@@ -97,21 +97,25 @@ wwws_status wwws_cache_read(wwws_backend* b, const wwws_batch* batch, const wwws
  * sees key j <= p; with window > 0 only j > p - window or j < sinks.
  *   out = sum_j softmax_j(scale * q . k_j) v_j,   0 where nothing is seen.
  * q and out: [n_tokens][n_heads][head_dim] of the backend's dtype, 16-byte aligned, strides in elements (multiples of
- * 8).  Scores, softmax and sums are fp32; the softmax weights are rounded to the backend's dtype for the second
- * product.  A hidden key never reaches a row's result, whatever its key and value hold; a
- * visible one that is infinite or not a number does (a value: in its own column).  Results do not depend on what else is in the batch's pages, and repeat bit for bit. */
+ * 8).  Scores, softmax and sums are fp32; the softmax weights are rounded to 16 bits for the second product (f16 or bf16 as
+ * the backend; f16 for few rows over a quantised cache, whatever the backend), weights in f16 with a factor that keeps them
+ * out of its subnormals.  A hidden key never reaches a row's result, whatever its key and value hold (e4m3 codes that are
+ * no numbers, which wwws_cache_append never writes, excepted); a visible one that is infinite or not a number does (a
+ * value: in its own column).  Results do not depend on what else is in the batch's pages, and repeat bit for bit.
+ * Where a sequence may have more than 32 new rows per kv head (48 over a quantised cache; a row is a new token and one of
+ * its query heads), the call is launched 32 sequences at a time. */
 wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
                         uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window, uint32_t sinks);
 
-/* What is done to the logits of each row, all arrays DEVICE and caller-owned; a NULL array leaves its part out.  Per row r, in fp32
- * and in this order, x being the logit of token v:
+/* What is done to the logits of each row, all arrays DEVICE and caller-owned; a NULL array leaves its part out.  Per row
+ * r, in fp32 and in this order, x being the logit of token v:
  *   v in the row's history          x = x > 0 ? x / repetition[r] : x * repetition[r]
  *   c times in its output           x = x - frequency[r] * c;  if c > 0: x = x - presence[r]
  *   v in its bias list              x = x + bias_value (the last entry of a repeated id holds; at most 2,047 entries a row)
  *   bit v of its mask is 0          x = -infinity
  * The history of row r, at most 2^20 - 1 tokens, is history[history_start[r] .. history_start[r + 1]): prompt_len[r]
- * prompt tokens (none if NULL; all of it if prompt_len[r] is more), then its output.  Masks are [n_masks][mask_stride] words of 32 tokens, lowest bit first; mask_index[r] < 0: no
- * mask for the row; mask_index NULL: row r has mask r. */
+ * prompt tokens (none if NULL; all of it if prompt_len[r] is more), then its output.  Masks are [n_masks][mask_stride]
+ * words of 32 tokens, lowest bit first; mask_index[r] < 0: no mask for the row; mask_index NULL: row r has mask r. */
 typedef struct {
     const int32_t* history; const int32_t* history_start; const int32_t* prompt_len; /* [..], [n_rows + 1], [n_rows] */
     const float* repetition; const float* presence; const float* frequency;           /* [n_rows] */

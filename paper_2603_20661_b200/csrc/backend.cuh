@@ -113,7 +113,6 @@ template <bool BF> __device__ __forceinline__ uint32_t real2(uint32_t both)  // 
 // Two-element vectors of the activation type, and the float conversions the kernels need.
 template <bool BF> struct Act;
 template <> struct Act<true> {
-    using T = __nv_bfloat16;
     static __device__ __forceinline__ float lo(uint32_t v) { return __uint_as_float(v << 16); }
     static __device__ __forceinline__ float hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
     static __device__ __forceinline__ uint32_t pack(float a, float b)   // a in the low half, both rounded to nearest even
@@ -122,7 +121,6 @@ template <> struct Act<true> {
     }
 };
 template <> struct Act<false> {
-    using T = __half;
     static __device__ __forceinline__ float lo(uint32_t v) { return __half2float(__ushort_as_half(uint16_t(v))); }
     static __device__ __forceinline__ float hi(uint32_t v) { return __half2float(__ushort_as_half(uint16_t(v >> 16))); }
     static __device__ __forceinline__ uint32_t pack(float a, float b)

@@ -222,9 +222,10 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
     a.sinks = sinks < batch->max_kv_len ? sinks : batch->max_kv_len;
     a.err = b->err;
     // Sequences go by their rows per kv head (new tokens * group): few to the row kernel, which reads the cache once per 16 rows, more to the tile
-    // kernel.  24 requests of 3,000 tokens at head_dim 128, row kernel / tile kernel in us: 16-bit cache, 36 rows 96 / 67; e4m3, 30 rows 68 / 107,
-    // 36 and 48 rows 89 / 109, 60 rows 111 / 110; int8, 48 rows 96 / 124.  Both run only where the host's counts allow both kinds; the short
-    // sequences are then taken to have one new token.
+    // kernel.  24 requests of 3,000 tokens, row kernel / tile kernel in us: 16-bit cache at head_dim 64, 30 rows 36 / 42, 36 rows 46 / 42, at 128 58 / 54 and
+    // 73 / 53; e4m3 at 64, 48 rows 48 / 56, 60 rows 62 / 56, at 128 61 / 77 and 79 / 79; int8 at 64 50 / 60 and 65 / 62, at 128 66 / 91 and 87 / 91.  (One request of
+    // 60,000 tokens would favour the row kernel beyond these: 60 rows at 128 84 / 92 in 16 bits, 70 / 95 in e4m3.)  Both run only where the host's
+    // counts allow both kinds; the short sequences are then taken to have one new token.
     a.few_rows = b->cfg.cache == WWWS_CACHE_16 ? kFewRows : kFewRowsQuant;
     const uint64_t most = uint64_t(batch->max_q_len) * a.group;
     const bool many = most > a.few_rows;

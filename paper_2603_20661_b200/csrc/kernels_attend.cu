@@ -6,8 +6,9 @@
 // orders of magnitude below the tensor peak, so the warp-level mma.sync does: what matters is how many bytes are in flight and how few instructions
 // each costs.
 //   - Keys are the 16 rows of the operand, query rows its 8 columns (S^T = K Q^T, O^T = V^T P^T): no half-empty 16-row tile of queries, and
-//     kGroups = 1 or 2 groups of 8 rows share the fragments of a key.  (Up to 32 rows come here, as two units of 16: one unit of 32 took 82 us where
-//     these take 69, five drafted tokens of 24 requests, since it has registers for no more than half the warps' work in flight.)
+//     kGroups = 1 or 2 groups of 8 rows share the fragments of a key.  (Up to 32 rows come here, 48 over a quantised cache, as units of 16, or of 8 where no
+//     sequence has more or a call mixes prompts with single tokens.  One unit of 32 took 82 us where two of 16 take 66, five drafted tokens of 24 requests,
+//     since it has registers for no more than half the warps' work in flight.)
 //   - Work is cut by keys, not by sequences: all (sequence, row tile, kv head) units laid end to end in tiles of kTK keys, and block i takes
 //     the i-th equal share (the lengths are read on the device: no plan, no host copy of them).  A unit cut by a share boundary leaves a
 //     partial result (m, sum, weighted values) in the workspace; the last of its blocks to arrive joins them in block order,
@@ -139,8 +140,8 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
 
     const uint32_t ring = uint32_t(__cvta_generic_to_shared(smem)) + warp * S::kRing;
     const uint8_t* ring_g = smem + warp * S::kRing;
-    float* comb_o = reinterpret_cast<float*>(smem);                                   // [kWarps][16][D], over the drained rings
-    float2* comb_ml = reinterpret_cast<float2*>(comb_o + kWarps * kRows * D);   // [kWarps][16]
+    float* comb_o = reinterpret_cast<float*>(smem);                                   // [kWarps][kRows][D], over the drained rings
+    float2* comb_ml = reinterpret_cast<float2*>(comb_o + kWarps * kRows * D);   // [kWarps][kRows]
 
     for (unsigned long long x = begin; x < end;) {
         // the segment: unit (sequence i, row tile r, kv head h), its tiles [t0, t1)
@@ -585,7 +586,7 @@ cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head
         const uint64_t seen = (a.sinks + S::kTK - 1) / S::kTK + (uint64_t(a.window) + a.b.max_q_len) / S::kTK + 2;
         if (a.window && seen < tiles) tiles = seen;
         // Units of at most 16 tiles are not cut: each counts the same number of tiles and shares end between units, which saves the parts and their
-        // joining (one request of 300 tokens: 10.3 us a call cut, 8.2 uncut) and costs some balance, little against it at this size.
+        // joining (one request of 300 tokens: 8.7 us on the GPU cut, 5.8 uncut) and costs some balance, little against it at this size.
         AttendArgs args = a;
         args.pad = tiles <= 16 ? uint32_t(tiles ? tiles : 1) : 0;
         // (one at least: where max_q_len is 0 it reports the sequences that have tokens)

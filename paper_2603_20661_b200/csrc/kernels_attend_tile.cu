@@ -9,10 +9,10 @@
 // other turn its S into P.  m is allowed to lag behind the true maximum by a factor 2^kLag, so that O is rescaled (a pass over
 // tensor memory) in the first few tiles only; the result is the same sum, since numerator and denominator share m.
 //   - Floor per key tile at head_dim 128: 4 x 128^3 multiply-adds, 2,048 clocks of the tensor cores, and 2 x 16,384 exponentials at 16 a clock,
-//     as many.  Measured: about 3,500 clocks, two prompts of 8,192 tokens (32 heads, 8 kv heads, 1.10e12 operations) in 1.17 ms,
-//     943 TFLOP/s, 57 % of the library's rate for a large product.  What is left is the chain of a row tile: scores, softmax (2,150
-//     clocks), P back, PV, the next scores; the two row tiles hide half of it from one another, and tensor memory (2 x 128 columns of S, 2 x
-//     head_dim of O) has no room for a third.  Tried and slower: 64-key tiles with two S each (1.26 ms: the cost per tile is mostly fixed),
+//     as many.  Measured: two prompts of 8,192 tokens (32 heads, 8 kv heads, 1.10e12 operations) in 1.10 to 1.14 ms, 965 to 1,000 TFLOP/s, 60 % of
+//     the library's rate for a large product; back to back for seconds 1.14 ms at a median of 1,680 MHz under the power cap, about 4,000 clocks
+//     a tile with its share of loads and stores.  What is left is the chain of a row tile: scores, softmax, P back, PV, the next scores; the two row
+//     tiles hide half of it from one another, and tensor memory (2 x 128 columns of S, 2 x head_dim of O) has no room for a third.  Tried and slower: 64-key tiles with two S each (1.26 ms: the cost per tile is mostly fixed),
 //     polynomials for a quarter of the exponentials (1.22 against 1.10 ms: their constants cost more moves than the unit saves).
 //   - The issuing warp stays converged and predicates each instruction on one lane: in a branch for one lane the descriptors went through
 //     vector registers, 90 clocks per instruction instead of 30.
@@ -20,7 +20,7 @@
 //     blocks, cut units joined by the last of their blocks.  The position of a share is found from closed sums, so
 //     causal triangles, windows and ragged lengths need no plan.
 //   - K and V tiles come by TMA page by page into the 128-byte-swizzled layout that the matrix instructions read; pages that no row
-//     sees are fetched from beyond the tensor's end, which fills zeros.
+//     sees are fetched from beyond the tensor's end, which fills zeros.  16-bit values are looked through by a warp of its own (see there).
 //   - Quantised caches: codes land in a staging ring, two more warps widen them into the operand layout (exactly: 16-bit floats
 //     hold the codes); scales multiply the scores (keys) and the weights (values) in fp32.
 #include <cuda.h>
