@@ -12,6 +12,14 @@
  *   wwws_shape_logits                     repetition, presence and frequency penalties, biases and grammar masks on
  *                                         logits, and the token that a temperature of zero picks;
  *                                         a judge's verdict is a row whose mask leaves the verdict tokens
+ * and, where a request is answered with several drafted tokens or several hypotheses at a time:
+ *   wwws_rotate / wwws_rotate_append      norms of queries and keys for each head and their rotation by position, in one
+ *                                         pass, which may write keys and values to the cache as well
+ *   wwws_attend_tree                      attention of a tree of drafted tokens over the paged cache
+ *   wwws_cache_compact                    the accepted tokens of a tree moved together
+ *   wwws_select_beams                     the best continuations over a request's beams and the vocabulary
+ *   wwws_pages_fork / wwws_cache_copy     sequences continued, dropped, cut back and given room: their pages counted,
+ *                                         shared, taken and given back, and the pages copied that two would write
  *
  * Conventions are those of wwws.h: every call returns a wwws_status and never aborts; all device work is enqueued on
  * the stream given at creation and is asynchronous (wwws_backend_sync and wwws_destroy_backend synchronise it); the
@@ -107,6 +115,86 @@ wwws_status wwws_cache_read(wwws_backend* b, const wwws_batch* batch, const wwws
 wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
                         uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window, uint32_t sinks);
 
+/* The same for new tokens that are a tree of drafts behind the context, the kv_len[i] - q_len tokens before them: parents
+ * come before their children, and a new token sees the context and, of the new tokens j up to itself, those whose bit is set in
+ * its row of `tree` (DEVICE [n_tokens][tree_words], 32 places a word, lowest bit first; tree_words * 32 >= max_q_len):
+ * its ancestors and itself, as a rule.  It stands d places behind the context, d being how many new tokens it sees but itself
+ * (none if it sees none); the window is counted from there and hides context alone. */
+wwws_status wwws_attend_tree(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
+                             uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window,
+                             uint32_t sinks, const uint32_t* tree, uint32_t tree_words);
+
+/* How queries and keys are turned.  Of the first `dim` elements of a head (a multiple of 16, 16 .. head_dim), pair i < dim / 2
+ * is (i, dim / 2 + i), or (2 i, 2 i + 1) where interleaved is 1; the elements behind them stay where they are.  At position p
+ * pair (a, b) becomes (a cos t - b sin t, b cos t + a sin t), t = 2 pi p turns[i] / 2^64; the product wraps around exactly, so
+ * that no position is too far.  A weight makes x into x * weight / sqrt(mean(x^2) + eps) over the whole head before that.
+ * In fp32, rounded once. */
+typedef struct {
+    const uint64_t* turns;  /* DEVICE [dim / 2] turns of pair i per position, times 2^64: f / (2 pi) * 2^64 of f radians */
+    const uint8_t* axis;    /* DEVICE [dim / 2] by which of a token's positions pair i turns, < n_axes; NULL: the first */
+    const float* q_weight;  /* DEVICE [head_dim], 16-byte aligned; NULL: queries are not normed */
+    const float* k_weight;  /* the same for keys */
+    float eps;              /* >= 0 */
+    uint32_t dim, n_axes, interleaved; /* n_axes 1 .. 8 */
+} wwws_rotation;
+
+/* Norm and turn queries and keys of n_tokens tokens (any number): q and q_out [n_tokens][n_heads][head_dim], k and k_out
+ * [n_tokens][n_kv_heads][head_dim] of the backend's dtype, 16-byte aligned, strides in elements (multiples of 8); an output
+ * may be its input with the same stride, and overlaps nothing otherwise.  positions: DEVICE [n_tokens][n_axes]. */
+wwws_status wwws_rotate(wwws_backend* b, const wwws_rotation* rotation, uint32_t n_tokens, const int32_t* positions,
+                        const void* q, uint64_t q_stride, const void* k, uint64_t k_stride, void* q_out,
+                        uint64_t q_out_stride, void* k_out, uint64_t k_out_stride);
+
+/* The same for a batch's new tokens, turned keys and the values v written to their pages as wwws_cache_append does (a quantised
+ * cache takes its codes from the turned keys in fp32).  positions NULL: each token's place in its sequence, on every axis. */
+wwws_status wwws_rotate_append(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages,
+                               const wwws_rotation* rotation, const int32_t* positions, const void* q, uint64_t q_stride,
+                               const void* k, uint64_t k_stride, const void* v, uint64_t v_stride, void* q_out,
+                               uint64_t q_out_stride);
+
+/* Sequences continued.  All arrays DEVICE; tables are [sequences][max_pages of the configuration].  refs counts how often each
+ * page of the pool is held: by the sequences of `table`, a page in held[j] (<= max_pages) first entries of row j, and by whatever
+ * else the caller counts; a page of 0 is free.  New sequence i takes the first keep[i] tokens of old sequence source[i] (keep[i] <=
+ * held[source[i]] * page_tokens; source[i] < 0: it starts empty, keep[i] is not read) and gets pages for room[i] tokens, or
+ * keep[i] if that is more.  Old sequences end: what no new one continues is let go.
+ *   - Pages wholly within keep[i] tokens are shared.
+ *   - The page that keep[i] ends inside will be written further: it stays with the first new sequence that ends inside it if nobody
+ *     holds it otherwise; every other one gets a page of its own and a row of `moves`: from, to, tokens (else -1, -1, 0).
+ *   - Fresh pages are the free ones of lowest number, in the order of (sequence, place).  Where the pool runs out a place gets
+ *     -1, a page outside the pool, and the next wwws_backend_sync says WWWS_ERR_ALLOC.
+ * A bad new sequence is reported and left empty; entries behind a row's pages are 0.  refs_out may be refs; nothing else may overlap. */
+typedef struct {
+    const int32_t* refs; int32_t* refs_out;                                          /* [n_pages] */
+    const int32_t* table; const int32_t* held;                                       /* [n_old][max_pages], [n_old] */
+    const int32_t* source; const int32_t* keep; const int32_t* room;                 /* [n_new] */
+    int32_t* table_out; int32_t* held_out; int32_t* moves;                           /* [n_new][max_pages], [n_new], [n_new][3] */
+    uint32_t n_old, n_new;                                                           /* <= max_seqs */
+} wwws_fork;
+wwws_status wwws_pages_fork(wwws_backend* b, const wwws_fork* fork);
+
+/* Copy the first moves[i][2] tokens of page moves[i][0] to page moves[i][1] in each of n_layers pools (HOST array of records); a
+ * negative target is no copy.  No page is the target of two moves, nor the target of one and the source of another. */
+wwws_status wwws_cache_copy(wwws_backend* b, const wwws_kv_pages* layers, uint32_t n_layers, const int32_t* moves,
+                            uint32_t n_moves);
+
+/* Move new token path[i][m] of sequence i to place m of its new tokens, for m < path_len[i], in each of n_layers pools: path
+ * ([n_seqs][path_stride] DEVICE, path_stride <= 2048) ascends, so that a place is written after it is read.  The sequence's last page of
+ * new tokens is its own.  A bad path moves nothing and is reported. */
+wwws_status wwws_cache_compact(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* layers, uint32_t n_layers,
+                               const int32_t* path, const int32_t* path_len, uint32_t path_stride);
+
+/* The best `keep` (1 .. 128) continuations of each request: row r of logits (dtype as for wwws_shape_logits, stride in elements) is
+ * beam r % beams of request r / beams, beams 1 .. 256; n_rows is a multiple of beams and <= max_rows; vocab <= 2^24.
+ *   score(r, v) = total[r] + logits[r][v] - log sum_w exp(logits[r][w])
+ * with the sum's terms in fp32 and the rest in 64 bits; largest first, ties to the lowest (row, token), within a row in the logits' order.
+ * score [requests][keep] is rounded to fp32, parent (the row) and token are int32; where a request has fewer continuations above
+ * -infinity: -infinity, -1, -1.  A row whose total is -infinity, infinite or NaN, or that holds a NaN or +infinity, has none.
+ * scratch: DEVICE, 16-byte aligned, of wwws_beams_scratch_bytes, free again when the stream has passed the call. */
+wwws_status wwws_beams_scratch_bytes(uint32_t n_rows, uint32_t vocab, uint32_t dtype, uint32_t keep, uint64_t* bytes_out);
+wwws_status wwws_select_beams(wwws_backend* b, uint32_t n_rows, uint32_t beams, uint32_t vocab, uint32_t dtype,
+                              const void* logits, uint64_t stride, const float* total, uint32_t keep, void* scratch,
+                              uint64_t scratch_bytes, float* score, int32_t* parent, int32_t* token);
+
 /* What is done to the logits of each row, all arrays DEVICE and caller-owned; a NULL array leaves its part out.  Per row
  * r, in fp32 and in this order, x being the logit of token v:
  *   v in the row's history          x = x > 0 ? x / repetition[r] : x * repetition[r]
@@ -134,7 +222,8 @@ wwws_status wwws_shape_logits(wwws_backend* b, const wwws_shaping* shaping, uint
 
 /* Wait for the stream and report what the kernels found wrong since the last call: WWWS_ERR_INDEX (a page, token or
  * mask id out of range), WWWS_ERR_ARG (offsets or lengths outside the batch's bounds), WWWS_ERR_TIMEOUT (a wait inside
- * wwws_attend ran out after about two seconds: its outputs are not to be trusted; the next call starts clean). */
+ * wwws_attend or wwws_attend_tree ran out after about two seconds: its outputs are not to be trusted; the next call starts clean),
+ * WWWS_ERR_ALLOC (the page pool ran out in wwws_pages_fork). */
 wwws_status wwws_backend_sync(wwws_backend* b);
 
 const char* wwws_backend_last_error(const wwws_backend* b);

@@ -13,6 +13,16 @@ library's CUDA kernels; there is no fallback.
     logits, token = b.shape_logits(logits, b.shaping(history=..., history_start=..., repetition=...))
     b.sync()                                                 # raises if a kernel met a bad id
 
+With several drafted tokens or several beams per request:
+
+    rotation = b.rotation(128, theta=1e6, q_weight=..., k_weight=...)
+    q = b.rotate_append(cache, batch, q, k, v, rotation)     # norms, rotation and the write to the cache in one pass
+    o = b.attend(cache, batch, q, tree=masks)                # the new tokens are a tree
+    b.compact(caches, batch, path, path_len)                 # accepted tokens to their places, caches = b.caches([cache of each layer])
+    score, parent, token = b.select_beams(logits, totals, beams=4, keep=8)
+    refs, table, held, moves = b.fork(refs, table, held, source, keep, room)
+    b.copy_pages(caches, moves)                              # the pages that two sequences would write
+
 Calls are enqueued on the stream that was current at creation (or the one given).  Tensors that a caller fills on another
 stream must be ready before the call; the binding records the backend's stream on them, so that their memory is not
 handed out again before the call has run.
@@ -20,11 +30,13 @@ handed out again before the call has run.
 from __future__ import annotations
 
 import ctypes as C
+from fractions import Fraction
 
 from .binding import WwwsError, load
 
 EXPORTS = ("wwws_backend_workspace_bytes", "wwws_create_backend", "wwws_destroy_backend", "wwws_cache_append", "wwws_cache_read",
-           "wwws_attend", "wwws_shape_logits", "wwws_backend_sync", "wwws_backend_last_error")
+           "wwws_attend", "wwws_attend_tree", "wwws_rotate", "wwws_rotate_append", "wwws_pages_fork", "wwws_cache_copy", "wwws_cache_compact",
+           "wwws_beams_scratch_bytes", "wwws_select_beams", "wwws_shape_logits", "wwws_backend_sync", "wwws_backend_last_error")
 CACHES = {"16": 0, "int8": 1, "e4m3": 2}
 
 
@@ -51,6 +63,18 @@ class ShapingRecord(C.Structure):
                                                             ("n_masks", C.c_uint32), ("mask_stride", C.c_uint32)]
 
 
+class RotationRecord(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("turns", "axis", "q_weight", "k_weight")] + [("eps", C.c_float)] + [(k, C.c_uint32) for k in ("dim", "n_axes", "interleaved")]
+
+
+class ForkRecord(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("refs", "refs_out", "table", "held", "source", "keep", "room", "table_out", "held_out", "moves")] + \
+               [("n_old", C.c_uint32), ("n_new", C.c_uint32)]
+
+
+# One turn in radians, to more digits than any frequency's 2^-64 of a turn needs.
+TAU = Fraction(6283185307179586476925286766559005768394, 10 ** 39)
+
 _ready = False
 
 
@@ -66,6 +90,14 @@ def _lib():
             "wwws_cache_append": [vp, vp, vp, vp, u64, vp, u64],
             "wwws_cache_read": [vp, vp, vp, vp, u64, vp, vp],
             "wwws_attend": [vp, vp, vp, vp, u64, vp, u64, C.c_float, u32, u32],
+            "wwws_attend_tree": [vp, vp, vp, vp, u64, vp, u64, C.c_float, u32, u32, vp, u32],
+            "wwws_rotate": [vp, vp, u32, vp, vp, u64, vp, u64, vp, u64, vp, u64],
+            "wwws_rotate_append": [vp, vp, vp, vp, vp, vp, u64, vp, u64, vp, u64, vp, u64],
+            "wwws_pages_fork": [vp, vp],
+            "wwws_cache_copy": [vp, vp, u32, vp, u32],
+            "wwws_cache_compact": [vp, vp, vp, u32, vp, vp, u32],
+            "wwws_beams_scratch_bytes": [u32, u32, u32, u32, C.POINTER(u64)],
+            "wwws_select_beams": [vp, u32, u32, u32, u32, vp, u64, vp, u32, vp, u64, vp, vp, vp],
             "wwws_shape_logits": [vp, vp, u32, u32, u32, vp, u64, vp, u64, vp],
             "wwws_backend_sync": [vp],
         }
@@ -110,6 +142,7 @@ class Backend:
         # records made by another backend fit where these are equal
         self._caches = ("cache", self.device, self._elem, n_pages, n_kv_heads, page_tokens, head_dim)
         self._batches, self._shapings = ("batch", self.device, max_pages), ("shaping", self.device)
+        self._layers, self._rotations = ("list of caches", *self._caches[1:]), ("rotation", self.device, head_dim)
         self._h = None
         nbytes = C.c_uint64()
         self._check(self._lib.wwws_backend_workspace_bytes(C.byref(cfg), C.byref(nbytes)))
@@ -125,6 +158,11 @@ class Backend:
     def _check(self, status):
         if status:
             raise WwwsError(status, self._lib.wwws_backend_last_error(self._h).decode())
+
+    def _check_plain(self, status):
+        """Of a call that has no handle."""
+        if status:
+            raise WwwsError(status, self._lib.wwws_backend_last_error(None).decode())
 
     def close(self):
         if getattr(self, "_h", None):
@@ -233,6 +271,37 @@ class Backend:
                           mask.shape[0] if mask is not None else 0, mask.shape[1] if mask is not None else 0)
         return _Record(c, tuple(tensors), self._shapings, rows.pop() if rows else None)
 
+    def caches(self, caches):
+        """The caches of a model's layers as one record, for what moves tokens in all of them."""
+        for c in caches:
+            self._fits(c, self._caches)
+        return _Record((KvPages * len(caches))(*(c.c for c in caches)), tuple(t for c in caches for t in c.tensors), self._layers, len(caches))
+
+    def rotation(self, dim, theta=10000.0, frequencies=None, axes=None, interleaved=False, q_weight=None, k_weight=None, eps=1e-6):
+        """How queries and keys are turned: the first `dim` elements of a head, pair i by frequencies[i] radians per position (default
+        theta ** (-2 i / dim)) along axis axes[i] of the positions (default the only one).  Pairs are (i, dim / 2 + i), interleaved (2 i, 2 i + 1).
+        q_weight, k_weight: float32 [head_dim], the weights of a norm over the head before that."""
+        torch = self._torch
+        if dim < 16 or dim % 16 or dim > self.head_dim:
+            raise ValueError(f"dim must be a multiple of 16, 16 .. {self.head_dim}, got {dim}")
+        if frequencies is None:
+            frequencies = [float(theta) ** (-2.0 * i / dim) for i in range(dim // 2)]
+        axes = list(axes) if axes is not None else None
+        if len(frequencies) != dim // 2 or axes is not None and len(axes) != dim // 2:
+            raise ValueError(f"frequencies and axes must name {dim // 2} pairs")
+        if axes is not None and not all(0 <= a < 8 for a in axes):
+            raise ValueError("axes must be 0 .. 7")
+        turns = [round(Fraction(float(f)) / TAU * 2 ** 64) % 2 ** 64 for f in frequencies]
+        for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None and self._array(t, torch.float32, name).shape[0] != self.head_dim:
+                raise ValueError(f"{name}: expected {self.head_dim} entries, got {t.shape[0]}")
+        with torch.cuda.stream(self._stream):
+            turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=self.device)
+            axis = torch.tensor(axes, dtype=torch.uint8, device=self.device) if axes is not None else None
+        n_axes = max(axes) + 1 if axes is not None else 1
+        tensors = (turns, axis, q_weight, k_weight)
+        return _Record(RotationRecord(*(None if t is None else t.data_ptr() for t in tensors), eps, dim, n_axes, int(bool(interleaved))), tensors, self._rotations, n_axes)
+
     # ---- the operators ----------------------------------------------------------------------
     def append(self, cache, batch, k, v):
         """Write the new tokens' keys and values ([n_tokens, n_kv_heads, head_dim]) to their pages."""
@@ -260,8 +329,10 @@ class Backend:
         self._check(self._lib.wwws_cache_read(self._h, batch.at, cache.at, row_start.data_ptr(), n_rows, k.data_ptr(), v.data_ptr()))
         return k, v
 
-    def attend(self, cache, batch, q, out=None, scale=None, window=0, sinks=0):
-        """Attention of the new tokens ([n_tokens, n_heads, head_dim]) over the cache; scale defaults to head_dim ** -0.5."""
+    def attend(self, cache, batch, q, out=None, scale=None, window=0, sinks=0, tree=None):
+        """Attention of the new tokens ([n_tokens, n_heads, head_dim]) over the cache; scale defaults to head_dim ** -0.5.
+        tree: int32 [n_tokens, words], the new tokens are drafts behind the context and see those whose bits are set in their row (their
+        ancestors and themselves); 32 places a word, lowest bit first."""
         self._fits(cache, self._caches)
         self._fits(batch, self._batches)
         qs = self._rows(q, self.n_heads, "q")
@@ -274,17 +345,137 @@ class Backend:
             raise ValueError(f"window and sinks must be 0 or more, got {window} and {sinks}")
         if q.shape[0] != batch.extra or out.shape[0] != batch.extra:
             raise ValueError(f"q and out must hold the batch's {batch.extra} tokens")
+        if tree is not None and self._array(tree, self._torch.int32, "tree", 2).shape[0] != batch.extra:
+            raise ValueError(f"tree: expected a row for each of the batch's {batch.extra} tokens, got {tree.shape[0]}")
         if aside:
-            self._used(q, out, *cache.tensors, *batch.tensors)
-        self._check(self._lib.wwws_attend(self._h, batch.at, cache.at, q.data_ptr(), qs, out.data_ptr(), os, self._scale if scale is None else scale, window, sinks))
+            self._used(q, out, tree, *cache.tensors, *batch.tensors)
+        given = self._h, batch.at, cache.at, q.data_ptr(), qs, out.data_ptr(), os, self._scale if scale is None else scale, window, sinks
+        self._check(self._lib.wwws_attend(*given) if tree is None else self._lib.wwws_attend_tree(*given, tree.data_ptr(), tree.shape[1]))
         return out
+
+    def _given_or_new(self, out, like, heads, name, aside):
+        if out is None:
+            return self._empty(like.shape, self.dtype, aside), heads * self.head_dim
+        if out.shape != like.shape:
+            raise ValueError(f"{name}: expected {tuple(like.shape)}, got {tuple(out.shape)}")
+        return out, self._rows(out, heads, name)
+
+    def _positions(self, positions, n_tokens, rotation):
+        if positions.dim() == 1 and rotation.extra == 1:
+            positions = positions.unsqueeze(1)
+        if tuple(self._array(positions, self._torch.int32, "positions", 2).shape) != (n_tokens, rotation.extra):
+            raise ValueError(f"positions: expected {(n_tokens, rotation.extra)}, got {tuple(positions.shape)}")
+        return positions
+
+    def rotate(self, q, k, positions, rotation, q_out=None, k_out=None):
+        """(q, k) normed and turned: q [n_tokens, n_heads, head_dim], k [n_tokens, n_kv_heads, head_dim], positions int32 [n_tokens] or
+        [n_tokens, axes].  An output may be its input."""
+        self._fits(rotation, self._rotations)
+        qs, ks = self._rows(q, self.n_heads, "q"), self._rows(k, self.n_kv_heads, "k")
+        n = q.shape[0]
+        if k.shape[0] != n:
+            raise ValueError(f"q and k hold different numbers of tokens: {n} and {k.shape[0]}")
+        positions = self._positions(positions, n, rotation)
+        aside = self._aside()
+        q_out, qos = self._given_or_new(q_out, q, self.n_heads, "q_out", aside)
+        k_out, kos = self._given_or_new(k_out, k, self.n_kv_heads, "k_out", aside)
+        if aside:
+            self._used(q, k, q_out, k_out, positions, *rotation.tensors)
+        self._check(self._lib.wwws_rotate(self._h, rotation.at, n, positions.data_ptr(), q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos))
+        return q_out, k_out
+
+    def rotate_append(self, cache, batch, q, k, v, rotation, positions=None, q_out=None):
+        """The new tokens' queries normed and turned; their keys, normed and turned too, and values written to their pages.  positions
+        default to the tokens' places in their sequences."""
+        self._fits(cache, self._caches)
+        self._fits(batch, self._batches)
+        self._fits(rotation, self._rotations)
+        qs, ks, vs = self._rows(q, self.n_heads, "q"), self._rows(k, self.n_kv_heads, "k"), self._rows(v, self.n_kv_heads, "v")
+        if q.shape[0] != batch.extra or k.shape[0] != batch.extra or v.shape[0] != batch.extra:
+            raise ValueError(f"q, k and v must hold the batch's {batch.extra} tokens")
+        if positions is not None:
+            positions = self._positions(positions, batch.extra, rotation)
+        aside = self._aside()
+        q_out, qos = self._given_or_new(q_out, q, self.n_heads, "q_out", aside)
+        if aside:
+            self._used(q, k, v, q_out, positions, *cache.tensors, *batch.tensors, *rotation.tensors)
+        self._check(self._lib.wwws_rotate_append(self._h, batch.at, cache.at, rotation.at, positions.data_ptr() if positions is not None else None, q.data_ptr(), qs, k.data_ptr(), ks,
+                                                 v.data_ptr(), vs, q_out.data_ptr(), qos))
+        return q_out
+
+    def compact(self, caches, batch, path, path_len):
+        """Move new token path[i, m] (int32 [n_seqs, most], ascending) of sequence i to place m of its new tokens, m < path_len[i], in every layer."""
+        self._fits(caches, self._layers)
+        self._fits(batch, self._batches)
+        n = batch.c.n_seqs
+        if self._array(path, self._torch.int32, "path", 2).shape[0] != n or self._array(path_len, self._torch.int32, "path_len").shape[0] != n:
+            raise ValueError(f"path and path_len must name the batch's {n} sequences")
+        if self._aside():
+            self._used(path, path_len, *caches.tensors, *batch.tensors)
+        self._check(self._lib.wwws_cache_compact(self._h, batch.at, caches.at, caches.extra, path.data_ptr(), path_len.data_ptr(), path.shape[1]))
+
+    def fork(self, refs, page_table, held, source, keep, room, in_place=False):
+        """Sequences continued, dropped and given room: new sequence i takes the first keep[i] tokens of old sequence source[i] (none if
+        below 0) and pages for room[i] tokens.  refs int32 [n_pages] counts who holds a page (0: free), page_table int32 [old, max_pages] and
+        held int32 [old] are what the old sequences hold; all of them end.  Returns (refs, page_table, held, moves) of the new ones; moves
+        int32 [new, 3] is for `copy_pages`.  in_place: the counts are written over refs."""
+        i32 = self._torch.int32
+        n, m = self._array(source, i32, "source").shape[0], self._array(held, i32, "held").shape[0]
+        for t, name, shape in ((refs, "refs", (self.n_pages,)), (page_table, "page_table", (m, self.max_pages)), (keep, "keep", (n,)), (room, "room", (n,))):
+            if tuple(self._array(t, i32, name, len(shape)).shape) != shape:
+                raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+        aside = self._aside()
+        refs_out = refs if in_place else self._empty((self.n_pages,), i32, aside)
+        table_out, held_out, moves = self._empty((n, self.max_pages), i32, aside), self._empty((n,), i32, aside), self._empty((n, 3), i32, aside)
+        if aside:
+            self._used(refs, page_table, held, source, keep, room)
+        record = ForkRecord(*(t.data_ptr() for t in (refs, refs_out, page_table, held, source, keep, room, table_out, held_out, moves)), m, n)
+        self._check(self._lib.wwws_pages_fork(self._h, C.addressof(record)))
+        return refs_out, table_out, held_out, moves
+
+    def copy_pages(self, caches, moves):
+        """Copy the first tokens of pages to other pages in every layer: moves int32 [n, 3] of (from, to, tokens), to < 0: none."""
+        self._fits(caches, self._layers)
+        if self._array(moves, self._torch.int32, "moves", 2).shape[1] != 3:
+            raise ValueError(f"moves: expected [n, 3], got {tuple(moves.shape)}")
+        if self._aside():
+            self._used(moves, *caches.tensors)
+        self._check(self._lib.wwws_cache_copy(self._h, caches.at, caches.extra, moves.data_ptr(), moves.shape[0]))
+
+    def _logits(self, logits):
+        dtype = self._codes.get(logits.dtype)
+        if logits.dim() != 2 or dtype is None or logits.device != self.device or logits.stride(1) != 1 and logits.shape[1] > 1:
+            raise ValueError(f"logits: expected [rows, vocab] of bf16, f16 or f32 with packed rows on {self.device}")
+        return dtype
+
+    def select_beams(self, logits, totals, beams, keep):
+        """The best continuations of each request: logits [requests * beams, vocab] (bf16, f16 or f32), totals float32 [requests * beams].
+        Returns (score float32, parent int32, token int32), each [requests, keep], best first: total + log-softmax of the logits, the row it
+        continues, the token; -infinity, -1, -1 where a request has fewer."""
+        dtype = self._logits(logits)
+        rows, vocab = logits.shape
+        if self._array(totals, self._torch.float32, "totals").shape[0] != rows:
+            raise ValueError(f"totals: expected {rows} entries, got {totals.shape[0]}")
+        if beams < 1 or rows % beams:
+            raise ValueError(f"beams must divide the {rows} rows, got {beams}")
+        if keep < 1:
+            raise ValueError(f"keep must be 1 or more, got {keep}")
+        nbytes = C.c_uint64()
+        self._check_plain(self._lib.wwws_beams_scratch_bytes(rows, vocab, dtype, keep, C.byref(nbytes)))
+        aside = self._aside()
+        scratch = self._empty((nbytes.value,), self._torch.uint8, aside)
+        shape = (rows // beams, keep)
+        score, parent, token = self._empty(shape, self._torch.float32, aside), self._empty(shape, self._torch.int32, aside), self._empty(shape, self._torch.int32, aside)
+        if aside:
+            self._used(logits, totals)
+        self._check(self._lib.wwws_select_beams(self._h, rows, beams, vocab, dtype, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, totals.data_ptr(), keep, scratch.data_ptr(),
+                                                nbytes.value, score.data_ptr(), parent.data_ptr(), token.data_ptr()))
+        return score, parent, token
 
     def shape_logits(self, logits, shaping, out=None, tokens=True):
         """(shaped logits, token per row): penalties, biases and masks on logits [rows, vocab] (bf16, f16 or f32)."""
         self._fits(shaping, self._shapings)
-        dtype = self._codes.get(logits.dtype)
-        if logits.dim() != 2 or dtype is None or logits.device != self.device or logits.stride(1) != 1 and logits.shape[1] > 1:
-            raise ValueError(f"logits: expected [rows, vocab] of bf16, f16 or f32 with packed rows on {self.device}")
+        dtype = self._logits(logits)
         rows, vocab = logits.shape
         if shaping.extra is not None and shaping.extra != rows:
             raise ValueError(f"the shaping names {shaping.extra} rows, logits has {rows}")

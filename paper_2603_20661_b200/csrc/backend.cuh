@@ -12,7 +12,7 @@
 namespace wwws {
 
 // Kinds of device-side problems, kept as a bit mask in the workspace's error word.
-enum BackendError : uint32_t { bePage = 1, beToken = 2, beMask = 4, beOffset = 8, beTimeout = 16 };
+enum BackendError : uint32_t { bePage = 1, beToken = 2, beMask = 4, beOffset = 8, beTimeout = 16, bePool = 32 };
 
 struct SeqBatch {
     const int32_t* q_start; const int32_t* kv_len; const int32_t* page_table;
@@ -42,6 +42,45 @@ struct AttendArgs {
     uint32_t pad;        // row kernel: 0, or the tiles that every unit counts (see kernels_attend.cu)
     uint32_t few_rows;   // sequences with at most this many rows per kv head (new tokens * group) go to the row kernel, others to the tile kernel
     uint32_t* err;
+    const uint32_t* tree; uint32_t tree_words;      // bits of the new tokens that each new token sees (see wwws_attend_tree); not read by the kernels without trees
+};
+
+struct RotateArgs {
+    wwws_rotation r;
+    SeqBatch b; Pages p;                             // with the write to the cache alone
+    const int32_t* positions;                        // NULL: the tokens' places
+    const uint8_t* q; const uint8_t* k; const uint8_t* v; uint8_t* q_out; uint8_t* k_out;
+    uint64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;      // in elements
+    uint32_t n_tokens, n_heads, n_kv_heads;
+    uint32_t parts;                                  // warps of a token
+    uint32_t* err;
+};
+
+struct ForkArgs {
+    const int32_t* refs; int32_t* refs_out;
+    const int32_t* table; const int32_t* held; const int32_t* source; const int32_t* keep; const int32_t* room;
+    int32_t* table_out; int32_t* held_out; int32_t* moves;
+    uint32_t n_old, n_new, n_pages, max_pages, page_shift;
+    uint32_t* owner; uint32_t* need;                 // workspace: [n_pages], [max_seqs]
+    uint32_t* err;
+};
+
+constexpr uint32_t kMaxLayers = 64;                  // layers of a launch: their records are parameters of the kernel
+struct Layer { uint8_t* k; uint8_t* v; float* k_scale; float* v_scale; };
+struct LayerArgs {
+    Layer layer[kMaxLayers];
+    uint32_t n_pages, n_kv_heads, page_shift, row_bytes;
+    uint32_t* err;
+};
+
+constexpr uint32_t kMaxBeams = 256, kMaxKeep = 128;
+struct BeamArgs {
+    const uint8_t* in; uint64_t stride;
+    const float* total;
+    float2* stat; unsigned long long* keys;          // per request: [beams][slices] (c, sum), [keep][beams][slices] keys
+    uint32_t* ticket;                                // [requests], zero between calls
+    float* score; int32_t* parent; int32_t* token;
+    uint32_t beams, vocab, keep, slices;
 };
 
 struct ShapeArgs {
@@ -79,7 +118,14 @@ cudaError_t launch_cache_read(const SeqBatch& b, const Pages& p, const int32_t* 
                               uint32_t head_dim, int dtype, int cache, uint32_t* err, cudaStream_t s);
 cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_attend_tile(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
+cudaError_t launch_attend_rows_tree(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_rotate(RotateArgs a, bool append, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
+cudaError_t launch_fork(const ForkArgs& a, cudaStream_t s);
+cudaError_t launch_copy_pages(const LayerArgs& a, uint32_t n_layers, const int32_t* moves, uint32_t n_moves, cudaStream_t s);
+cudaError_t launch_compact(const LayerArgs& a, uint32_t n_layers, const SeqBatch& b, const int32_t* path, const int32_t* path_len, uint32_t path_stride, cudaStream_t s);
+uint64_t beams_scratch(uint32_t rows, uint32_t vocab, int dtype, uint32_t keep);
+cudaError_t launch_beams(BeamArgs a, uint32_t rows, int dtype, void* scratch, cudaStream_t s);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void report(uint32_t* err, uint32_t bit) { atomicOr(err, bit); }
@@ -94,6 +140,24 @@ __device__ __forceinline__ bool sequence(const SeqBatch& b, uint32_t i, int& q0,
     // tokens before the first sequence or behind the last are nobody's: reported, since no block will come by them
     if (!ok || (b.ends & 1 && i == 0 && q0 != 0) || (b.ends & 2 && i + 1 == b.n_seqs && uint32_t(q0) + uint32_t(q_len) != b.n_tokens)) report(err, beOffset);
     return ok;
+}
+
+// The new tokens rel .. rel + 31 (places behind the context) that the token of row `row` sees, a bit each; what lies before them is context: ones.
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t* tree, uint32_t words, int row, int rel)
+{
+    const uint32_t* w = tree + uint64_t(uint32_t(row)) * words;
+    auto word = [&](int i) { return i < 0 ? ~0u : uint32_t(i) < words ? __ldg(w + i) : 0u; };
+    return __funnelshift_r(word(rel >> 5), word((rel >> 5) + 1), uint32_t(rel) & 31u);
+}
+// How far behind the context a new token stands: the new tokens that it sees, itself not counted.
+__device__ __forceinline__ int tree_depth(const uint32_t* tree, uint32_t words, int row, int tok)
+{
+    int n = 0;
+    for (int i = 0; i * 32 <= tok; ++i) {
+        const uint32_t x = tree_bits(tree, words, row, i * 32);
+        n += __popc(tok - i * 32 >= 31 ? x : x & ((2u << (tok - i * 32)) - 1));
+    }
+    return max(n - 1, 0);
 }
 
 // A weight of 0 does not silence a value that is infinite or not a number, so the attention kernels look for these among the 16-bit values that some rows of a

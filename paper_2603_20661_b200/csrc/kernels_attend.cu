@@ -22,10 +22,17 @@
 // Fragments: mma.m16n8k16 leaves the order of the k index free as long as both operands agree.  For K Q^T a thread takes 16 consecutive bytes of
 // its key's row (8 or 16 elements = 2 or 4 k-steps) and the query fragments follow that order; for 8-bit values, where no transposing load
 // fits, a thread takes head_dim / 8 consecutive columns of four keys' rows and row tile i of V^T is columns 2i and 2i + 1 of each thread's.
+// With WWWS_TREE the new tokens are a tree (kernels_attend_tree.cu): one of them sees another where its mask has a bit, the context as before.
 #include "backend.cuh"
+
+#ifndef WWWS_TREE
+#define WWWS_TREE 0
+#endif
 
 namespace wwws {
 namespace {
+
+constexpr bool kTree = WWWS_TREE;
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr float kLow = -3.0e38f;            // below every score: 2^(x - kLow) is never formed, 2^(-inf - kLow) is 0
@@ -158,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
         const int n_rows = min(int(kRows), q_len * int(G) - int(row0));
         const int place0 = kv - q_len;                                   // place of the sequence's first new token
         const int first_place = place0 + int(row0 / G), last_place = place0 + int((row0 + n_rows - 1) / G);
-        const int lo_key = a.window ? max(0, first_place - int(a.window) + 1) : 0, hi_key = min(kv, last_place + 1);
+        const int lo_key = a.window ? max(0, (kTree ? place0 : first_place) - int(a.window) + 1) : 0, hi_key = min(kv, last_place + 1);
 
         // Query fragments (columns are rows n + 8 g), in the order in which the keys' chunks are taken.  Quantised: f16 times 2^e of the row, whose
         // largest element then lies in [2^14, 2^15); rm is what turns a product into x.
@@ -312,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                     }
                 }
             const float* scales = reinterpret_cast<const float*>(vt + S::kTile);
-            const bool masked = bad || key0 + TK - 1 > first_place || (a.window && key0 < last_place - int(a.window) + 1 && key0 + TK > int(a.sinks));
+            const bool masked = bad || key0 + TK - 1 > (kTree ? place0 - 1 : first_place) || (a.window && key0 < last_place - int(a.window) + 1 && key0 + TK > int(a.sinks));
             // value scales relative to the largest so far
             float vs[KT][2];
             if constexpr (kQuant) {
@@ -344,10 +351,25 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                     s[g][k][0] *= rm[g][0] * f0; s[g][k][1] *= rm[g][1] * f0; s[g][k][2] *= rm[g][0] * f1; s[g][k][3] *= rm[g][1] * f1;
                 }
                 if (masked) {
+                    uint32_t drafted[2] = { 0, 0 };
+                    int left[2] = { 0, 0 };                  // context up to here has left the window
+                    if constexpr (kTree) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int tok = place_of(g, e) - place0;
+                            drafted[e] = tree_bits(a.tree, a.tree_words, q0 + tok, key0 - place0);
+                            if (a.window) left[e] = place0 + tree_depth(a.tree, a.tree_words, q0 + tok, tok) - int(a.window);
+                        }
+                    }
 #pragma unroll
                     for (int k = 0; k < KT; ++k)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
+                            if constexpr (kTree) {
+                                const int at = k * 16 + n + 8 * (e >> 1), key = key0 + at;
+                                if (key > place_of(g, e & 1) || !(drafted[e & 1] >> at & 1u) || (a.window && key < place0 && key <= left[e & 1] && key >= int(a.sinks))) s[g][k][e] = -INFINITY;
+                                continue;
+                            }
                             const int key = key0 + k * 16 + n + 8 * (e >> 1), p = place_of(g, e & 1);
                             if (key > p || (a.window && key <= p - int(a.window) && key >= int(a.sinks))) s[g][k][e] = -INFINITY;
                         }
@@ -398,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                 }
             }
             if constexpr (!kQuant) {
-                if (masked && first_place != last_place) {   // (rows of one token see the same keys; five drafted tokens of 24 requests: 74.4 -> 76.9 us)
+                if (masked && (kTree || first_place != last_place)) {   // (rows of one token see the same keys; five drafted tokens of 24 requests: 74.4 -> 76.9 us)
                     uint8_t* values = smem + (vt - smem);
                     uint32_t top_half = 0;
 #pragma unroll
@@ -409,6 +431,11 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
                             auto value = [&](int d) { return uint32_t(*reinterpret_cast<const uint16_t*>(values + S::v_at(kk, d / 8) + d % 8 * 2)); };
                             auto sees = [&](int g, int e) {
                                 const int key = key0 + kk, p = place_of(g, e);
+                                if constexpr (kTree) {
+                                    const int tok = p - place0;
+                                    if (key >= place0) return key <= p && (tree_bits(a.tree, a.tree_words, q0 + tok, key - place0) & 1u) != 0;
+                                    return !a.window || key > place0 + tree_depth(a.tree, a.tree_words, q0 + tok, tok) - int(a.window) || key < int(a.sinks);
+                                }
                                 return key <= p && (!a.window || key > p - int(a.window) || key < int(a.sinks));
                             };
 #pragma unroll
@@ -571,6 +598,9 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
 }  // namespace
 
 // `rows`: rows per kv head of the longest sequence that comes here.
+#if WWWS_TREE
+#define launch_attend_rows launch_attend_rows_tree
+#endif
 cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s)
 {
     auto go = [&](auto bf, auto kind, auto dim, auto groups) -> cudaError_t {
