@@ -77,10 +77,10 @@ constexpr uint32_t kMaxBeams = 256, kMaxKeep = 128;
 struct BeamArgs {
     const uint8_t* in; uint64_t stride;
     const float* total;
-    float2* stat; unsigned long long* keys;          // per request: [beams][slices] (c, sum), [keep][beams][slices] keys
+    float2* stat; float4* top; unsigned long long* heads;      // scratch, per row: [slices] maximum and sum, [chunks] maxima of four pieces, [chunks] best keys
     uint32_t* ticket;                                // [requests], zero between calls
     float* score; int32_t* parent; int32_t* token;
-    uint32_t beams, vocab, keep, slices;
+    uint32_t beams, vocab, keep, slices, chunks, per_slice;    // chunks of a row and of a slice
 };
 
 struct ShapeArgs {
@@ -124,7 +124,7 @@ cudaError_t launch_rotate(RotateArgs a, bool append, uint32_t head_dim, int dtyp
 cudaError_t launch_fork(const ForkArgs& a, cudaStream_t s);
 cudaError_t launch_copy_pages(const LayerArgs& a, uint32_t n_layers, const int32_t* moves, uint32_t n_moves, cudaStream_t s);
 cudaError_t launch_compact(const LayerArgs& a, uint32_t n_layers, const SeqBatch& b, const int32_t* path, const int32_t* path_len, uint32_t path_stride, cudaStream_t s);
-uint64_t beams_scratch(uint32_t rows, uint32_t vocab, int dtype, uint32_t keep);
+uint64_t beams_scratch(uint32_t rows, uint32_t vocab, int dtype);
 cudaError_t launch_beams(BeamArgs a, uint32_t rows, int dtype, void* scratch, cudaStream_t s);
 
 #ifdef __CUDACC__

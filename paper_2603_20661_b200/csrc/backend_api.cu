@@ -408,7 +408,7 @@ wwws_status wwws_beams_scratch_bytes(uint32_t n_rows, uint32_t vocab, uint32_t d
 {
     if (!bytes_out) return fail(nullptr, WWWS_ERR_ARG, "bytes_out is NULL");
     if (n_rows > 65535 || vocab == 0 || vocab > (1u << 24) || dtype > WWWS_F32 || keep < 1 || keep > kMaxKeep) return fail(nullptr, WWWS_ERR_ARG, "n_rows must be <= 65535, vocab 1..2^24, dtype a wwws_dtype, keep 1..128");
-    *bytes_out = beams_scratch(n_rows, vocab, int(dtype), keep);
+    *bytes_out = beams_scratch(n_rows, vocab, int(dtype));
     return WWWS_OK;
 }
 
@@ -425,7 +425,7 @@ wwws_status wwws_select_beams(wwws_backend* b, uint32_t n_rows, uint32_t beams, 
     const uintptr_t size = dtype == WWWS_F32 ? 4 : 2;
     if (!logits || reinterpret_cast<uintptr_t>(logits) % size || stride < vocab) return fail(b, WWWS_ERR_ARG, "logits is NULL or not aligned to its elements, or its stride is below vocab");
     if (!total || !score || !parent || !token) return fail(b, WWWS_ERR_ARG, "total, score, parent or token is NULL");
-    if (!scratch || !aligned(scratch) || scratch_bytes < beams_scratch(n_rows, vocab, int(dtype), keep)) return fail(b, WWWS_ERR_ALLOC, "scratch is NULL, not 16-byte aligned or too small");
+    if (!scratch || !aligned(scratch) || scratch_bytes < beams_scratch(n_rows, vocab, int(dtype))) return fail(b, WWWS_ERR_ALLOC, "scratch is NULL, not 16-byte aligned or too small");
     ON_DEVICE(b);
     BeamArgs a{};
     a.in = static_cast<const uint8_t*>(logits); a.stride = stride; a.total = total; a.ticket = b->row_ticket; a.score = score; a.parent = parent; a.token = token;

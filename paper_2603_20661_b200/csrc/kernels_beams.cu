@@ -1,24 +1,32 @@
 // Beam search's selection: of every request, the best continuations over its beams and the vocabulary.
 //
-// score(beam, v) = total_beam + x_v - log sum_w exp(x_w).  Within a beam the order is that of the logits, so a block takes a slice of one row, keeps its
-// `keep` best logits and its part of the sum, and the last block of a request to arrive joins the slices: the rows' sums, then the best scores, in 64 bits.
-// Bound by HBM: the logits are read once (into registers, a slice is 256 threads * kVecs * 16 bytes) and nothing else is long.
-//   - Sum: sum_w 2^((x_w - m) L), m the slice's largest, L = log2 e in fp32, two elements at a time; the logarithm is m + log2(sum) / L in 64 bits.
-//   - Selection in one pass over registers: of 64 (or 256) groups of threads the keep-th largest maximum is a bound that at least `keep` elements
-//     reach, and hardly more do (-64 ln(1 - keep / 64) of them on random data); these are ranked by counting.  Keys are (value, lowest index first), all different,
-//     so neither the ranks nor the result depend on the order of arrival.  Slices with more than kMost elements at the bound (constant rows) take
-//     the largest key `keep` times instead.
+// score(beam, v) = total_beam + x_v - log sum_w exp(x_w), compared in 64 bits, ties to the lowest (beam, token).
+// Bound by HBM: the logits are read once and nothing else is long.
+//   - Stream: a warp takes chunks of a row, 64 bytes a lane, the next chunk's loads in flight meanwhile, and keeps nothing but each chunk's maximum and, per lane, a
+//     running maximum m and sum_w 2^((x_w - m) L), L = log2 e in fp32, two elements at a time; the logarithm is m + log2(sum) / L in 64 bits.  No barriers: blocks
+//     that kept the best of their slices as they went spent two thirds of their time at them (256 rows of 131,072 bf16 logits: 42 us).
+//   - Selection, by the last block of a request to arrive: the best `keep` elements lie in the `keep` chunks of largest maxima (in the order of score, beam,
+//     token: each of these holds one at least as good as any element elsewhere).  Those are found among the threads' maxima, read again, mostly from L2, and what
+//     reaches the last one's maximum is ranked by counting.
+//   - Where more than kMost elements or chunks reach a bound (constant rows) the best element is taken out `keep` times, the best of every chunk being kept in the scratch.
+//   - Element to lane goes by the token, not by the address: equal rows have equal sums to the bit, wherever they begin.  Rows off 16-byte boundaries are
+//     read at these all the same and shifted, the rest of a piece coming from the next lane.
 #include "backend.cuh"
 #include "tcgen.cuh"
 
 namespace wwws {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kMost = 1024;              // elements at or above a bound that are ranked at once
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMost = 1024;              // chunks or elements that are ranked at once
+constexpr int kVecs = 4;                 // 16-byte pieces of a lane and chunk
+constexpr uint32_t kHeld = 2048;         // chunks of a request whose maxima are kept at hand
 constexpr float kLog2e = 1.44269504f;
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// A sum relative to m as one relative to mn >= m; a NaN goes on into it.
+__device__ __forceinline__ float part_of(float s, float m, float mn) { return s == 0.0f ? 0.0f : s * ex2((m - mn) * kLog2e); }
 
 // Floats in the order of whole numbers (no NaN); 0 stands below all of them.
 __device__ __forceinline__ uint32_t ordered(float x) { const uint32_t b = __float_as_uint(x); return b & 0x80000000u ? ~b : b | 0x80000000u; }
@@ -27,6 +35,7 @@ __device__ __forceinline__ unsigned long long key_of(float x, uint32_t token) { 
 
 template <int DT> struct Elem {
     static constexpr int kPer = DT == WWWS_F32 ? 4 : 8, kSize = DT == WWWS_F32 ? 4 : 2;      // elements of 16 bytes
+    static constexpr uint32_t kChunk = kVecs * 32 * kPer;                                    // tokens
     static constexpr uint32_t kNone = DT == WWWS_F32 ? 0xff800000u : DT == WWWS_BF16 ? 0xff80ff80u : 0xfc00fc00u;      // -infinity
     static __device__ __forceinline__ float at(const uint4& v, int e)
     {
@@ -43,299 +52,460 @@ template <int DT> struct Elem {
         else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
     }
+    static __device__ __forceinline__ float element(const uint8_t* row, uint32_t token)
+    {
+        if constexpr (DT == WWWS_F32) return __ldg(reinterpret_cast<const float*>(row) + token);
+        else return Act<DT == WWWS_BF16>::lo(__ldg(reinterpret_cast<const uint16_t*>(row) + token));
+    }
     static __device__ __forceinline__ float largest(uint32_t w)
     {
         if constexpr (DT == WWWS_F32) return __uint_as_float(w);
         else return fmaxf(Act<DT == WWWS_BF16>::lo(w), Act<DT == WWWS_BF16>::hi(w));
     }
+    static __device__ __forceinline__ float largest(const uint4& v) { return largest(larger(larger(v.x, v.y), larger(v.z, v.w))); }
 };
 
-// The best of the request's parts, by a whole block.
-__device__ void join(const BeamArgs& a, uint32_t seq, unsigned char* shared)
-{
-    double* score_of = reinterpret_cast<double*>(shared);                                        // [kMost]
-    unsigned long long* id_of = reinterpret_cast<unsigned long long*>(shared + 8 * kMost);       // [kMost] beam, token
-    __shared__ double lse[kMaxBeams], tops[kThreads];
-    __shared__ uint32_t n_found;
-    __shared__ double bound_s;
-    const uint32_t tid = threadIdx.x, lists = a.beams * a.slices, n = lists * a.keep;
-    const float2* stat = a.stat + uint64_t(seq) * lists;
-    const unsigned long long* keys = a.keys + uint64_t(seq) * n;
-    for (uint32_t b = tid; b < a.beams; b += kThreads) {
-        float c = -INFINITY;
-        for (uint32_t s = 0; s < a.slices; ++s) c = fmaxf(c, __ldcg(&stat[b * a.slices + s].x));
-        double sum = 0.0;
-        for (uint32_t s = 0; s < a.slices; ++s) {
-            const float2 p = __ldcg(&stat[b * a.slices + s]);
-            if (!(p.y == 0.0f)) sum += double(p.y) * exp2((double(p.x) - double(c)) * double(kLog2e));              // (a NaN goes on into the sum)
-        }
-        lse[b] = double(c) + log2(sum) / double(kLog2e);                                         // a row without a sum: NaN, and none of its scores counts
-    }
-    if (tid == 0) n_found = 0;
-    __syncthreads();
-    auto score = [&](uint32_t i, unsigned long long& id) {
-        const unsigned long long key = __ldcg(keys + i);
-        const uint32_t b = i % lists / a.slices;
-        id = (unsigned long long)b << 32 | uint32_t(~key);
-        const double y = double(__ldg(a.total + uint64_t(seq) * a.beams + b)) + (double(unordered(uint32_t(key >> 32))) - lse[b]);
-        return key == 0 || !(y > -INFINITY) ? -INFINITY : y;
-    };
-    double top = -INFINITY;
-    unsigned long long id;
-    for (uint32_t i = tid; i < n; i += kThreads) { const double y = score(i, id); top = y > top ? y : top; }
-    tops[tid] = top;
-    __syncthreads();
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < kThreads; ++j) rank += tops[j] > top || (tops[j] == top && j < tid);
-    if (rank == a.keep - 1) bound_s = top;
-    __syncthreads();
-    const double bound = bound_s;
-    if (top >= bound)
-        for (uint32_t i = tid; i < n; i += kThreads) {
-            const double y = score(i, id);
-            if (y >= bound && y > -INFINITY) {
-                const uint32_t at = atomicAdd(&n_found, 1u);
-                if (at < kMost) { score_of[at] = y; id_of[at] = id; }
-            }
-        }
-    __syncthreads();
-    uint32_t found = n_found;
-    auto put = [&](uint32_t r, double y, unsigned long long w) {
-        const uint64_t to = uint64_t(seq) * a.keep + r;
-        a.score[to] = float(y); a.parent[to] = int32_t(seq * a.beams + uint32_t(w >> 32)); a.token[to] = int32_t(uint32_t(w));
-    };
-    if (found > kMost) {                 // the best one, `keep` times over
-        double last = INFINITY; unsigned long long last_id = 0; bool any = true, begun = false;
-        for (uint32_t r = 0; r < a.keep; ++r) {
-            double best = -INFINITY; unsigned long long best_id = ~0ull;
-            if (any)
-                for (uint32_t i = tid; i < n; i += kThreads) {
-                    const double y = score(i, id);
-                    if (begun && !(y < last || (y == last && id > last_id))) continue;
-                    if (y > best || (y == best && id < best_id)) { best = y; best_id = id; }
+// The pieces of a chunk that this lane holds, as they lie in memory: 16 bytes at a 16-byte boundary, -infinity in the place of what is not the row's.
+// In a skewed row piece u begins `skew` bytes before the lane's tokens, which end in the next lane's piece (lane 31: in the first lane's next one).
+template <int DT, bool kSkewed> struct Pieces {
+    using E = Elem<DT>;
+    uint4 raw[kVecs], behind;                    // behind: of lane 0, what follows the chunk
+
+    static __device__ __forceinline__ uint4 piece(const uint8_t* row, int64_t at, uint32_t vocab)      // `at`: token at which the 16 bytes begin
+    {
+        if (at >= 0 && at + E::kPer <= int64_t(vocab)) return __ldg(reinterpret_cast<const uint4*>(row + at * E::kSize));
+        uint32_t w[4] = { E::kNone, E::kNone, E::kNone, E::kNone };
+#pragma unroll
+        for (int e = 0; e < E::kPer; ++e)
+            if (at + e >= 0 && at + e < int64_t(vocab)) {
+                if constexpr (DT == WWWS_F32) w[e] = __ldg(reinterpret_cast<const uint32_t*>(row) + at + e);
+                else {
+                    const uint32_t h = __ldg(reinterpret_cast<const uint16_t*>(row) + at + e);
+                    w[e / 2] = e % 2 ? (w[e / 2] & 0xffffu) | h << 16 : (w[e / 2] & 0xffff0000u) | h;
                 }
-            __syncthreads();
-            score_of[tid] = best; id_of[tid] = best_id;
-            __syncthreads();
-            for (uint32_t k = kThreads / 2; k; k >>= 1) {
-                if (tid < k && (score_of[tid + k] > score_of[tid] || (score_of[tid + k] == score_of[tid] && id_of[tid + k] < id_of[tid]))) { score_of[tid] = score_of[tid + k]; id_of[tid] = id_of[tid + k]; }
-                __syncthreads();
             }
-            last = score_of[0]; last_id = id_of[0]; begun = true;
-            any = last > -INFINITY;
-            if (any && tid == 0) put(r, last, last_id);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void load(const uint8_t* row, uint32_t skew, uint32_t c, uint32_t lane, uint32_t vocab)
+    {
+        const int64_t first = int64_t(c) * E::kChunk - (kSkewed ? int(skew / E::kSize) : 0), at = first + lane * E::kPer;
+        if (first >= 0 && first + E::kChunk + (kSkewed ? E::kPer : 0) <= int64_t(vocab)) {           // (the same for the whole warp)
+            const uint4* from = reinterpret_cast<const uint4*>(row + at * E::kSize);
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) raw[u] = __ldg(from + u * 32);
+            if constexpr (kSkewed) if (lane == 0) behind = __ldg(from + kVecs * 32);
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < kVecs + (kSkewed && lane == 0); ++u) {
+                const uint4 v = piece(row, at + u * 32 * E::kPer, vocab);
+#pragma unroll
+                for (int k = 0; k < kVecs; ++k) if (u == k) raw[k] = v;
+                if (u == kVecs) behind = v;
+            }
         }
-        return;                          // (more than kMost >= keep of them are above -infinity)
     }
-    for (uint32_t i = tid; i < found; i += kThreads) {
-        const double y = score_of[i]; const unsigned long long w = id_of[i];
-        uint32_t r = 0;
-        for (uint32_t j = 0; j < found; ++j) r += score_of[j] > y || (score_of[j] == y && id_of[j] < w);
-        if (r < a.keep) put(r, y, w);
+    __device__ __forceinline__ void take(uint4 (&x)[kVecs], uint32_t skew, uint32_t lane) const
+    {
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) x[u] = raw[u];
+        if constexpr (kSkewed) {
+            if (skew == 0) return;
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) x[u] = shifted(raw[u], lane == 0 ? (u + 1 < kVecs ? raw[u + 1 < kVecs ? u + 1 : 0] : behind) : raw[u], skew, lane);
+        }
     }
-    for (uint32_t r = found + tid; r < a.keep; r += kThreads) {
-        const uint64_t to = uint64_t(seq) * a.keep + r;
-        a.score[to] = -INFINITY; a.parent[to] = -1; a.token[to] = -1;
+    // the lane's tokens from its 16 bytes and the next lane's, who gives `give`
+    static __device__ __forceinline__ uint4 shifted(const uint4& raw, const uint4& give, uint32_t skew, uint32_t lane)
+    {
+        uint32_t w0 = raw.x, w1 = raw.y, w2 = raw.z, w3 = raw.w;
+        uint32_t w4 = __shfl_sync(0xffffffffu, give.x, (lane + 1) & 31), w5 = __shfl_sync(0xffffffffu, give.y, (lane + 1) & 31), w6 = __shfl_sync(0xffffffffu, give.z, (lane + 1) & 31);
+        const uint32_t w7 = __shfl_sync(0xffffffffu, give.w, (lane + 1) & 31), by = (skew & 2) * 8;
+        if (skew == 0) return raw;
+        if (skew & 8) { w0 = w2; w1 = w3; w2 = w4; w3 = w5; w4 = w6; w5 = w7; }
+        if (skew & 4) { w0 = w1; w1 = w2; w2 = w3; w3 = w4; w4 = w5; }
+        return make_uint4(__funnelshift_r(w0, w1, by), __funnelshift_r(w1, w2, by), __funnelshift_r(w2, w3, by), __funnelshift_r(w3, w4, by));
+    }
+};
+
+template <int DT, bool kSkewed> struct Row {
+    const uint8_t* base; uint32_t skew;
+    __device__ __forceinline__ Row(const BeamArgs& a, uint32_t row)
+    {
+        base = a.in + uint64_t(row) * a.stride * Elem<DT>::kSize;
+        skew = kSkewed ? uint32_t(reinterpret_cast<uintptr_t>(base) & 15) : 0;
+    }
+    __device__ __forceinline__ void chunk(uint4 (&x)[kVecs], uint32_t c, uint32_t lane, uint32_t vocab) const
+    {
+        Pieces<DT, kSkewed> p;
+        p.load(base, skew, c, lane, vocab);
+        p.take(x, skew, lane);
+    }
+};
+
+// 64-bit floats in the order of whole numbers; 0 stands below all of them.  (Scores are worked out in 64-bit floats and compared as whole numbers: the joining of a
+// request of 4 beams took 20 us with comparisons on the 64-bit unit.)
+__device__ __forceinline__ unsigned long long ordered(double y) { const long long b = __double_as_longlong(y); return b < 0 ? ~b : b | (1ll << 63); }
+__device__ __forceinline__ double unordered(unsigned long long k) { return __longlong_as_double(k >> 63 ? k & ~(1ull << 63) : ~k); }
+__device__ __forceinline__ float to_float(unsigned long long k) { return k ? float(unordered(k)) : -INFINITY; }           // (rounding keeps the order)
+
+// (ordered score, id) in the order of the result: the larger score, then the lower id (beam, then token or chunk).
+struct Best { unsigned long long y, id; };
+__device__ __forceinline__ bool before(unsigned long long y, unsigned long long id, unsigned long long z, unsigned long long jd) { return y > z || (y == z && id < jd); }
+
+struct Joint {                                                                                   // shared memory of a block that joins a request
+    Best found[kMost];
+    Best chunk[kMaxKeep];                                                                        // the best chunks
+    double lse[kMaxBeams];
+    float off[kMaxBeams];                                                                        // total - lse, about
+    float tops[kThreads];
+    float held[kHeld];
+    uint32_t piece[kMaxKeep * kVecs];                                                            // (best chunk, piece of it)
+    float x_least[kMaxKeep];
+    float bound;
+    uint32_t n, n_pieces;
+};
+
+// What is largest of the block's (y, id), for all threads.
+__device__ Best block_best(Joint& s, unsigned long long y, unsigned long long id)
+{
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+        const unsigned long long z = __shfl_xor_sync(0xffffffffu, y, k), jd = __shfl_xor_sync(0xffffffffu, id, k);
+        if (before(z, jd, y, id)) { y = z; id = jd; }
+    }
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) s.found[threadIdx.x / 32] = Best{ y, id };
+    __syncthreads();
+    Best b = s.found[0];
+    for (int w = 1; w < kWarps; ++w) if (const Best o = s.found[w]; before(o.y, o.id, b.y, b.id)) b = o;
+    return b;
+}
+
+// The score of a logit of beam b, ordered; 0: none.
+__device__ __forceinline__ unsigned long long score_of(const BeamArgs& a, const Joint& s, uint32_t seq, uint32_t b, float x)
+{
+    const double y = double(__ldg(a.total + uint64_t(seq) * a.beams + b)) + (double(x) - s.lse[b]);
+    return x > -INFINITY && y > double(-INFINITY) ? ordered(y) : 0;
+}
+__device__ __forceinline__ void put(const BeamArgs& a, uint32_t seq, uint32_t r, unsigned long long y, unsigned long long id)
+{
+    const uint64_t to = uint64_t(seq) * a.keep + r;
+    a.score[to] = to_float(y);
+    a.parent[to] = y ? int32_t(seq * a.beams + uint32_t(id >> 32)) : -1; a.token[to] = y ? int32_t(uint32_t(id)) : -1;
+}
+
+template <int DT, bool kSkewed> __device__ __noinline__ void join_slowly(const BeamArgs& a, uint32_t seq, Joint& s)
+{
+    using E = Elem<DT>;
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, n = a.beams * a.chunks;
+    auto score = [&](uint32_t b, float x) { return score_of(a, s, seq, b, x); };
+    // Too many at a bound: the best element of every chunk, then the best of these `keep` times over, its chunk looked through again for what comes behind it.
+    unsigned long long* heads = a.heads + uint64_t(seq) * n;
+    auto head = [&](uint32_t i, unsigned long long last) {       // the largest key of chunk i below `last`, by a warp
+        const uint32_t b = i / a.chunks, c = i - b * a.chunks;
+        uint4 x[kVecs];
+        Row<DT, kSkewed>(a, seq * a.beams + b).chunk(x, c, lane, a.vocab);
+        unsigned long long best = 0;
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+            for (int e = 0; e < E::kPer; ++e) {
+                const float v = E::at(x[u], e);
+                const unsigned long long k = v > -INFINITY ? key_of(v, c * E::kChunk + (u * 32 + lane) * E::kPer + e) : 0;
+                if (k < last && k > best) best = k;
+            }
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) { const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, k); best = o > best ? o : best; }
+        if (lane == 0) heads[i] = best;
+    };
+    for (uint32_t i = warp; i < n; i += kWarps) head(i, ~0ull);
+    for (uint32_t r = 0; r < a.keep; ++r) {
+        __syncthreads();                                                                         // (orders the block's writes to the heads too)
+        unsigned long long best = 0, id = ~0ull;
+        for (uint32_t i = tid; i < n; i += kThreads) {
+            const unsigned long long k = __ldcg(heads + i);
+            const uint32_t b = i / a.chunks;
+            const unsigned long long z = k ? score(b, unordered(uint32_t(k >> 32))) : 0, jd = (unsigned long long)b << 32 | uint32_t(~k);
+            if (z && before(z, jd, best, id)) { best = z; id = jd; }
+        }
+        const Best w = block_best(s, best, id);
+        if (tid == 0) put(a, seq, r, w.y, w.id);
+        if (w.y && warp == 0) {
+            const uint32_t b = uint32_t(w.id >> 32), token = uint32_t(w.id), i = b * a.chunks + token / E::kChunk;
+            const unsigned long long k = __ldcg(heads + i);
+            __syncwarp();
+            head(i, k);
+        }
     }
 }
 
-template <int DT, int kVecs> __global__ void __launch_bounds__(kThreads) k_beams(BeamArgs a)
+template <int DT, bool kSkewed> __device__ void join(const BeamArgs& a, uint32_t seq, Joint& s)
 {
     using E = Elem<DT>;
-    constexpr int P = E::kPer;
-    __shared__ __align__(16) unsigned char shared[16 * kMost];
-    __shared__ float tops[kThreads], parts[kThreads / 32];
-    __shared__ uint32_t n_found, last_flag;
-    __shared__ float bound_s;
-    unsigned long long* found_keys = reinterpret_cast<unsigned long long*>(shared);
-    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-    const uint32_t slice = blockIdx.x, row = blockIdx.y, seq = row / a.beams, list = row % a.beams * a.slices + slice, lists = a.beams * a.slices;
-    unsigned long long* keys = a.keys + uint64_t(seq) * lists * a.keep + list;                   // key r at r * lists: neighbouring lists lie side by side
-    const float total = __ldg(a.total + row);
-    if (tid == 0) n_found = 0;
-    if (fabsf(total) < INFINITY) {
-        const uint8_t* base = a.in + uint64_t(row) * a.stride * E::kSize;
-        // Element e of piece u of this thread is token first + u * kThreads * P + e, wherever the row begins: equal rows have equal sums, to the bit.
-        const uint32_t skew = uint32_t(reinterpret_cast<uintptr_t>(base) & 15);
-        const uint32_t first = (slice * kVecs * kThreads + tid) * P;
-        uint4 x[kVecs];
-        auto edge = [&](uint32_t at) {                         // a piece that the row ends (or, from the middle of 16 bytes, begins) in
-            uint32_t w[4] = { E::kNone, E::kNone, E::kNone, E::kNone };
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, n = a.beams * a.chunks;
+    const float2* stat = a.stat + uint64_t(seq) * a.beams * a.slices;
+    const float4* top = a.top + uint64_t(seq) * n;
+    const float* total = a.total + uint64_t(seq) * a.beams;
+    if (tid == 0) s.n = 0;
+    // the chunks' maxima, kHeld of them in shared memory
+    auto look = [&](uint32_t i) { const float4 v = __ldcg(top + i); return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); };
+#pragma unroll 4
+    for (uint32_t i = tid; i < min(n, kHeld); i += kThreads) s.held[i] = look(i);
+#pragma unroll 1
+    for (uint32_t b = tid / 8; b < (a.beams + 31) / 32 * 32; b += kThreads / 8) {                // 8 lanes per row
+        float m = -INFINITY, sum = 0.0f;
+        if (b < a.beams)
+            for (uint32_t k = tid % 8; k < a.slices; k += 8) {
+                const float2 p = __ldcg(&stat[b * a.slices + k]);
+                const float mn = fmaxf(m, p.x);
+                sum = part_of(sum, m, mn) + part_of(p.y, p.x, mn);
+                m = mn;
+            }
 #pragma unroll
-            for (int e = 0; e < P; ++e)
-                if (at + e < a.vocab) {
-                    if constexpr (DT == WWWS_F32) w[e] = __ldg(reinterpret_cast<const uint32_t*>(base) + at + e);
-                    else {
-                        const uint32_t h = __ldg(reinterpret_cast<const uint16_t*>(base) + at + e);
-                        w[e / 2] = e % 2 ? (w[e / 2] & 0xffffu) | h << 16 : (w[e / 2] & 0xffff0000u) | h;
-                    }
+        for (int k = 1; k < 8; k <<= 1) {
+            const float om = __shfl_xor_sync(0xffffffffu, m, k), os = __shfl_xor_sync(0xffffffffu, sum, k), mn = fmaxf(m, om);
+            sum = part_of(sum, m, mn) + part_of(os, om, mn);
+            m = mn;
+        }
+        // log2 of the sum as its exponent and the logarithm of 0.75 .. 1.5, whose fp32 error is 2^-24
+        const int e = int((__float_as_uint(sum) - 0x3f400000u)) >> 23;
+        const float rest = __uint_as_float(__float_as_uint(sum) - (uint32_t(e) << 23));
+        if (tid % 8 == 0 && b < a.beams) {
+            const double lse = sum > 0.0f && sum < INFINITY ? double(m) + (double(e) + double(log2f(rest))) * (1.0 / double(kLog2e)) : double(NAN);      // NaN: the row counts for nothing
+            s.lse[b] = lse;
+            s.off[b] = float(double(__ldg(total + b)) - lse);
+        }
+    }
+    __syncthreads();
+    auto score = [&](uint32_t b, float x) { return score_of(a, s, seq, b, x); };
+    // f(rank, entry) of what was found: an entry is compared by 4, 2 or 1 threads
+    auto ranked = [&](uint32_t found, auto&& f) {
+        const uint32_t by = found <= kThreads / 4 ? 4 : found <= kThreads / 2 ? 2 : 1;
+#pragma unroll 1
+        for (uint32_t base = 0; base < found; base += kThreads / by) {
+            const uint32_t i = base + tid / by;
+            const Best o = s.found[min(i, found - 1)];
+            uint32_t r = 0;
+#pragma unroll 4
+            for (uint32_t j = tid % by; j < found; j += by) r += before(s.found[j].y, s.found[j].id, o.y, o.id);
+            if (by >= 2) r += __shfl_xor_sync(0xffffffffu, r, 1);
+            if (by >= 4) r += __shfl_xor_sync(0xffffffffu, r, 2);
+            if (i < found && tid % by == 0) f(r, o);
+        }
+    };
+    // Scores in fp32, as bounds on either side: three roundings of numbers no larger than the two terms, so 2^-22 of them is more than they are off.
+    auto about = [&](uint32_t i, float x, float side) {
+        const float off = s.off[i / a.chunks], y = x + off + side * (fabsf(x) + fabsf(off)) * 0x1p-22f;
+        return !(x > -INFINITY && off == off) ? -INFINITY : y == y ? y : side * INFINITY;            // (beyond fp32's range no bound is one on either side)
+    };
+    auto largest = [&](uint32_t i) { return i < kHeld ? s.held[i] : look(i); };
+    // Lower bounds, their maxima in groups of threads (about four times as many as are kept): the keep-th largest bounds the best chunks from below.
+    float least_here = -INFINITY, most_here = -INFINITY;
+#pragma unroll 1
+    for (uint32_t i = tid; i < n; i += kThreads) {
+        const float x = largest(i);
+        least_here = fmaxf(least_here, about(i, x, -1.0f)); most_here = fmaxf(most_here, about(i, x, 1.0f));
+    }
+    const uint32_t size = a.keep <= 32 ? 4 : a.keep <= 64 ? 2 : 1, each = kThreads / size / size;      // threads of a group; values that each of them compares
+    float t = least_here;
+    if (size >= 2) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
+    if (size >= 4) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+    const uint32_t me = tid / size, from = tid % size * each;
+    if (tid % size == 0) s.tops[me] = t;
+    __syncthreads();
+    uint32_t rank = 0;
+#pragma unroll 1
+    for (uint32_t j = from; j < from + each; j += 4) {
+        const float4 o = *reinterpret_cast<const float4*>(s.tops + j);
+        rank += (o.x > t || (o.x == t && j < me)) + (o.y > t || (o.y == t && j + 1 < me)) + (o.z > t || (o.z == t && j + 2 < me)) + (o.w > t || (o.w == t && j + 3 < me));
+    }
+    if (size >= 2) rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    if (size >= 4) rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+    if (rank == a.keep - 1) s.bound = t;
+    __syncthreads();
+    const float bound = s.bound;
+    if (most_here >= bound)
+#pragma unroll 1
+        for (uint32_t i = tid; i < n; i += kThreads) {
+            const float x = largest(i);
+            if (about(i, x, 1.0f) >= bound)
+                if (const unsigned long long z = score(i / a.chunks, x)) {
+                    const uint32_t at = atomicAdd(&s.n, 1u);
+                    if (at < kMost) s.found[at] = Best{ z, i };
                 }
-            return make_uint4(w[0], w[1], w[2], w[3]);
-        };
-        if (skew == 0) {
-#pragma unroll
-            for (int u = 0; u < kVecs; ++u) {
-                const uint32_t at = first + u * kThreads * P;
-                if (at + P <= a.vocab) x[u] = __ldcs(reinterpret_cast<const uint4*>(base + uint64_t(at) * E::kSize));
-                else x[u] = edge(at);
-            }
-        } else {                                               // two neighbouring 16 bytes, the second from L1 as a rule, shifted
-#pragma unroll
-            for (int u = 0; u < kVecs; ++u) {
-                const uint32_t at = first + u * kThreads * P;
-                if (at && at + 2 * P <= a.vocab) {
-                    const uint4* from = reinterpret_cast<const uint4*>(base - skew + uint64_t(at) * E::kSize);
-                    const uint4 lo = __ldg(from), hi = __ldg(from + 1);
-                    uint32_t w0 = lo.x, w1 = lo.y, w2 = lo.z, w3 = lo.w, w4 = hi.x, w5 = hi.y, w6 = hi.z;
-                    if (skew & 8) { w0 = w2; w1 = w3; w2 = w4; w3 = w5; w4 = w6; w5 = hi.w; }
-                    if (skew & 4) { w0 = w1; w1 = w2; w2 = w3; w3 = w4; w4 = w5; }
-                    const uint32_t by = (skew & 2) * 8;
-                    x[u] = make_uint4(__funnelshift_r(w0, w1, by), __funnelshift_r(w1, w2, by), __funnelshift_r(w2, w3, by), __funnelshift_r(w3, w4, by));
-                } else x[u] = edge(at);
-            }
         }
-        uint32_t most = E::kNone;
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) most = E::larger(E::larger(most, E::larger(x[u].x, x[u].y)), E::larger(x[u].z, x[u].w));
-        const float mine = E::largest(most);
-        // maxima of groups of threads, of warps, of the slice
-        float m = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const uint32_t groups = a.keep <= 32 ? kThreads / 4 : kThreads;
-        if (groups == kThreads) tops[tid] = mine; else if (tid % 4 == 0) tops[tid / 4] = m;
-#pragma unroll
-        for (int k = 4; k < 32; k <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-        if (lane == 0) parts[warp] = m;
+    __syncthreads();
+    uint32_t found = s.n;
+    if (found <= kMost) {
+        ranked(found, [&](uint32_t r, const Best& o) { if (r < a.keep) s.chunk[r] = o; });
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, parts[w]);
-        if (tid < groups) {
-            const float t = tops[tid];
-            uint32_t rank = 0;
-            for (uint32_t j = 0; j < groups; j += 4) {
-                const float4 o = *reinterpret_cast<const float4*>(tops + j);
-                rank += (o.x > t || (o.x == t && j < tid)) + (o.y > t || (o.y == t && j + 1 < tid)) + (o.z > t || (o.z == t && j + 2 < tid)) + (o.w > t || (o.w == t && j + 3 < tid));
-            }
-            if (rank == a.keep - 1) bound_s = t;
+        if (tid == 0) s.n = s.n_pieces = 0;
+        const uint32_t n_chunks = min(found, a.keep);
+        const unsigned long long least = n_chunks == a.keep ? s.chunk[a.keep - 1].y : 1;         // as many elements reach it
+        __syncthreads();
+        // the pieces of these chunks that have such elements, and the least logit that may be one (in fp32, with the same allowance)
+        for (uint32_t k = tid; k < n_chunks * kVecs; k += kThreads) {
+            const uint32_t i = uint32_t(s.chunk[k / kVecs].id), b = i / a.chunks;
+            const float off = s.off[b], y = to_float(least) - off, x_least = n_chunks < a.keep ? -INFINITY : y - (fabsf(y) + 2.0f * fabsf(off)) * 0x1p-22f;
+            if (k % kVecs == 0) s.x_least[k / kVecs] = x_least;
+            if (const float x = reinterpret_cast<const float*>(top + i)[k % kVecs]; x > -INFINITY && !(x < x_least)) s.piece[atomicAdd(&s.n_pieces, 1u)] = k;
         }
-        // the slice's part of the sum
-        float s0 = 0.0f, s1 = 0.0f;
-        if (m > -INFINITY) {
-            const uint64_t less = pack2(-m, -m), by = pack2(kLog2e, kLog2e);
-            uint64_t both = pack2(0.0f, 0.0f);
+        __syncthreads();
+        // Pieces are read element by element, a lane's at intervals of 32, two pieces of a warp at a time.
+        const uint32_t pieces = s.n_pieces;
+#pragma unroll 1
+        for (uint32_t p0 = 2 * warp; p0 < pieces; p0 += 2 * kWarps) {
+            float v[2][E::kPer];
+            uint32_t token[2], beam[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t k = s.piece[min(p0 + j, pieces - 1)], i = uint32_t(s.chunk[k / kVecs].id);
+                beam[j] = i / a.chunks;
+                token[j] = (i - beam[j] * a.chunks) * E::kChunk + k % kVecs * 32 * E::kPer + lane;
+                const uint8_t* row = a.in + uint64_t(seq * a.beams + beam[j]) * a.stride * E::kSize;
+#pragma unroll
+                for (int e = 0; e < E::kPer; ++e) v[j][e] = token[j] + e * 32 < a.vocab ? E::element(row, token[j] + e * 32) : -INFINITY;
+            }
+            uint32_t hit = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float x_least = p0 + j < pieces ? s.x_least[s.piece[p0 + j] / kVecs] : INFINITY;
+#pragma unroll
+                for (int e = 0; e < E::kPer; ++e) hit |= uint32_t(!(v[j][e] < x_least)) << (j * E::kPer + e);
+            }
+            if (p0 + 1 >= pieces) hit &= (1u << E::kPer) - 1;
+#pragma unroll 1
+            while (hit) {
+                const int at = __ffs(hit) - 1, j = at / E::kPer, e = at % E::kPer;
+                hit &= hit - 1;
+                float w = v[0][0];
+#pragma unroll
+                for (int q = 1; q < 2 * E::kPer; ++q) if (at == q) w = v[q / E::kPer][q % E::kPer];
+                const uint32_t b = j ? beam[1] : beam[0];
+                if (const unsigned long long z = score(b, w); z >= least) {
+                    const uint32_t to = atomicAdd(&s.n, 1u);
+                    if (to < kMost) s.found[to] = Best{ z, (unsigned long long)b << 32 | ((j ? token[1] : token[0]) + uint32_t(e) * 32) };
+                }
+            }
+        }
+        __syncthreads();
+        found = s.n;
+        if (found <= kMost) {
+            ranked(found, [&](uint32_t r, const Best& o) { if (r < a.keep) put(a, seq, r, o.y, o.id); });
+            for (uint32_t r = found + tid; r < a.keep; r += kThreads) put(a, seq, r, 0, 0);
+            return;
+        }
+    }
+    join_slowly<DT, kSkewed>(a, seq, s);
+}
+
+template <int DT, bool kSkewed> __global__ void __launch_bounds__(kThreads, 4) k_beams(BeamArgs a)
+{
+    using E = Elem<DT>;
+    __shared__ __align__(16) unsigned char shared[sizeof(Joint)];
+    __shared__ float2 parts[kWarps];
+    __shared__ uint32_t last_flag;
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const uint32_t slice = blockIdx.x, row = blockIdx.y, seq = row / a.beams;
+    const float total = __ldg(a.total + row);
+    const uint32_t c0 = slice * a.per_slice + warp, c1 = min(a.chunks, (slice + 1) * a.per_slice);
+    float4* top = a.top + uint64_t(row) * a.chunks;
+    float m = -INFINITY, s = 0.0f;
+    if (fabsf(total) < INFINITY) {
+        const Row<DT, kSkewed> from(a, row);
+        Pieces<DT, kSkewed> next;
+        if (c0 < c1) next.load(from.base, from.skew, c0, lane, a.vocab);
+        uint64_t sum = pack2(0.0f, 0.0f);
+        for (uint32_t c = c0; c < c1; c += kWarps) {
+            uint4 x[kVecs];
+            next.take(x, from.skew, lane);
+            if (c + kWarps < c1) next.load(from.base, from.skew, c + kWarps, lane, a.vocab);
+            float y = -INFINITY;
+            uint32_t best[kVecs];
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) { const float t = fmaxf(-INFINITY, E::largest(x[u])); y = fmaxf(y, t); best[u] = __reduce_max_sync(0xffffffffu, ordered(t)); }
+            if (lane == 0) top[c] = make_float4(unordered(best[0]), unordered(best[1]), unordered(best[2]), unordered(best[3]));
+            if (y > m) {
+                const float less = ex2((m - y) * kLog2e);          // (0 the first time)
+                sum = mul2(sum, pack2(less, less)); m = y;
+            }
+            const float mm = m == -INFINITY ? 0.0f : m;
+            const uint64_t less = pack2(-mm, -mm), by = pack2(kLog2e, kLog2e);
 #pragma unroll
             for (int u = 0; u < kVecs; ++u)
 #pragma unroll
-                for (int e = 0; e < P; e += 2) {
+                for (int e = 0; e < E::kPer; e += 2) {
                     float y0, y1;
                     unpack2(mul2(add2(pack2(E::at(x[u], e), E::at(x[u], e + 1)), less), by), y0, y1);
-                    both = add2(both, pack2(ex2(y0), ex2(y1)));
-                }
-            unpack2(both, s0, s1);
-        } else {                                               // nothing above -infinity, but there may be NaN
-#pragma unroll 1
-            for (int e = 0; e < P; ++e)
-#pragma unroll
-                for (int u = 0; u < kVecs; ++u) if (const float v = E::at(x[u], e); v != v) s0 = v;
-        }
-        float sum = s0 + s1;
-#pragma unroll
-        for (int k = 1; k < 32; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        __syncthreads();                                       // the maxima are read, the bound is written
-        if (lane == 0) parts[warp] = sum;
-        const float bound = bound_s;
-        if (mine >= bound && mine > -INFINITY) {
-#pragma unroll
-            for (int u = 0; u < kVecs; ++u)
-#pragma unroll
-                for (int e = 0; e < P; ++e) {
-                    const float v = E::at(x[u], e);
-                    if (v >= bound && v > -INFINITY) {
-                        const uint32_t at = atomicAdd(&n_found, 1u);
-                        if (at < kMost) found_keys[at] = key_of(v, first + u * kThreads * P + e);
-                    }
+                    sum = add2(sum, pack2(ex2(y0), ex2(y1)));
                 }
         }
-        __syncthreads();
-        if (tid == 0) {
-            float t = 0.0f;
-            for (int w = 0; w < kThreads / 32; ++w) t += parts[w];
-            a.stat[uint64_t(seq) * lists + list] = make_float2(m, t);
-        }
-        const uint32_t found = n_found;
-        if (found <= kMost) {
-            for (uint32_t i = tid; i < found; i += kThreads) {
-                const unsigned long long k = found_keys[i];
-                uint32_t r = 0;
-                for (uint32_t j = 0; j < found; ++j) r += found_keys[j] > k;
-                if (r < a.keep) keys[uint64_t(r) * lists] = k;
-            }
-            for (uint32_t r = found + tid; r < a.keep; r += kThreads) keys[uint64_t(r) * lists] = 0;
-        } else {
-            unsigned long long last = ~0ull;
-            for (uint32_t r = 0; r < a.keep; ++r) {
-                unsigned long long best = 0;
+        float s0, s1;
+        unpack2(sum, s0, s1);
+        s = s0 + s1;
+    } else if (lane == 0)
+        for (uint32_t c = c0; c < c1; c += kWarps) top[c] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    // the slice's maximum and sum
 #pragma unroll
-                for (int u = 0; u < kVecs; ++u)
-#pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        const float v = E::at(x[u], e);
-                        if (v > -INFINITY) {
-                            const unsigned long long k = key_of(v, first + u * kThreads * P + e);
-                            if (k < last && k > best) best = k;
-                        }
-                    }
-                for (int k = 1; k < 32; k <<= 1) { const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, k); best = o > best ? o : best; }
-                __syncthreads();
-                if (lane == 0) found_keys[warp] = best;
-                __syncthreads();
-                for (int w = 0; w < kThreads / 32; ++w) best = found_keys[w] > best ? found_keys[w] : best;
-                last = best;                                   // (more than kMost >= keep elements are above -infinity: there always is one)
-                if (tid == 0) keys[uint64_t(r) * lists] = best;
-            }
-        }
-    } else {
-        if (tid == 0) a.stat[uint64_t(seq) * lists + list] = make_float2(-INFINITY, 0.0f);
-        for (uint32_t r = tid; r < a.keep; r += kThreads) keys[uint64_t(r) * lists] = 0;
+    for (int k = 1; k < 32; k <<= 1) {
+        const float om = __shfl_xor_sync(0xffffffffu, m, k), os = __shfl_xor_sync(0xffffffffu, s, k), mn = fmaxf(m, om);
+        s = part_of(s, m, mn) + part_of(os, om, mn);
+        m = mn;
     }
-    __threadfence();
+    if (lane == 0) parts[warp] = make_float2(m, s);
     __syncthreads();
-    if (tid == 0) last_flag = atomicAdd(&a.ticket[seq], 1u) == lists - 1;
+    if (tid == 0) {
+        for (int w = 1; w < kWarps; ++w) {
+            const float2 o = parts[w];
+            const float mn = fmaxf(m, o.x);
+            s = part_of(s, m, mn) + part_of(o.y, o.x, mn);
+            m = mn;
+        }
+        __stcg(a.stat + uint64_t(row) * a.slices + slice, make_float2(m, s));
+        __threadfence();                                           // (the other threads' maxima too: they came before the barrier)
+        last_flag = atomicAdd(&a.ticket[seq], 1u) == a.beams * a.slices - 1;
+    }
     __syncthreads();
     if (last_flag) {
         __threadfence();
-        join(a, seq, shared);
+        join<DT, kSkewed>(a, seq, *reinterpret_cast<Joint*>(shared));
         if (tid == 0) a.ticket[seq] = 0;
     }
 }
 
-// 16-byte pieces of a thread: 8 (32 KB of a row per block) where that leaves a block for every SM, else 2.
-constexpr int kWide = 8, kNarrow = 2;
-uint32_t slices_for(uint32_t vocab, int dtype, int vecs)
+uint32_t chunks_of(uint32_t vocab, int dtype)
 {
-    const uint64_t per = dtype == WWWS_F32 ? 4 : 8, pieces = (vocab + per - 1) / per;
-    return uint32_t((pieces + uint64_t(vecs) * kThreads - 1) / (uint64_t(vecs) * kThreads));
+    const uint32_t chunk = dtype == WWWS_F32 ? Elem<WWWS_F32>::kChunk : Elem<WWWS_BF16>::kChunk;
+    return (vocab + chunk - 1) / chunk;
 }
-int vecs_for(uint32_t rows, uint32_t vocab, int dtype) { return uint64_t(rows) * slices_for(vocab, dtype, kWide) >= 148 ? kWide : kNarrow; }
+// Chunks of a slice: whole rounds of a block's warps, as many as leave the GPU about four blocks an SM, in one wave.
+uint32_t slice_of(uint32_t rows, uint32_t vocab, int dtype)
+{
+    const uint32_t rounds = (chunks_of(vocab, dtype) + kWarps - 1) / kWarps, slices = rows && rows < 148 * 4 ? 148 * 4 / rows : 1;
+    return (rounds + slices - 1) / slices * kWarps;
+}
 
 }  // namespace
 
-uint64_t beams_scratch(uint32_t rows, uint32_t vocab, int dtype, uint32_t keep)
+uint64_t beams_scratch(uint32_t rows, uint32_t vocab, int dtype)
 {
-    const uint64_t lists = uint64_t(rows) * slices_for(vocab, dtype, vecs_for(rows, vocab, dtype));
-    return lists * 8 * (keep + 1ull);
+    const uint64_t chunks = chunks_of(vocab, dtype), per = slice_of(rows, vocab, dtype);
+    return rows * (8 * ((chunks + per - 1) / per) + (16 + 8) * chunks);
 }
 
 cudaError_t launch_beams(BeamArgs a, uint32_t rows, int dtype, void* scratch, cudaStream_t s)
 {
-    const int vecs = vecs_for(rows, a.vocab, dtype);
-    a.slices = slices_for(a.vocab, dtype, vecs);
-    a.stat = static_cast<float2*>(scratch);
-    a.keys = reinterpret_cast<unsigned long long*>(a.stat + uint64_t(rows) * a.slices);
+    a.chunks = chunks_of(a.vocab, dtype);
+    a.per_slice = slice_of(rows, a.vocab, dtype);
+    a.slices = (a.chunks + a.per_slice - 1) / a.per_slice;
+    a.top = static_cast<float4*>(scratch);
+    a.heads = reinterpret_cast<unsigned long long*>(a.top + uint64_t(rows) * a.chunks);
+    a.stat = reinterpret_cast<float2*>(a.heads + uint64_t(rows) * a.chunks);
+    const bool skewed = (reinterpret_cast<uintptr_t>(a.in) | (rows > 1 ? a.stride * (dtype == WWWS_F32 ? 4 : 2) : 0)) & 15;
     const dim3 grid(a.slices, rows);
     auto go = [&](auto dt) {
-        if (vecs == kWide) k_beams<decltype(dt)::value, kWide><<<grid, kThreads, 0, s>>>(a);
-        else k_beams<decltype(dt)::value, kNarrow><<<grid, kThreads, 0, s>>>(a);
+        if (skewed) k_beams<decltype(dt)::value, true><<<grid, kThreads, 0, s>>>(a);
+        else k_beams<decltype(dt)::value, false><<<grid, kThreads, 0, s>>>(a);
         return cudaGetLastError();
     };
     using std::integral_constant;

@@ -119,6 +119,27 @@ def test_best_ones_beside_one_another():
         check(x.flip(1).contiguous(), torch.tensor([0.0, -0.1], device="cuda"), 1, 100)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("keep", [3, 40])
+@pytest.mark.parametrize("vocab", [33000, 33001])
+def test_many_rows_whose_slices_are_long(dtype, keep, vocab):
+    """Enough rows that a block takes a whole one, tile by tile: rows that rise, fall, are constant, begin with nothing, and some at random."""
+    g = torch.Generator("cuda").manual_seed(vocab + keep)
+    x = torch.randn(600, vocab, generator=g, device="cuda")
+    x[0::8] = torch.linspace(-6.0, 6.0, vocab, device="cuda")
+    x[1::8] = torch.linspace(6.0, -6.0, vocab, device="cuda")
+    x[2::8] = 0.5
+    x[3::8, : vocab - 2000] = -math.inf
+    x[4::8, :20000] = -math.inf
+    x[5::8] = -math.inf
+    x[5::8, vocab - 1] = 0.0
+    x = x.to(dtype)
+    totals = -3.0 * torch.rand(600, generator=g, device="cuda")
+    totals[::13] = -math.inf
+    check(x, totals, 3, keep)
+    check(x, totals, 200, keep)
+
+
 def test_large_and_unreal_logits():
     g = torch.Generator("cuda").manual_seed(4)
     x = torch.randn(6, 20003, generator=g, device="cuda")
