@@ -97,6 +97,7 @@ constexpr uint32_t kFewRows = 32, kFewRowsQuant = 48;     // most rows per kv he
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 
 constexpr uint32_t kTileSeqs = 32;                    // sequences of a launch of the tile kernel, at most (see wwws_attend)
+constexpr uint32_t kTreeSeqs = 256;                   // sequences of a launch of the tree kernel, at most: their running sum has to fit beside the rings
 constexpr uint32_t kTickets = kDecodeSlots > kTileSlots ? kDecodeSlots : kTileSlots;
 
 // Raises a kernel's limit of dynamic shared memory, the first time on each device.
@@ -119,6 +120,7 @@ cudaError_t launch_cache_read(const SeqBatch& b, const Pages& p, const int32_t* 
 cudaError_t launch_attend_rows(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_attend_tile(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_attend_rows_tree(const AttendArgs& a, uint32_t rows, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
+cudaError_t launch_tree(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_shape_logits(const ShapeArgs& a, int dtype, cudaStream_t s);
 cudaError_t launch_rotate(RotateArgs a, bool append, uint32_t head_dim, int dtype, int cache, cudaStream_t s);
 cudaError_t launch_fork(const ForkArgs& a, cudaStream_t s);

@@ -210,8 +210,21 @@ wwws_status attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages
     a.few_rows = b->cfg.cache == WWWS_CACHE_16 ? kFewRows : kFewRowsQuant;
     const uint64_t most = uint64_t(batch->max_q_len) * a.group;
     if (tree) {
-        a.few_rows = ~0u;
-        return launched(b, launch_attend_rows_tree(a, uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend_tree");
+        // All of a call's sequences go to one kernel: to the row kernel where the longest has few rows (the same figures), for f16 over quantised caches, and where the tiles of
+        // the longest sequences that the bounds allow could pass 31 bits.
+        const uint64_t tiles = uint64_t(kTreeSeqs) * ((uint64_t(batch->max_kv_len) + 127) / 128 + 1) * ((most + 63) / 64) * b->cfg.n_kv_heads;
+        if (most <= a.few_rows || (b->cfg.dtype == WWWS_F16 && b->cfg.cache != WWWS_CACHE_16) || tiles >= (1ull << 31)) {
+            a.few_rows = ~0u;
+            return launched(b, launch_attend_rows_tree(a, uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend_tree");
+        }
+        cudaError_t e = cudaSuccess;
+        for (uint32_t first = 0; e == cudaSuccess && first < batch->n_seqs; first += kTreeSeqs) {
+            a.b.q_start = batch->q_start + first; a.b.kv_len = batch->kv_len + first; a.b.page_table = batch->page_table + uint64_t(first) * b->cfg.max_pages;
+            a.b.n_seqs = batch->n_seqs - first < kTreeSeqs ? batch->n_seqs - first : kTreeSeqs;
+            a.b.ends = (first == 0 ? 1u : 0u) | (first + a.b.n_seqs == batch->n_seqs ? 2u : 0u);
+            e = launch_tree(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+        }
+        return launched(b, e, "wwws_attend_tree");
     }
     const bool many = most > a.few_rows;
     const bool few = !many || uint64_t(batch->n_tokens) != uint64_t(batch->n_seqs) * batch->max_q_len;

@@ -1,0 +1,681 @@
+// Attention of a tree of drafted tokens with many rows per kv head over the paged cache: tcgen05 tiles fed by TMA.
+//
+// A row is a (drafted token, query head) pair; the query heads of a kv head lie side by side.  Per tile of 128 keys and 128 rows
+//     S = Q K^T            into tensor memory, fp32
+//     P = 2^(x - m)        x = scale * log2(e) * S, running maximum m and sum per row, a row per thread; P back into tensor memory, 16 bits
+//     O = O + P V          O stays in tensor memory, fp32
+// Bound by HBM: a tile of keys and values of head_dim 128 in 16 bits is 64 KB, 2,850 clocks of an SM's share of HBM, against 1,024 clocks of the tensor cores and as
+// many of the exponential unit per 128 rows.  So what counts is that loads never wait for anything:
+//   - Two pipelines, each with an S, an O and four softmax warps, take the jobs (a tile for 128 rows) in turn: while the tensor cores work for one, the
+//     other's softmax runs.  A unit of more than 128 rows (16-bit caches) gives each pipeline its own 128 rows and every tile; one of fewer
+//     gives them every other tile of the same rows, and their results are joined at the end.
+//   - One warp issues the matrix instructions in the order PV(n), S(n + 2); one issues the copies of pages, into rings of their own for keys and values.
+//   - Work is cut by key tiles: all (unit, tile) pairs laid end to end, an equal share for each of 148 blocks, found from a running sum over the
+//     sequences; cut units are joined by the last of their blocks, in block order.  Every role works out its segments by itself.
+//   - m is allowed to lag behind the true maximum by a factor 2^8, so that O is rescaled in the first few tiles only.
+//   - Quantised caches: codes land in a staging ring, four warps widen them into the operands' layout (exactly: 16-bit floats hold the codes);
+//     scales multiply the scores (keys) and the weights (values) in fp32.
+//   - Pages that no row sees are read from page 0 and their values put to zero before they are used, as is everything else of a tile that no row sees.
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "backend.cuh"
+#include "tcgen.cuh"
+
+namespace wwws {
+namespace {
+
+constexpr int kBM = 128, kBN = 128;
+constexpr float kLow = -3.0e38f;
+constexpr float kLag = 8.0f;
+
+template <bool BF, int CACHE, int D> struct Cfg {
+    static constexpr bool kQuant = CACHE != WWWS_CACHE_16;
+    static constexpr int kSlabs = D / 64;
+    static constexpr int kQTiles = kQuant ? 1 : 2;          // row tiles of a unit, at most (a quantised cache's rings leave no room for two)
+    static constexpr int kTile = kBN * D * 2, kCodes = kBN * D;
+    static constexpr int kQ = kBM * D * 2;
+    static constexpr int kK = kQuant ? 2 : D == 128 ? 3 : 4, kV = kQuant ? 2 : D == 128 ? 2 : 4, kStaging = kQuant ? (D == 128 ? 3 : 6) : 0;
+    static constexpr int kOffK = kQTiles * kQ, kOffV = kOffK + kK * kTile, kOffStaging = kOffV + kV * kTile;
+    // [keys, values][4 tiles][128]: the keys' of three more tiles may come while a tile's scores are weighted (the third's wait for that tile's product)
+    static constexpr int kOffScales = kOffStaging + kStaging * kCodes;
+    static constexpr int kOffBars = kOffScales + (kQuant ? 2 * 4 * kBN * 4 : 0);        // the sequences' running sum lies behind
+    static constexpr int kOffPrefix = kOffBars + 256;
+    static constexpr int kFixed = kOffPrefix + 1024;                        // the rings start at a 1,024-byte boundary
+    static constexpr int kConvert = kQuant ? 4 : 1;                         // warps that widen codes, or look through 16-bit values
+    static constexpr int kWarpConvert = 8, kWarpMma = kWarpConvert + kConvert, kWarpLoad = kWarpMma + 1, kThreads = (kWarpLoad + 1) * 32;
+    static constexpr float kRaise = !BF && !kQuant ? 7.0f : 0.0f;           // weights in f16 carry 2^7, and so do their sums: 2^15 at most
+    static constexpr uint32_t kColS = 0, kColO = 256, kColP = 64, kCols = 512;          // P over the upper half of S
+};
+
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// What a call's sequences and a block's share of them come to.
+struct Plan {
+    const uint32_t* prefix;              // [n_seqs + 1] tiles of all earlier sequences, per kv head
+    uint32_t share, begin, end;
+    int tq, step;                        // tokens of a row tile, of a unit
+};
+struct Seg {
+    int q0, q_len, kv, place0, h, tok0;
+    int t0, t1, tiles;                   // key tiles [t0, t1) of the unit's
+    int lo, n_sink, lo_tile;             // first key that the window leaves to any row; tiles with sinks; first tile behind them
+    uint32_t seq, x0;                    // sequence; position of tile t0
+    bool two;                            // two row tiles
+    __device__ __forceinline__ int key_of(int t) const { return (t < n_sink ? t : lo_tile + t - n_sink) * kBN; }
+    __device__ __forceinline__ int jobs() const { return two ? 2 * (t1 - t0) : t1 - t0; }
+    // whether a tile has keys that some row of the unit may not see
+    __device__ __forceinline__ bool mixed(const AttendArgs& a, int key0) const
+    {
+        return key0 + kBN > place0 || (a.window && key0 < place0 + q_len - int(a.window) && key0 + kBN > int(a.sinks));
+    }
+    // whether any row of the unit may see a key
+    __device__ __forceinline__ bool seen(const AttendArgs& a, int key) const { return key < kv && (!a.window || key >= lo || key < int(a.sinks)); }
+};
+
+__device__ __forceinline__ void span(const AttendArgs& a, int q_len, int kv, int& lo, int& lo_tile, int& n_sink, int& tiles)
+{
+    lo = a.window ? max(0, kv - q_len - int(a.window) + 1) : 0;
+    const int all = (max(kv, 0) + kBN - 1) / kBN;
+    lo_tile = min(lo / kBN, all);
+    n_sink = a.window ? min((min(int(a.sinks), kv) + kBN - 1) / kBN, lo_tile) : 0;
+    tiles = max(1, n_sink + all - lo_tile);                  // one (empty) tile even where nothing is seen: the rows get zeros
+}
+
+// The segment that begins at position x.
+__device__ __forceinline__ Seg segment(const AttendArgs& a, const Plan& p, uint32_t x)
+{
+    Seg s;
+    const uint32_t hkv = a.p.n_kv_heads, per_head = x / hkv;
+    uint32_t i = 0, hi = a.b.n_seqs;
+    while (hi - i > 1) { const uint32_t mid = (i + hi) >> 1; if (p.prefix[mid] <= per_head) i = mid; else hi = mid; }
+    s.seq = i; s.x0 = x;
+    s.q0 = __ldg(a.b.q_start + i); s.q_len = __ldg(a.b.q_start + i + 1) - s.q0; s.kv = __ldg(a.b.kv_len + i); s.place0 = s.kv - s.q_len;
+    span(a, s.q_len, s.kv, s.lo, s.lo_tile, s.n_sink, s.tiles);
+    const uint32_t rel = x - p.prefix[i] * hkv, unit = rel / uint32_t(s.tiles);
+    s.t0 = int(rel - unit * uint32_t(s.tiles));
+    s.t1 = int(min(uint32_t(s.tiles), uint32_t(s.t0) + (p.end - x)));
+    s.h = int(unit % hkv); s.tok0 = int(unit / hkv) * p.step;
+    s.two = p.step > p.tq && s.tok0 + p.tq < s.q_len;
+    return s;
+}
+
+template <bool BF, int CACHE, int D>
+__global__ void __launch_bounds__(Cfg<BF, CACHE, D>::kThreads, 1)
+k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
+{
+    using C = Cfg<BF, CACHE, D>;
+    using A = Act<BF>;
+    constexpr bool kQuant = C::kQuant;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint32_t warp_sum[C::kThreads / 32], words[4];        // words: [0] tensor memory, [1] dead, [2] last to arrive, [3] bit 0: a bad page was met, bit 1: a value that is no number was taken out
+    uint8_t* smem = raw + ((1024 - (smem_at(raw) & 1023)) & 1023);
+    const uint32_t base = smem_at(smem), bars = base + C::kOffBars;
+    volatile uint32_t* dead = words + 1;
+    auto k_full = [&](uint32_t s) { return bars + 8 * s; };
+    auto k_empty = [&](uint32_t s) { return bars + 8 * (C::kK + s); };
+    auto v_full = [&](uint32_t s) { return bars + 8 * (2 * C::kK + s); };
+    auto v_empty = [&](uint32_t s) { return bars + 8 * (2 * C::kK + C::kV + s); };
+    constexpr int kRest = 2 * (C::kK + C::kV);
+    auto st_full = [&](uint32_t s) { return bars + 8 * (kRest + s); };
+    auto st_empty = [&](uint32_t s) { return bars + 8 * (kRest + C::kStaging + s); };
+    auto v_ready = [&](uint32_t s) { return bars + 8 * (kRest + s); };              // 16-bit values, looked through
+    constexpr int kMore = kRest + (kQuant ? 2 * C::kStaging : C::kV);
+    const uint32_t q_full = bars + 8 * kMore, done = q_full + 8, drained = q_full + 16;
+    auto s_full = [&](int w) { return q_full + 24 + 8 * w; };
+    auto p_full = [&](int w) { return q_full + 40 + 8 * w; };
+    const uint32_t meeting = q_full + 56;
+    static_assert(8 * (kMore + 8) <= 256, "barriers fit");
+    uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + C::kOffPrefix);
+
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
+    const uint32_t hkv = a.p.n_kv_heads, G = a.group;
+    Plan plan;
+    plan.prefix = prefix; plan.tq = kBM / int(G); plan.step = C::kQTiles * plan.tq;
+
+    // ---- the block's share ----
+    uint32_t carry = 0;
+    for (uint32_t b0 = 0; b0 < a.b.n_seqs; b0 += C::kThreads) {
+        uint32_t v = 0;
+        if (b0 + tid < a.b.n_seqs) {
+            int q0, q_len, kv, lo, lt, ns, tiles;
+            if (sequence(a.b, b0 + tid, q0, q_len, kv, a.err) && q_len) { span(a, q_len, kv, lo, lt, ns, tiles); v = uint32_t((q_len + plan.step - 1) / plan.step) * uint32_t(tiles); }
+        }
+        uint32_t inc = v;
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, inc, m); if (lane >= m) inc += y; }
+        if (lane == 31) warp_sum[warp] = inc;
+        __syncthreads();
+        uint32_t before = carry;
+        for (int k = 0; k < C::kThreads / 32; ++k) { if (k < warp) before += warp_sum[k]; carry += warp_sum[k]; }
+        if (b0 + tid < a.b.n_seqs) prefix[b0 + tid] = before + inc - v;
+        __syncthreads();
+    }
+    const uint32_t total = carry * hkv;
+    plan.share = max((total + gridDim.x - 1) / gridDim.x, 2u);
+    plan.begin = min(blockIdx.x * plan.share, total); plan.end = min(total, plan.begin + plan.share);
+    if (tid == 0) {
+        words[1] = words[3] = 0;
+        for (int s = 0; s < C::kK; ++s) { bar_init(k_full(s), kQuant ? C::kConvert * 32 : 1); bar_init(k_empty(s), 1); }
+        for (int s = 0; s < C::kV; ++s) { bar_init(v_full(s), kQuant ? C::kConvert * 32 : 1); bar_init(v_empty(s), 1); if (!kQuant) bar_init(v_ready(s), 1); }
+        for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), C::kConvert * 32); }
+        bar_init(q_full, 256); bar_init(done, 1); bar_init(drained, 1); bar_init(meeting, 256);
+        for (int w = 0; w < 2; ++w) { bar_init(s_full(w), 1); bar_init(p_full(w), 128); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    if (warp == 0) tmem_alloc(smem_at(words), C::kCols);
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, words[0], 0);
+#define WAIT(bar, parity) __all_sync(0xffffffffu, bar_wait(bar, parity, dead))
+
+    if (warp == C::kWarpLoad) {
+        // ---- copies: a key and a value tile in turn, a lane per box of a page ----
+        const uint32_t page_tokens = 1u << a.p.page_shift;
+        constexpr int kBoxSlabs = kQuant ? 1 : C::kSlabs;
+        const int n_box = kBN / int(page_tokens) * kBoxSlabs;
+        uint32_t it = 0;                                            // tiles
+        bool ok = true;
+        for (uint32_t x = plan.begin; ok && x < plan.end;) {
+            const Seg g = segment(a, plan, x);
+            x += uint32_t(g.t1 - g.t0);
+            for (int t = g.t0; ok && t < g.t1; ++t, ++it) {
+                const int b = lane / kBoxSlabs, key = g.key_of(t) + b * int(page_tokens);
+                int row = int(uint32_t(g.h) << a.p.page_shift);     // page 0
+                if (lane < n_box && key < g.kv && (!a.window || key + int(page_tokens) > g.lo || key < int(a.sinks))) {
+                    const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
+                    if (page < a.p.n_pages) row = int((page * hkv + uint32_t(g.h)) << a.p.page_shift);
+                    else { report(a.err, bePage); atomicOr(words + 3, 1u); }        // (the others see it by way of the barriers below)
+                }
+                __syncwarp();
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    uint32_t full, dst;
+                    if constexpr (kQuant) {
+                        const uint32_t n = 2 * it + kv, s = n % C::kStaging;
+                        if (n >= C::kStaging && !(ok = WAIT(st_empty(s), (n / C::kStaging - 1) & 1))) break;
+                        full = st_full(s); dst = base + C::kOffStaging + s * C::kCodes + b * int(page_tokens) * D;
+                    } else {
+                        const uint32_t s = it % (kv ? C::kV : C::kK), turn = it / (kv ? C::kV : C::kK);
+                        if (turn && !(ok = WAIT(kv ? v_empty(s) : k_empty(s), (turn - 1) & 1))) break;
+                        full = kv ? v_full(s) : k_full(s);
+                        dst = base + (kv ? C::kOffV : C::kOffK) + s * C::kTile + lane % kBoxSlabs * (kBN * 128) + b * int(page_tokens) * 128;
+                    }
+                    if (lane == 0) bar_expect(full, kQuant ? C::kCodes : C::kTile);
+                    __syncwarp();
+                    if (lane < n_box) tma_2d(dst, kv ? &v_map : &k_map, kQuant ? 0 : lane % kBoxSlabs * 64, row, full);
+                    __syncwarp();
+                }
+            }
+        }
+        // leave no copy in flight behind: where all went well they have landed long ago; otherwise the waits end after 1e8 cycles
+        const long long t0 = clock64();
+        auto landed = [&](uint32_t bar, uint32_t parity) { while (!bar_try(bar, parity) && clock64() - t0 < 100000000ll) {} };
+        if constexpr (kQuant) {
+            for (uint32_t n = 2 * it > C::kStaging ? 2 * it - C::kStaging : 0; n < 2 * it; ++n) landed(st_full(n % C::kStaging), (n / C::kStaging) & 1);
+        } else {
+            for (uint32_t n = it > C::kK ? it - C::kK : 0; n < it; ++n) landed(k_full(n % C::kK), (n / C::kK) & 1);
+            for (uint32_t n = it > C::kV ? it - C::kV : 0; n < it; ++n) landed(v_full(n % C::kV), (n / C::kV) & 1);
+        }
+    } else if (warp == C::kWarpMma) {
+        // ---- matrix instructions ----
+        constexpr uint32_t kDescS = mma_desc(BF, false, kBN), kDescO = mma_desc(BF, true, D);
+        const uint32_t one = elect_one();
+        uint32_t it = 0, seg = 0, jobs_of[2] = { 0, 0 };            // tiles before the segment; segments; jobs of each pipeline (the parity of p_full)
+        bool ok = true;
+        auto commit = [&](uint32_t bar) { tc_commit_one(one, bar); };
+        for (uint32_t x = plan.begin; ok && x < plan.end; ++seg) {
+            const Seg g = segment(a, plan, x);
+            const uint32_t n = uint32_t(g.t1 - g.t0);
+            x += n;
+            const bool two = g.two;
+            const int jobs = g.jobs();
+            // job k: tile k or k / 2 of the segment, row tile 0 or k % 2
+            auto scores = [&](int k) {
+                const int w = k & 1;
+                const uint32_t item = it + uint32_t(two ? k >> 1 : k), s = item % C::kK;
+                if (!two || w == 0) { if (!(ok = WAIT(k_full(s), (item / C::kK) & 1))) return; tc_after(); }
+                const uint64_t qa = smem_desc(base + (two ? w : 0) * C::kQ, 16, 1024), kb = smem_desc(base + C::kOffK + s * C::kTile, 16, 1024);
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e)                    // (descriptors count 16 bytes)
+                    mma_ss(one, tmem + C::kColS + w * 128, qa + (e / 4 * (kBM * 128) + e % 4 * 32) / 16, kb + (e / 4 * (kBN * 128) + e % 4 * 32) / 16, kDescS, e > 0);
+                commit(s_full(w));
+                if (!two || w == 1) commit(k_empty(s));
+            };
+            if (!(ok = WAIT(q_full, seg & 1))) break;
+            tc_after();
+            scores(0);
+            if (ok && jobs > 1) scores(1);
+            for (int k = 0; ok && k < jobs; ++k) {
+                const int w = k & 1;
+                const uint32_t item = it + uint32_t(two ? k >> 1 : k), s = item % C::kV;
+                if (!two || w == 0) { if (!(ok = WAIT(kQuant ? v_full(s) : v_ready(s), (item / C::kV) & 1))) break; }
+                if (!(ok = WAIT(p_full(w), jobs_of[w] & 1))) break;
+                ++jobs_of[w];
+                tc_after();
+                const uint64_t vb = smem_desc(base + C::kOffV + s * C::kTile, kBN * 128, 1024);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mma_ts(one, tmem + C::kColO + w * D, tmem + C::kColS + w * 128 + C::kColP + e * 8, vb + e * 2048 / 16, kDescO, k >= 2 || e > 0);
+                if (!two || w == 1) commit(v_empty(s));
+                if (k + 2 < jobs) scores(k + 2);
+            }
+            if (ok) commit(done);
+            it += n;
+        }
+        commit(drained);                                            // nor any matrix instruction, or its arrival at a barrier
+        const long long t0 = clock64();
+        while (!bar_try(drained, 0) && clock64() - t0 < 100000000ll) {}
+    } else if (warp >= C::kWarpConvert) {
+        const int t = tid - C::kWarpConvert * 32;
+        uint32_t it = 0;
+        bool ok = true;
+        for (uint32_t x = plan.begin; ok && x < plan.end;) {
+            const Seg g = segment(a, plan, x);
+            x += uint32_t(g.t1 - g.t0);
+            const int32_t* table = a.b.page_table + uint64_t(g.seq) * a.b.table_stride;
+            auto page_of = [&](int key) { return uint32_t(__ldg(table + (uint32_t(key) >> a.p.page_shift))); };
+            for (int tile = g.t0; ok && tile < g.t1; ++tile, ++it) {
+                const int key0 = g.key_of(tile);
+                if constexpr (kQuant) {
+                    // ---- codes of a staged tile to the operand layout, scales beside them: a key per thread ----
+                    static_assert(C::kConvert * 32 == kBN, "a thread per key");
+                    constexpr int kChunks = D / 16;                 // 16 codes each
+                    const int key = key0 + t;
+                    const uint32_t page = g.seen(a, key) ? page_of(key) : ~0u;
+                    const bool on = page < a.p.n_pages;
+                    float scale[2] = { 0.0f, 0.0f };
+                    if (on) {
+                        const uint64_t cell = ((uint64_t(page) * hkv + uint32_t(g.h)) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1));
+                        scale[0] = __ldg(a.p.k_scale + cell) * a.scale_log2; scale[1] = __ldg(a.p.v_scale + cell);
+                    }
+                    const bool all = __all_sync(0xffffffffu, on);   // (the rows of a warp are its threads' keys)
+                    const uint32_t rows_on = __ballot_sync(0xffffffffu, on);
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const uint32_t n = 2 * it + kv, ss = n % C::kStaging, s = it % (kv ? C::kV : C::kK), turn = it / (kv ? C::kV : C::kK);
+                        if (!(ok = WAIT(st_full(ss), (n / C::kStaging) & 1))) break;
+                        if (turn && !(ok = WAIT(kv ? v_empty(s) : k_empty(s), (turn - 1) & 1))) break;
+                        const uint8_t* from = smem + C::kOffStaging + ss * C::kCodes;
+                        uint8_t* to = smem + (kv ? C::kOffV : C::kOffK) + s * C::kTile;
+                        // a warp takes its 32 rows, neighbouring lanes neighbouring pieces of a row
+#pragma unroll 4
+                        for (int e = 0; e < kChunks; ++e) {
+                            const int at = e * 32 + lane, c = at % kChunks, r = t / 32 * 32 + at / kChunks;
+                            uint4 v = *reinterpret_cast<const uint4*>(from + r * D + c * 16);
+                            if (!all && !(rows_on >> (r & 31) & 1)) v = make_uint4(0, 0, 0, 0);
+                            const uint4 lo = make_uint4(widen<BF, CACHE>(v.x & 0xffffu), widen<BF, CACHE>(v.x >> 16), widen<BF, CACHE>(v.y & 0xffffu), widen<BF, CACHE>(v.y >> 16));
+                            const uint4 hi = make_uint4(widen<BF, CACHE>(v.z & 0xffffu), widen<BF, CACHE>(v.z >> 16), widen<BF, CACHE>(v.w & 0xffffu), widen<BF, CACHE>(v.w >> 16));
+                            uint8_t* row = to + c / 4 * (kBN * 128) + r * 128;
+                            const int p0 = ((2 * (c % 4)) ^ (r & 7)) * 16, p1 = ((2 * (c % 4) + 1) ^ (r & 7)) * 16;
+                            if (c < 4) { *reinterpret_cast<uint4*>(row + p0) = lo; *reinterpret_cast<uint4*>(row + p1) = hi; }
+                            else { *reinterpret_cast<uint4*>(row + p1) = hi; *reinterpret_cast<uint4*>(row + p0) = lo; }     // the other order: no bank twice
+                        }
+                        reinterpret_cast<float*>(smem + C::kOffScales)[(kv * 4 + it % 4) * kBN + t] = scale[kv];
+                        fence_async_proxy();
+                        bar_arrive(kv ? v_full(s) : k_full(s));
+                        bar_arrive(st_empty(ss));
+                    }
+                } else {
+                    // ---- 16-bit values: those that no row of the unit sees become zeros (a weight of 0 does not silence a NaN), and so do, where some rows see them
+                    // and others do not, those that are no numbers: they are added to the rows that see them at the segment's end ----
+                    const uint32_t s = it % C::kV;
+                    if (!(ok = WAIT(v_full(s), (it / C::kV) & 1))) break;
+                    const bool bad = *static_cast<volatile uint32_t*>(words + 3) & 1;
+                    if (bad || g.mixed(a, key0)) {
+#pragma unroll 1
+                        for (int r = t; r < kBN; r += 32) {
+                            const int key = key0 + r;
+                            const bool seen = g.seen(a, key) && (!bad || page_of(key) < a.p.n_pages);
+                            uint8_t* row = smem + C::kOffV + s * C::kTile + r * 128;
+                            auto piece = [&](int e) { return reinterpret_cast<uint4*>(row + e / 8 * (kBN * 128) + ((e ^ r) & 7) * 16); };     // (neighbours meet no bank twice)
+                            uint32_t top = 0;
+                            if (seen) {
+#pragma unroll
+                                for (int e = 0; e < 8 * C::kSlabs; ++e) largest_halves(top, *piece(e));
+                            }
+                            if (!seen || unreal2<BF>(top)) {
+#pragma unroll 1
+                                for (int e = 0; e < 8 * C::kSlabs; ++e) {
+                                    const uint4 v = *piece(e);
+                                    *piece(e) = seen ? make_uint4(real2<BF>(v.x), real2<BF>(v.y), real2<BF>(v.z), real2<BF>(v.w)) : make_uint4(0, 0, 0, 0);
+                                }
+                                if (seen) atomicOr(words + 3, 2u);
+                            }
+                        }
+                        fence_async_proxy();
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(v_ready(s));
+                }
+            }
+        }
+    } else {
+        // ---- softmax: pipeline w, a row per thread ----
+        const int w = warp / 4, r = tid % 128;
+        const uint32_t lanes = uint32_t(warp % 4 * 32) << 16;
+        const uint32_t tS = tmem + C::kColS + w * 128 + lanes, tP = tS + C::kColP, tO = tmem + C::kColO + w * D + lanes;
+        float2* ml_of = reinterpret_cast<float2*>(smem);            // [2][128], over the queries of a segment that is done with them
+        const float f = kQuant ? 1.0f : a.scale_log2;
+        const uint32_t kHidden = f < 0.0f ? 0x7f800000u : 0xff800000u;              // x f = -infinity
+        uint32_t it = 0, seg = 0, n_done = 0, meetings = 0;         // tiles before the segment, segments, jobs of this pipeline, meetings
+        bool ok = true;
+        auto meet = [&] { bar_arrive(meeting); ok = WAIT(meeting, meetings & 1); ++meetings; return ok; };      // of both pipelines (bounded, as every wait here)
+        for (uint32_t x = plan.begin; ok && x < plan.end; ++seg) {
+            const Seg g = segment(a, plan, x);
+            const int n = g.t1 - g.t0;
+            x += uint32_t(n);
+            const int rt = g.two ? w : 0;                           // row tile of this pipeline
+            const int tok = g.tok0 + rt * plan.tq + r / int(G);
+            const bool row_on = r < plan.tq * int(G) && tok < g.q_len;
+            const bool any_on = __any_sync(0xffffffffu, row_on);
+            const int tree_row = g.q0 + min(tok, g.q_len - 1);
+            // queries of row tile rt (the pipelines share one: the first brings it), put to zero where there is no row
+            if (g.two || w == 0) {
+                const uint4* from = reinterpret_cast<const uint4*>(a.q + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.q_stride + (uint64_t(g.h) * G + r % int(G)) * D) * 2);
+                uint8_t* row = smem + rt * C::kQ + r * 128;
+#pragma unroll
+                for (int e = 0; e < D / 8; ++e) *reinterpret_cast<uint4*>(row + e / 8 * (kBM * 128) + ((e ^ r) & 7) * 16) = row_on ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
+                fence_async_proxy();
+            }
+            bar_arrive(q_full);
+            const int depth_place = a.window && row_on ? g.place0 + tree_depth(a.tree, a.tree_words, tree_row, tok) : 0;      // where the window counts from
+            const int32_t* table = a.b.page_table + uint64_t(g.seq) * a.b.table_stride;
+            float m = kLow, l = 0.0f;
+            const int jobs = g.jobs();
+            for (int k = w; k < jobs; k += 2) {
+                const int tile = g.two ? k >> 1 : k, key0 = g.key_of(g.t0 + tile);
+                const uint32_t item = it + uint32_t(tile);
+                if (!(ok = WAIT(s_full(w), n_done & 1))) break;
+                tc_after();
+                if (any_on) {
+                    // which columns [c0, c0 + 32) the row sees, a bit each
+                    const bool bad = *static_cast<volatile uint32_t*>(words + 3) & 1, masked = bad || g.mixed(a, key0);
+                    auto visible = [&](int c0) {
+                        const int first = key0 + c0, rel = first - g.place0;
+                        const int end = min(max(tok - rel + 1, 0), 32);            // columns before `end` are not ahead of the row
+                        uint32_t bits = (end == 32 ? ~0u : (1u << end) - 1) & tree_bits(a.tree, a.tree_words, tree_row, rel);
+                        if (a.window) {
+                            const int from = min(max(depth_place - first + 1 - int(a.window), 0), min(max(-rel, 0), 32));      // context before `from` has left the window, unless it is a sink
+                            const int sunk = min(max(int(a.sinks) - first, 0), 32);
+                            bits &= (from == 32 ? 0u : ~0u << from) | (sunk == 32 ? ~0u : (1u << sunk) - 1);
+                        }
+                        if (bad)
+#pragma unroll 1
+                            for (int e = 0; e < 2; ++e)
+                                if (const int key = first + 16 * e; key >= 0 && key < g.kv && bits >> (16 * e) & 0xffffu && uint32_t(__ldg(table + (uint32_t(key) >> a.p.page_shift))) >= a.p.n_pages) bits &= ~(0xffffu << (16 * e));
+                        return row_on ? bits : 0u;
+                    };
+                    const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + item % 4 * kBN;
+                    const float* vs = ks + 4 * kBN;
+                    if constexpr (kQuant) { if (!(ok = WAIT(v_full(item % C::kV), (item / C::kV) & 1))) break; }       // both scales are there (the next turn of this stage waits for the product)
+                    // 32 columns: times the keys' scales (which hold the softmax scale) where the cache has them, hidden ones put away
+                    auto fetch = [&](uint32_t* v, int c0) {
+                        if constexpr (kQuant) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(ks + c0 + e);
+                                float y0, y1, y2, y3;
+                                unpack2(mul2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), k4.x), y0, y1);
+                                unpack2(mul2(pack2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), k4.y), y2, y3);
+                                v[e] = __float_as_uint(y0); v[e + 1] = __float_as_uint(y1); v[e + 2] = __float_as_uint(y2); v[e + 3] = __float_as_uint(y3);
+                            }
+                        }
+                        if (masked) {                               // (the same for the whole warp)
+                            const uint32_t bits = visible(c0);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = bits & (1u << e) ? v[e] : kHidden;
+                        }
+                    };
+                    uint32_t v0[32], v1[32], v2[32];
+                    float top = f < 0.0f ? INFINITY : -INFINITY;
+                    auto widest = [&](const uint32_t* v) {
+                        if (f >= 0.0f) {
+                            float t0 = top, t1 = -INFINITY;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) { t0 = fmaxf(t0, __uint_as_float(v[e])); t1 = fmaxf(t1, __uint_as_float(v[e + 1])); }
+                            top = fmaxf(t0, t1);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) top = fminf(top, __uint_as_float(v[e]));
+                        }
+                    };
+                    __syncwarp();
+                    tm_ld32(tS, v0); tm_ld32(tS + 32, v1);
+                    tm_wait_ld32(v0); tie32(v1);
+                    fetch(v0, 0); widest(v0);
+                    fetch(v1, 32); widest(v1);
+                    __syncwarp();
+                    tm_ld32(tS + 64, v1); tm_ld32(tS + 96, v2);
+                    tm_wait_ld32(v1); tie32(v2);
+                    fetch(v1, 64); widest(v1);
+                    fetch(v2, 96); widest(v2);
+                    top *= f;
+                    if (!row_on) top = m;
+                    if (__any_sync(0xffffffffu, top > m + kLag)) {  // O so far shrinks (the products into it are done: the scores came behind them)
+                        const float mn = fmaxf(m, top), less = ex2(m - mn);
+                        if (k >= 2) {
+#pragma unroll 1
+                            for (int c0 = 0; c0 < D; c0 += 16) {
+                                uint32_t o[16];
+                                tm_ld16(tO + c0, o);
+                                tm_wait_ld16(o);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * less);
+                                tm_st16(tO + c0, o);
+                            }
+                        }
+                        l *= less; m = mn;
+                    }
+                    const uint64_t f2 = pack2(f, f), m2 = pack2(C::kRaise - m, C::kRaise - m);
+                    uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
+                    auto weights = [&](const uint32_t* v, int c0) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float y0, y1;
+                            unpack2(fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, m2), y0, y1);
+                            y0 = ex2(y0); y1 = ex2(y1);
+                            const uint64_t y = pack2(y0, y1);
+                            if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
+                            if constexpr (kQuant) {
+                                const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(vs + c0 + e / 4 * 4);
+                                unpack2(mul2(y, e % 4 ? v4.y : v4.x), y0, y1);
+                                if (masked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
+                            }
+                            p[e / 2] = A::pack(y0, y1);
+                        }
+                        tm_st16(tP + c0 / 2, p);
+                    };
+                    weights(v2, 96);
+                    tm_ld32(tS, v0); tm_ld32(tS + 32, v2);          // read again: registers for the other half only
+                    weights(v1, 64);
+                    tm_wait_ld32(v0); tie32(v2);
+                    fetch(v0, 0); weights(v0, 0);
+                    fetch(v2, 32); weights(v2, 32);
+                    float s0, s1;
+                    unpack2(add2(sum_a, sum_b), s0, s1);
+                    l += s0 + s1;
+                    tm_wait_st();
+                }
+                __syncwarp();
+                tc_before();
+                bar_arrive(p_full(w));
+                ++n_done;
+            }
+            if (!ok) break;
+            it += uint32_t(n);
+            if (!(ok = WAIT(done, seg & 1))) break;
+            tc_after();
+            // ---- the segment's result: of this thread's row, or, where the pipelines shared the rows, of half its columns ----
+            const bool joined = !g.two;
+            float other_m = kLow, other_l = 0.0f;
+            if (joined) {
+                ml_of[w * kBM + r] = make_float2(m, l);
+                if (!meet()) break;
+                const float2 o = ml_of[(w ^ 1) * kBM + r];
+                other_m = o.x; other_l = o.y;
+            }
+            const float mm = fmaxf(m, other_m), mine = ex2(m - mm), theirs = ex2(other_m - mm);
+            const float ll = w ? other_l * theirs + l * mine : l * mine + other_l * theirs;
+            const bool use_mine = w == 0 || jobs > 1, use_other = joined && (w == 1 || jobs > 1);       // (a pipeline without a job has no O)
+            const uint32_t tOther = tmem + C::kColO + (w ^ 1) * D + lanes;
+            const int c_from = joined ? w * (D / 2) : 0, c_to = joined ? c_from + D / 2 : D;
+            const bool whole = g.t0 == 0 && g.t1 == g.tiles;
+            const uint32_t slot = 2 * blockIdx.x + (g.x0 == plan.begin ? 0 : 1);
+            uint8_t* dst = a.out + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.out_stride + (uint64_t(g.h) * G + r % int(G)) * D) * 2;
+            const float inv = ll > 0.0f ? 1.0f / ll : ll;           // 0: nothing seen; NaN stays NaN
+            const bool unreal_met = !kQuant && (*static_cast<volatile uint32_t*>(words + 3) & 2);
+#pragma unroll 1
+            for (int c0 = c_from; c0 < c_to; c0 += 32) {
+                uint32_t v[32], o[32];
+                tm_ld32(tO + c0, v); tm_ld32(tOther + c0, o);
+                tm_wait_ld32(v); tie32(o);
+                float y[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float p = use_mine ? __uint_as_float(v[e]) * mine : 0.0f, q = use_other ? __uint_as_float(o[e]) * theirs : 0.0f;
+                    y[e] = w ? q + p : p + q;                       // (the same order whichever half it is)
+                }
+                if constexpr (!kQuant) {
+                    if (unreal_met && row_on) {                     // values that are no numbers, to the rows that see them
+#pragma unroll 1
+                        for (int t = g.t0; t < g.t1; ++t) {
+                            const int key0 = g.key_of(t);
+                            if (!g.mixed(a, key0)) continue;
+#pragma unroll 1
+                            for (int key = key0; key < min(key0 + kBN, g.place0 + tok + 1); ++key) {
+                                if (key < 0) continue;
+                                const bool sees = key >= g.place0 ? (tree_bits(a.tree, a.tree_words, tree_row, key - g.place0) & 1u) != 0 : !a.window || key > depth_place - int(a.window) || key < int(a.sinks);
+                                const uint32_t page = sees ? uint32_t(__ldg(table + (uint32_t(key) >> a.p.page_shift))) : ~0u;
+                                if (page >= a.p.n_pages) continue;
+                                const uint4* from = reinterpret_cast<const uint4*>(a.p.v + (((uint64_t(page) * hkv + uint32_t(g.h)) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1))) * (D * 2) + c0 * 2);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const uint4 q = __ldg(from + e);
+                                    const uint32_t u[4] = { q.x, q.y, q.z, q.w };
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) { const uint32_t half = u[j / 2] >> (j % 2 * 16) & 0xffffu; if (unreal<BF>(half)) y[8 * e + j] += A::lo(half); }
+                                }
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (row_on) {
+                    if (whole) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            *reinterpret_cast<uint4*>(dst + (c0 + e) * 2) = make_uint4(A::pack(y[e] * inv, y[e + 1] * inv), A::pack(y[e + 2] * inv, y[e + 3] * inv),
+                                                                                      A::pack(y[e + 4] * inv, y[e + 5] * inv), A::pack(y[e + 6] * inv, y[e + 7] * inv));
+                    } else {
+                        float4* part = reinterpret_cast<float4*>(a.s.part_o) + ((uint64_t(slot) * 2 + rt) * (D / 4) + c0 / 4) * kBM + r;      // [slot][row tile][D / 4][128] float4
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) part[e * kBM] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+                    }
+                }
+                __syncwarp();
+            }
+            if (!whole && row_on && (g.two || w == 0)) a.s.part_ml[(slot * 2 + rt) * kBM + r] = make_float2(mm, ll);
+            tc_before();
+            if (!whole) {
+                // the unit's blocks are consecutive; the last to arrive joins their parts in that order
+                const uint32_t u0 = g.x0 - uint32_t(g.t0), u1 = u0 + uint32_t(g.tiles);
+                const uint32_t blk0 = u0 / plan.share, blk1 = (u1 - 1) / plan.share, first_slot = 2 * blk0 + (u0 % plan.share ? 1 : 0);
+                __threadfence();
+                if (!meet()) break;
+                if (tid == 0) { __threadfence(); words[2] = atomicAdd(&a.s.ticket[first_slot], 1u) == blk1 - blk0; }
+                __syncwarp();
+                if (!meet()) break;
+                if (words[2]) {
+                    __threadfence();
+                    if (row_on) {
+                        auto slot_of = [&](uint32_t b) { return (b == blk0 ? first_slot : 2 * b) * 2 + rt; };
+                        float tm = kLow, tl = 0.0f;
+                        for (uint32_t b = blk0; b <= blk1; ++b) {
+                            const float2 p = __ldcg(a.s.part_ml + slot_of(b) * kBM + r);
+                            const float mn = fmaxf(tm, p.x);
+                            tl = tl * ex2(tm - mn) + p.y * ex2(p.x - mn); tm = mn;
+                        }
+                        const float part_inv = tl > 0.0f ? 1.0f / tl : tl;
+#pragma unroll 1
+                        for (int c = c_from / 4; c < c_to / 4; c += 8) {
+                            float4 acc[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+                            for (uint32_t b = blk0; b <= blk1; ++b) {
+                                const uint32_t s = slot_of(b);
+                                const float by = ex2(__ldcg(a.s.part_ml + s * kBM + r).x - tm);
+                                const float4* part = reinterpret_cast<const float4*>(a.s.part_o) + (uint64_t(s) * (D / 4) + c) * kBM + r;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) { const float4 v = __ldcg(part + e * kBM); acc[e].x += v.x * by; acc[e].y += v.y * by; acc[e].z += v.z * by; acc[e].w += v.w * by; }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; e += 2)
+                                *reinterpret_cast<uint4*>(dst + (c + e) * 8) = make_uint4(A::pack(acc[e].x * part_inv, acc[e].y * part_inv), A::pack(acc[e].z * part_inv, acc[e].w * part_inv),
+                                                                                          A::pack(acc[e + 1].x * part_inv, acc[e + 1].y * part_inv), A::pack(acc[e + 1].z * part_inv, acc[e + 1].w * part_inv));
+                        }
+                    }
+                    if (tid == 0) a.s.ticket[first_slot] = 0;
+                }
+            }
+            if (joined && !meet()) break;                           // each has read the other's sums and O before the next segment's are written
+        }
+    }
+#undef WAIT
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    if (tid == 0 && words[1]) report(a.err, beTimeout);
+    if (warp == 0) { tc_after(); tmem_free(tmem, C::kCols); }
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder()
+{
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(p) : nullptr;
+    }();
+    return f;
+}
+
+}  // namespace
+
+cudaError_t launch_tree(const AttendArgs& a, uint32_t head_dim, int dtype, int cache, cudaStream_t s)
+{
+    const EncodeTiled encode = encoder();
+    if (!encode) return cudaErrorNotSupported;
+    const bool quant = cache != WWWS_CACHE_16;
+    CUtensorMap maps[2];
+    for (int kv = 0; kv < 2; ++kv) {
+        const cuuint64_t dims[2] = { head_dim, uint64_t(a.p.n_pages) * a.p.n_kv_heads << a.p.page_shift };
+        const cuuint64_t strides[1] = { head_dim * (quant ? 1ull : 2ull) };
+        const cuuint32_t box[2] = { quant ? head_dim : 64, 1u << a.p.page_shift }, ones[2] = { 1, 1 };
+        if (encode(&maps[kv], quant ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : dtype == WWWS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, kv ? a.p.v : a.p.k, dims, strides, box, ones,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, quant ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    auto go = [&](auto bf, auto kind, auto dim) -> cudaError_t {
+        using C = Cfg<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
+        static_assert(C::kFixed + (kTreeSeqs + 1) * 4 <= 232448 - 256, "shared memory of a block");
+        constexpr auto kernel = k_tree<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
+        const uint32_t smem = C::kFixed + (a.b.n_seqs + 1) * 4;
+        if (cudaError_t e = allow_smem<kernel>(C::kFixed + (kTreeSeqs + 1) * 4); e != cudaSuccess) return e;
+        kernel<<<kTileBlocks, C::kThreads, smem, s>>>(a, maps[0], maps[1]);
+        return cudaGetLastError();
+    };
+    using std::integral_constant;
+    auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? go(bf, kind, integral_constant<int, 64>()) : go(bf, kind, integral_constant<int, 128>()); };
+    // (f16 weights over a quantised cache would have to follow the values' scales: those calls go to the row kernel)
+    if (dtype == WWWS_BF16) return cache == WWWS_CACHE_16 ? dim(std::true_type(), integral_constant<int, 0>()) : cache == WWWS_CACHE_INT8 ? dim(std::true_type(), integral_constant<int, 1>()) : dim(std::true_type(), integral_constant<int, 2>());
+    return cache == WWWS_CACHE_16 ? dim(std::false_type(), integral_constant<int, 0>()) : cudaErrorNotSupported;
+}
+
+}  // namespace wwws
