@@ -12,9 +12,10 @@
 //   - One warp issues the matrix instructions in the order PV(n), S(n + 2); one issues the copies of pages, into rings of their own for keys and values.
 //   - Work is cut by key tiles: all (unit, tile) pairs laid end to end, an equal share for each of 148 blocks, found from a running sum over the
 //     sequences; cut units are joined by the last of their blocks, in block order.  Every role works out its segments by itself.
-//   - m is allowed to lag behind the true maximum by a factor 2^8, so that O is rescaled in the first few tiles only.
-//   - Quantised caches: codes land in a staging ring, four warps widen them into the operands' layout (exactly: 16-bit floats hold the codes);
-//     scales multiply the scores (keys) and the weights (values) in fp32.
+//   - m is allowed to lag behind the true maximum by a factor (2^8, 2^1 over quantised caches), so that O is rescaled in the first few tiles only.
+//   - Quantised caches: codes land in a staging ring, four warps widen them into the operands' layout, to f16 whatever the backend (exactly, and for e4m3 by the
+//     hardware: widening to bf16 took three times the instructions and the whole call 168 us instead of @@); scales multiply the scores (keys) and the weights (values) in fp32.
+//     bf16 queries become f16 by a power of two per row (exact down to 2^-28 of the row's largest); weights are kept relative to the largest value scale of the segment so far.
 //   - Pages that no row sees are read from page 0 and their values put to zero before they are used, as is everything else of a tile that no row sees.
 #include <cuda.h>
 
@@ -28,7 +29,6 @@ namespace {
 
 constexpr int kBM = 128, kBN = 128;
 constexpr float kLow = -3.0e38f;
-constexpr float kLag = 8.0f;
 
 template <bool BF, int CACHE, int D> struct Cfg {
     static constexpr bool kQuant = CACHE != WWWS_CACHE_16;
@@ -40,12 +40,16 @@ template <bool BF, int CACHE, int D> struct Cfg {
     static constexpr int kOffK = kQTiles * kQ, kOffV = kOffK + kK * kTile, kOffStaging = kOffV + kV * kTile;
     // [keys, values][4 tiles][128]: the keys' of three more tiles may come while a tile's scores are weighted (the third's wait for that tile's product)
     static constexpr int kOffScales = kOffStaging + kStaging * kCodes;
-    static constexpr int kOffBars = kOffScales + (kQuant ? 2 * 4 * kBN * 4 : 0);        // the sequences' running sum lies behind
+    static constexpr int kOffMl = kOffScales + (kQuant ? 2 * 4 * kBN * 4 : 0);
+    static constexpr int kOffBars = kOffMl + (kQuant ? 2 * kBM * 16 : 0);               // the sequences' running sum lies behind
     static constexpr int kOffPrefix = kOffBars + 256;
     static constexpr int kFixed = kOffPrefix + 1024;                        // the rings start at a 1,024-byte boundary
     static constexpr int kConvert = kQuant ? 4 : 1;                         // warps that widen codes, or look through 16-bit values
     static constexpr int kWarpConvert = 8, kWarpMma = kWarpConvert + kConvert, kWarpLoad = kWarpMma + 1, kThreads = (kWarpLoad + 1) * 32;
-    static constexpr float kRaise = !BF && !kQuant ? 7.0f : 0.0f;           // weights in f16 carry 2^7, and so do their sums: 2^15 at most
+    static constexpr bool kB = BF && !kQuant;                               // the operands' type
+    // How far (log2) m may lag behind, and the factor that weights in f16 and their sums carry: 2^15 at most together.  Over a quantised cache bf16 backends are
+    // held to bf16's range, so the factor is the larger part there: what is lost is 2^-38 of the row's largest weight (2^-31 failed columns of faint weights alone).
+    static constexpr float kLag = kQuant ? 1.0f : 8.0f, kRaise = kQuant ? 14.0f : kB ? 0.0f : 7.0f;
     static constexpr uint32_t kColS = 0, kColO = 256, kColP = 64, kCols = 512;          // P over the upper half of S
 };
 
@@ -101,12 +105,25 @@ __device__ __forceinline__ Seg segment(const AttendArgs& a, const Plan& p, uint3
     return s;
 }
 
+// The power of two that brings the largest of a row of bf16 into [2^14, 2^15); returns its inverse.  (A row of zeros, subnormals or with a NaN or an infinity stays.)
+template <int N> __device__ __forceinline__ float lifted(const uint4 (&q)[N], float& mul)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) largest_halves(top, q[e]);
+    const uint32_t ex = max(top & 0xffffu, top >> 16) >> 7;
+    const uint32_t me = ex == 0 || ex == 255 ? 127 : min(max(127 + 127 + 14 - int(ex), 1), 253);
+    mul = __uint_as_float(me << 23);
+    return __uint_as_float((254 - me) << 23);
+}
+
 template <bool BF, int CACHE, int D>
 __global__ void __launch_bounds__(Cfg<BF, CACHE, D>::kThreads, 1)
 k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
     using C = Cfg<BF, CACHE, D>;
     using A = Act<BF>;
+    using W = Act<C::kB>;
     constexpr bool kQuant = C::kQuant;
     extern __shared__ uint8_t raw[];
     __shared__ uint32_t warp_sum[C::kThreads / 32], words[4];        // words: [0] tensor memory, [1] dead, [2] last to arrive, [3] bit 0: a bad page was met, bit 1: a value that is no number was taken out
@@ -177,52 +194,62 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         const uint32_t page_tokens = 1u << a.p.page_shift;
         constexpr int kBoxSlabs = kQuant ? 1 : C::kSlabs;
         const int n_box = kBN / int(page_tokens) * kBoxSlabs;
-        uint32_t it = 0;                                            // tiles
+        uint32_t it = 0, staged = 0, k_sent = 0, v_sent = 0;        // tiles before the segment; copies so far
         bool ok = true;
         for (uint32_t x = plan.begin; ok && x < plan.end;) {
             const Seg g = segment(a, plan, x);
             x += uint32_t(g.t1 - g.t0);
-            for (int t = g.t0; ok && t < g.t1; ++t, ++it) {
-                const int b = lane / kBoxSlabs, key = g.key_of(t) + b * int(page_tokens);
-                int row = int(uint32_t(g.h) << a.p.page_shift);     // page 0
-                if (lane < n_box && key < g.kv && (!a.window || key + int(page_tokens) > g.lo || key < int(a.sinks))) {
-                    const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
-                    if (page < a.p.n_pages) row = int((page * hkv + uint32_t(g.h)) << a.p.page_shift);
-                    else { report(a.err, bePage); atomicOr(words + 3, 1u); }        // (the others see it by way of the barriers below)
+            // keys of a tile, then the values of the one before: the next scores do not wait for a place among the values
+            int row = 0;
+            for (int t = g.t0; ok && t <= g.t1; ++t) {
+                const int b = lane / kBoxSlabs, values_row = row;
+                if (t < g.t1) {
+                    const int key = g.key_of(t) + b * int(page_tokens);
+                    row = int(uint32_t(g.h) << a.p.page_shift);     // page 0
+                    if (lane < n_box && key < g.kv && (!a.window || key + int(page_tokens) > g.lo || key < int(a.sinks))) {
+                        const uint32_t page = uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift)));
+                        if (page < a.p.n_pages) row = int((page * hkv + uint32_t(g.h)) << a.p.page_shift);
+                        else { report(a.err, bePage); atomicOr(words + 3, 1u); }        // (the others see it by way of the barriers below)
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
+                    if (kv ? t == g.t0 : t == g.t1) continue;
+                    const uint32_t tile = it + uint32_t(t - g.t0) - kv;
                     uint32_t full, dst;
                     if constexpr (kQuant) {
-                        const uint32_t n = 2 * it + kv, s = n % C::kStaging;
-                        if (n >= C::kStaging && !(ok = WAIT(st_empty(s), (n / C::kStaging - 1) & 1))) break;
+                        const uint32_t s = staged % C::kStaging;
+                        if (staged >= C::kStaging && !(ok = WAIT(st_empty(s), (staged / C::kStaging - 1) & 1))) break;
+                        ++staged;
                         full = st_full(s); dst = base + C::kOffStaging + s * C::kCodes + b * int(page_tokens) * D;
                     } else {
-                        const uint32_t s = it % (kv ? C::kV : C::kK), turn = it / (kv ? C::kV : C::kK);
+                        const uint32_t s = tile % (kv ? C::kV : C::kK), turn = tile / (kv ? C::kV : C::kK);
                         if (turn && !(ok = WAIT(kv ? v_empty(s) : k_empty(s), (turn - 1) & 1))) break;
+                        ++(kv ? v_sent : k_sent);
                         full = kv ? v_full(s) : k_full(s);
                         dst = base + (kv ? C::kOffV : C::kOffK) + s * C::kTile + lane % kBoxSlabs * (kBN * 128) + b * int(page_tokens) * 128;
                     }
                     if (lane == 0) bar_expect(full, kQuant ? C::kCodes : C::kTile);
                     __syncwarp();
-                    if (lane < n_box) tma_2d(dst, kv ? &v_map : &k_map, kQuant ? 0 : lane % kBoxSlabs * 64, row, full);
+                    if (lane < n_box) tma_2d(dst, kv ? &v_map : &k_map, kQuant ? 0 : lane % kBoxSlabs * 64, kv ? values_row : row, full);
                     __syncwarp();
                 }
             }
+            it += uint32_t(g.t1 - g.t0);
         }
         // leave no copy in flight behind: where all went well they have landed long ago; otherwise the waits end after 1e8 cycles
         const long long t0 = clock64();
         auto landed = [&](uint32_t bar, uint32_t parity) { while (!bar_try(bar, parity) && clock64() - t0 < 100000000ll) {} };
         if constexpr (kQuant) {
-            for (uint32_t n = 2 * it > C::kStaging ? 2 * it - C::kStaging : 0; n < 2 * it; ++n) landed(st_full(n % C::kStaging), (n / C::kStaging) & 1);
+            for (uint32_t n = staged > C::kStaging ? staged - C::kStaging : 0; n < staged; ++n) landed(st_full(n % C::kStaging), (n / C::kStaging) & 1);
         } else {
-            for (uint32_t n = it > C::kK ? it - C::kK : 0; n < it; ++n) landed(k_full(n % C::kK), (n / C::kK) & 1);
-            for (uint32_t n = it > C::kV ? it - C::kV : 0; n < it; ++n) landed(v_full(n % C::kV), (n / C::kV) & 1);
+            for (uint32_t n = k_sent > C::kK ? k_sent - C::kK : 0; n < k_sent; ++n) landed(k_full(n % C::kK), (n / C::kK) & 1);
+            for (uint32_t n = v_sent > C::kV ? v_sent - C::kV : 0; n < v_sent; ++n) landed(v_full(n % C::kV), (n / C::kV) & 1);
         }
     } else if (warp == C::kWarpMma) {
         // ---- matrix instructions ----
-        constexpr uint32_t kDescS = mma_desc(BF, false, kBN), kDescO = mma_desc(BF, true, D);
+        constexpr uint32_t kDescS = mma_desc(C::kB, false, kBN), kDescO = mma_desc(C::kB, true, D);
         const uint32_t one = elect_one();
         uint32_t it = 0, seg = 0, jobs_of[2] = { 0, 0 };            // tiles before the segment; segments; jobs of each pipeline (the parity of p_full)
         bool ok = true;
@@ -270,55 +297,80 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         while (!bar_try(drained, 0) && clock64() - t0 < 100000000ll) {}
     } else if (warp >= C::kWarpConvert) {
         const int t = tid - C::kWarpConvert * 32;
-        uint32_t it = 0;
-        bool ok = true;
+        uint32_t it = 0, staged = 0, next_page = ~0u;
+        bool ok = true, next_on = false;
+        float next_scale[2] = { 0.0f, 0.0f };
+        // of a quantised cache: this thread's key's page of a tile; its scales, whose page has been looked up
+        auto look_up = [&](const Seg& g, int tile) {
+            const int key = g.key_of(tile) + t;
+            next_page = tile < g.t1 && g.seen(a, key) ? uint32_t(__ldg(a.b.page_table + uint64_t(g.seq) * a.b.table_stride + (uint32_t(key) >> a.p.page_shift))) : ~0u;
+        };
+        auto scales_of = [&](const Seg& g, int tile) {
+            const int key = g.key_of(tile) + t;
+            next_on = next_page < a.p.n_pages;
+            next_scale[0] = next_scale[1] = 0.0f;
+            if (next_on) {
+                const uint64_t cell = ((uint64_t(next_page) * hkv + uint32_t(g.h)) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1));
+                next_scale[0] = __ldg(a.p.k_scale + cell); next_scale[1] = __ldg(a.p.v_scale + cell);
+            }
+        };
         for (uint32_t x = plan.begin; ok && x < plan.end;) {
             const Seg g = segment(a, plan, x);
             x += uint32_t(g.t1 - g.t0);
             const int32_t* table = a.b.page_table + uint64_t(g.seq) * a.b.table_stride;
             auto page_of = [&](int key) { return uint32_t(__ldg(table + (uint32_t(key) >> a.p.page_shift))); };
-            for (int tile = g.t0; ok && tile < g.t1; ++tile, ++it) {
-                const int key0 = g.key_of(tile);
-                if constexpr (kQuant) {
-                    // ---- codes of a staged tile to the operand layout, scales beside them: a key per thread ----
-                    static_assert(C::kConvert * 32 == kBN, "a thread per key");
-                    constexpr int kChunks = D / 16;                 // 16 codes each
-                    const int key = key0 + t;
-                    const uint32_t page = g.seen(a, key) ? page_of(key) : ~0u;
-                    const bool on = page < a.p.n_pages;
-                    float scale[2] = { 0.0f, 0.0f };
-                    if (on) {
-                        const uint64_t cell = ((uint64_t(page) * hkv + uint32_t(g.h)) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1));
-                        scale[0] = __ldg(a.p.k_scale + cell) * a.scale_log2; scale[1] = __ldg(a.p.v_scale + cell);
+            if constexpr (kQuant) {
+                // ---- codes of a staged tile to the operand layout, scales beside them: a key per thread; keys of a tile, then the values of the one before ----
+                static_assert(C::kConvert * 32 == kBN, "a thread per key");
+                constexpr int kChunks = D / 16;                     // 16 codes each
+                uint32_t rows_on = 0;
+                float v_scale = 0.0f;
+                look_up(g, g.t0); scales_of(g, g.t0); look_up(g, g.t0 + 1);
+                for (int tile = g.t0; ok && tile <= g.t1; ++tile) {
+                    // (the scales of the next tile and the page of the one behind it are on their way meanwhile: three waits for memory a tile cost more than the widening)
+                    const uint32_t values_on = rows_on;
+                    const float scale[2] = { next_scale[0], v_scale };
+                    if (tile < g.t1) {
+                        rows_on = __ballot_sync(0xffffffffu, next_on);      // (the rows of a warp are its threads' keys)
+                        v_scale = next_scale[1];
+                        scales_of(g, tile + 1); look_up(g, tile + 2);
                     }
-                    const bool all = __all_sync(0xffffffffu, on);   // (the rows of a warp are its threads' keys)
-                    const uint32_t rows_on = __ballot_sync(0xffffffffu, on);
-#pragma unroll
+#pragma unroll 1
                     for (int kv = 0; kv < 2; ++kv) {
-                        const uint32_t n = 2 * it + kv, ss = n % C::kStaging, s = it % (kv ? C::kV : C::kK), turn = it / (kv ? C::kV : C::kK);
-                        if (!(ok = WAIT(st_full(ss), (n / C::kStaging) & 1))) break;
+                        if (kv ? tile == g.t0 : tile == g.t1) continue;
+                        const uint32_t item = it + uint32_t(tile - g.t0) - uint32_t(kv), ss = staged % C::kStaging, s = item % (kv ? C::kV : C::kK), turn = item / (kv ? C::kV : C::kK);
+                        if (!(ok = WAIT(st_full(ss), (staged / C::kStaging) & 1))) break;
                         if (turn && !(ok = WAIT(kv ? v_empty(s) : k_empty(s), (turn - 1) & 1))) break;
+                        ++staged;
+                        const uint32_t on = kv ? values_on : rows_on;
                         const uint8_t* from = smem + C::kOffStaging + ss * C::kCodes;
                         uint8_t* to = smem + (kv ? C::kOffV : C::kOffK) + s * C::kTile;
-                        // a warp takes its 32 rows, neighbouring lanes neighbouring pieces of a row
-#pragma unroll 4
+                        // a warp takes its 32 rows, neighbouring lanes neighbouring pieces of a row; all of a lane's pieces are read before the first is written
+                        uint4 codes[kChunks];
+#pragma unroll
+                        for (int e = 0; e < kChunks; ++e) codes[e] = *reinterpret_cast<const uint4*>(from + t / 32 * 32 * D + (e * 32 + lane) * 16);
+                        bar_arrive(st_empty(ss));
+#pragma unroll
                         for (int e = 0; e < kChunks; ++e) {
-                            const int at = e * 32 + lane, c = at % kChunks, r = t / 32 * 32 + at / kChunks;
-                            uint4 v = *reinterpret_cast<const uint4*>(from + r * D + c * 16);
-                            if (!all && !(rows_on >> (r & 31) & 1)) v = make_uint4(0, 0, 0, 0);
-                            const uint4 lo = make_uint4(widen<BF, CACHE>(v.x & 0xffffu), widen<BF, CACHE>(v.x >> 16), widen<BF, CACHE>(v.y & 0xffffu), widen<BF, CACHE>(v.y >> 16));
-                            const uint4 hi = make_uint4(widen<BF, CACHE>(v.z & 0xffffu), widen<BF, CACHE>(v.z >> 16), widen<BF, CACHE>(v.w & 0xffffu), widen<BF, CACHE>(v.w >> 16));
+                            const int c = lane % kChunks, r = t / 32 * 32 + e * (32 / kChunks) + lane / kChunks;
+                            uint4 v = codes[e];
+                            if (!(on >> (r & 31) & 1)) v = make_uint4(0, 0, 0, 0);
+                            const uint4 lo = make_uint4(widen<false, CACHE>(v.x & 0xffffu), widen<false, CACHE>(v.x >> 16), widen<false, CACHE>(v.y & 0xffffu), widen<false, CACHE>(v.y >> 16));
+                            const uint4 hi = make_uint4(widen<false, CACHE>(v.z & 0xffffu), widen<false, CACHE>(v.z >> 16), widen<false, CACHE>(v.w & 0xffffu), widen<false, CACHE>(v.w >> 16));
                             uint8_t* row = to + c / 4 * (kBN * 128) + r * 128;
                             const int p0 = ((2 * (c % 4)) ^ (r & 7)) * 16, p1 = ((2 * (c % 4) + 1) ^ (r & 7)) * 16;
                             if (c < 4) { *reinterpret_cast<uint4*>(row + p0) = lo; *reinterpret_cast<uint4*>(row + p1) = hi; }
                             else { *reinterpret_cast<uint4*>(row + p1) = hi; *reinterpret_cast<uint4*>(row + p0) = lo; }     // the other order: no bank twice
                         }
-                        reinterpret_cast<float*>(smem + C::kOffScales)[(kv * 4 + it % 4) * kBN + t] = scale[kv];
+                        reinterpret_cast<float*>(smem + C::kOffScales)[(kv * 4 + item % 4) * kBN + t] = scale[kv];
                         fence_async_proxy();
                         bar_arrive(kv ? v_full(s) : k_full(s));
-                        bar_arrive(st_empty(ss));
                     }
-                } else {
+                }
+                it += uint32_t(g.t1 - g.t0);
+            } else {
+                for (int tile = g.t0; ok && tile < g.t1; ++tile, ++it) {
+                    const int key0 = g.key_of(tile);
                     // ---- 16-bit values: those that no row of the unit sees become zeros (a weight of 0 does not silence a NaN), and so do, where some rows see them
                     // and others do not, those that are no numbers: they are added to the rows that see them at the segment's end ----
                     const uint32_t s = it % C::kV;
@@ -357,33 +409,64 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         const int w = warp / 4, r = tid % 128;
         const uint32_t lanes = uint32_t(warp % 4 * 32) << 16;
         const uint32_t tS = tmem + C::kColS + w * 128 + lanes, tP = tS + C::kColP, tO = tmem + C::kColO + w * D + lanes;
-        float2* ml_of = reinterpret_cast<float2*>(smem);            // [2][128], over the queries of a segment that is done with them
-        const float f = kQuant ? 1.0f : a.scale_log2;
-        const uint32_t kHidden = f < 0.0f ? 0x7f800000u : 0xff800000u;              // x f = -infinity
+        float4* ml_of = reinterpret_cast<float4*>(smem + (kQuant ? C::kOffMl : 0));         // [2][128], where there is no room over the queries of a segment that is done with them
+        float f = a.scale_log2;                                     // what turns a product into x (over a quantised cache, of this row, and times the key's scale)
+        const bool falling = a.scale_log2 < 0.0f;
+        const uint32_t kHidden = falling ? 0x7f800000u : 0xff800000u;               // x f = -infinity
         uint32_t it = 0, seg = 0, n_done = 0, meetings = 0;         // tiles before the segment, segments, jobs of this pipeline, meetings
         bool ok = true;
         auto meet = [&] { bar_arrive(meeting); ok = WAIT(meeting, meetings & 1); ++meetings; return ok; };      // of both pipelines (bounded, as every wait here)
+        auto token_of = [&](const Seg& g) { return g.tok0 + (g.two ? w : 0) * plan.tq + r / int(G); };
+        auto on_of = [&](const Seg& g) { return r < plan.tq * int(G) && token_of(g) < g.q_len; };
+        // Brings the queries of the pipeline's row tile (where the pipelines share one, the first brings it), zeros where there is no row, and returns f.
+        auto bring = [&](const Seg& g) {
+            const bool on = on_of(g);
+            float f = a.scale_log2;
+            if (g.two || w == 0 || (kQuant && BF)) {
+                const uint4* from = reinterpret_cast<const uint4*>(a.q + (uint64_t(g.q0 + (on ? token_of(g) : 0)) * a.q_stride + (uint64_t(g.h) * G + r % int(G)) * D) * 2);
+                uint8_t* row = smem + (g.two ? w : 0) * C::kQ + r * 128;
+                uint4 q[D / 8];
+#pragma unroll
+                for (int e = 0; e < D / 8; ++e) q[e] = on ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
+                if constexpr (kQuant && BF) {
+                    float mul;
+                    f *= lifted(q, mul);
+#pragma unroll
+                    for (int e = 0; e < D / 8; ++e)
+                        q[e] = make_uint4(W::pack(A::lo(q[e].x) * mul, A::hi(q[e].x) * mul), W::pack(A::lo(q[e].y) * mul, A::hi(q[e].y) * mul),
+                                          W::pack(A::lo(q[e].z) * mul, A::hi(q[e].z) * mul), W::pack(A::lo(q[e].w) * mul, A::hi(q[e].w) * mul));
+                }
+                if (g.two || w == 0) {
+#pragma unroll
+                    for (int e = 0; e < D / 8; ++e) *reinterpret_cast<uint4*>(row + e / 8 * (kBM * 128) + ((e ^ r) & 7) * 16) = q[e];
+                    fence_async_proxy();
+                }
+            }
+            bar_arrive(q_full);
+            return f;
+        };
+        if (plan.begin < plan.end) f = bring(segment(a, plan, plan.begin));
         for (uint32_t x = plan.begin; ok && x < plan.end; ++seg) {
             const Seg g = segment(a, plan, x);
             const int n = g.t1 - g.t0;
             x += uint32_t(n);
+            float f_after = f;
             const int rt = g.two ? w : 0;                           // row tile of this pipeline
-            const int tok = g.tok0 + rt * plan.tq + r / int(G);
-            const bool row_on = r < plan.tq * int(G) && tok < g.q_len;
+            const int tok = token_of(g);
+            const bool row_on = on_of(g);
             const bool any_on = __any_sync(0xffffffffu, row_on);
             const int tree_row = g.q0 + min(tok, g.q_len - 1);
-            // queries of row tile rt (the pipelines share one: the first brings it), put to zero where there is no row
-            if (g.two || w == 0) {
-                const uint4* from = reinterpret_cast<const uint4*>(a.q + (uint64_t(g.q0 + (row_on ? tok : 0)) * a.q_stride + (uint64_t(g.h) * G + r % int(G)) * D) * 2);
-                uint8_t* row = smem + rt * C::kQ + r * 128;
-#pragma unroll
-                for (int e = 0; e < D / 8; ++e) *reinterpret_cast<uint4*>(row + e / 8 * (kBM * 128) + ((e ^ r) & 7) * 16) = row_on ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
-                fence_async_proxy();
+            // the row's masks, up to itself, where two words hold them (looked up tile by tile they cost a fifth of a call over short contexts)
+            const bool short_tree = g.q_len <= 64;
+            unsigned long long mask = 0;
+            if (short_tree && row_on) {
+                const uint32_t* from = a.tree + uint64_t(uint32_t(tree_row)) * a.tree_words;
+                mask = __ldg(from) | (unsigned long long)(a.tree_words > 1 ? __ldg(from + 1) : 0u) << 32;
+                mask &= tok < 63 ? (2ull << tok) - 1 : ~0ull;
             }
-            bar_arrive(q_full);
             const int depth_place = a.window && row_on ? g.place0 + tree_depth(a.tree, a.tree_words, tree_row, tok) : 0;      // where the window counts from
             const int32_t* table = a.b.page_table + uint64_t(g.seq) * a.b.table_stride;
-            float m = kLow, l = 0.0f;
+            float m = kLow, l = 0.0f, unit = 0.0f, unit_inv = 0.0f; // unit: the largest value scale of this pipeline's tiles so far, what O is relative to
             const int jobs = g.jobs();
             for (int k = w; k < jobs; k += 2) {
                 const int tile = g.two ? k >> 1 : k, key0 = g.key_of(g.t0 + tile);
@@ -395,8 +478,12 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     const bool bad = *static_cast<volatile uint32_t*>(words + 3) & 1, masked = bad || g.mixed(a, key0);
                     auto visible = [&](int c0) {
                         const int first = key0 + c0, rel = first - g.place0;
-                        const int end = min(max(tok - rel + 1, 0), 32);            // columns before `end` are not ahead of the row
-                        uint32_t bits = (end == 32 ? ~0u : (1u << end) - 1) & tree_bits(a.tree, a.tree_words, tree_row, rel);
+                        uint32_t bits;
+                        if (short_tree) bits = rel <= -32 ? ~0u : rel >= 64 ? 0u : uint32_t(rel >= 0 ? mask >> rel : mask << -rel | ((1ull << -rel) - 1));
+                        else {
+                            const int end = min(max(tok - rel + 1, 0), 32);        // columns before `end` are not ahead of the row
+                            bits = (end == 32 ? ~0u : (1u << end) - 1) & tree_bits(a.tree, a.tree_words, tree_row, rel);
+                        }
                         if (a.window) {
                             const int from = min(max(depth_place - first + 1 - int(a.window), 0), min(max(-rel, 0), 32));      // context before `from` has left the window, unless it is a sink
                             const int sunk = min(max(int(a.sinks) - first, 0), 32);
@@ -410,7 +497,9 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     };
                     const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + item % 4 * kBN;
                     const float* vs = ks + 4 * kBN;
-                    if constexpr (kQuant) { if (!(ok = WAIT(v_full(item % C::kV), (item / C::kV) & 1))) break; }       // both scales are there (the next turn of this stage waits for the product)
+                    // (two versions: asking for every pair of weights cost a quantised cache more than the pairs)
+                    auto weigh = [&](auto masked_one) {
+                    constexpr bool kMasked = decltype(masked_one)::value;
                     // 32 columns: times the keys' scales (which hold the softmax scale) where the cache has them, hidden ones put away
                     auto fetch = [&](uint32_t* v, int c0) {
                         if constexpr (kQuant) {
@@ -423,16 +512,16 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                                 v[e] = __float_as_uint(y0); v[e + 1] = __float_as_uint(y1); v[e + 2] = __float_as_uint(y2); v[e + 3] = __float_as_uint(y3);
                             }
                         }
-                        if (masked) {                               // (the same for the whole warp)
+                        if constexpr (kMasked) {
                             const uint32_t bits = visible(c0);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) v[e] = bits & (1u << e) ? v[e] : kHidden;
                         }
                     };
-                    uint32_t v0[32], v1[32], v2[32];
-                    float top = f < 0.0f ? INFINITY : -INFINITY;
+                    uint32_t v0[32], v1[32];
+                    float top = falling ? INFINITY : -INFINITY;
                     auto widest = [&](const uint32_t* v) {
-                        if (f >= 0.0f) {
+                        if (!falling) {
                             float t0 = top, t1 = -INFINITY;
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) { t0 = fmaxf(t0, __uint_as_float(v[e])); t1 = fmaxf(t1, __uint_as_float(v[e + 1])); }
@@ -448,14 +537,24 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     fetch(v0, 0); widest(v0);
                     fetch(v1, 32); widest(v1);
                     __syncwarp();
-                    tm_ld32(tS + 64, v1); tm_ld32(tS + 96, v2);
-                    tm_wait_ld32(v1); tie32(v2);
-                    fetch(v1, 64); widest(v1);
-                    fetch(v2, 96); widest(v2);
+                    tm_ld32(tS + 64, v0); tm_ld32(tS + 96, v1);
+                    tm_wait_ld32(v0); tie32(v1);
+                    fetch(v0, 64); widest(v0);
+                    fetch(v1, 96); widest(v1);
                     top *= f;
                     if (!row_on) top = m;
-                    if (__any_sync(0xffffffffu, top > m + kLag)) {  // O so far shrinks (the products into it are done: the scores came behind them)
-                        const float mn = fmaxf(m, top), less = ex2(m - mn);
+                    float largest = 0.0f;
+                    if constexpr (kQuant) {
+                        if (!(ok = WAIT(v_full(item % C::kV), (item / C::kV) & 1))) return;       // the values' scales are there (the next turn of this stage waits for the product)
+                        const float4 v4 = *reinterpret_cast<const float4*>(vs + lane * 4);
+                        largest = fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w));
+                        largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(largest, unit))));      // (scales are not negative; a NaN is none here)
+                    }
+                    if (__any_sync(0xffffffffu, top > m + C::kLag) || largest > unit) {        // O so far shrinks (the products into it are done: the scores came behind them)
+                        const float mn = fmaxf(m, top);
+                        float less = ex2(m - mn);
+                        l *= less; m = mn;
+                        if (kQuant && largest > unit) { less *= __fdiv_rn(unit, largest); unit = largest; unit_inv = __fdiv_rn(1.0f, largest); }
                         if (k >= 2) {
 #pragma unroll 1
                             for (int c0 = 0; c0 < D; c0 += 16) {
@@ -467,7 +566,6 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                                 tm_st16(tO + c0, o);
                             }
                         }
-                        l *= less; m = mn;
                     }
                     const uint64_t f2 = pack2(f, f), m2 = pack2(C::kRaise - m, C::kRaise - m);
                     uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
@@ -482,23 +580,27 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                             if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
                             if constexpr (kQuant) {
                                 const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(vs + c0 + e / 4 * 4);
-                                unpack2(mul2(y, e % 4 ? v4.y : v4.x), y0, y1);
-                                if (masked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
+                                unpack2(mul2(mul2(y, pack2(unit_inv, unit_inv)), e % 4 ? v4.y : v4.x), y0, y1);
+                                if constexpr (kMasked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
                             }
-                            p[e / 2] = A::pack(y0, y1);
+                            p[e / 2] = W::pack(y0, y1);
                         }
                         tm_st16(tP + c0 / 2, p);
                     };
-                    weights(v2, 96);
-                    tm_ld32(tS, v0); tm_ld32(tS + 32, v2);          // read again: registers for the other half only
-                    weights(v1, 64);
-                    tm_wait_ld32(v0); tie32(v2);
+                    weights(v0, 64);
+                    tm_ld32(tS, v0);                                // read again: registers for one half only
+                    weights(v1, 96);
+                    tm_ld32(tS + 32, v1);
+                    tm_wait_ld32(v0); tie32(v1);
                     fetch(v0, 0); weights(v0, 0);
-                    fetch(v2, 32); weights(v2, 32);
+                    fetch(v1, 32); weights(v1, 32);
                     float s0, s1;
                     unpack2(add2(sum_a, sum_b), s0, s1);
                     l += s0 + s1;
                     tm_wait_st();
+                    };
+                    if (masked) weigh(std::true_type()); else weigh(std::false_type());
+                    if (!ok) break;
                 }
                 __syncwarp();
                 tc_before();
@@ -511,15 +613,21 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             tc_after();
             // ---- the segment's result: of this thread's row, or, where the pipelines shared the rows, of half its columns ----
             const bool joined = !g.two;
-            float other_m = kLow, other_l = 0.0f;
+            float other_m = kLow, other_l = 0.0f, other_unit = 1.0f;
+            if (!kQuant) unit = 1.0f;
             if (joined) {
-                ml_of[w * kBM + r] = make_float2(m, l);
+                ml_of[w * kBM + r] = make_float4(m, l, unit, 0.0f);
                 if (!meet()) break;
-                const float2 o = ml_of[(w ^ 1) * kBM + r];
-                other_m = o.x; other_l = o.y;
+                const float4 o = ml_of[(w ^ 1) * kBM + r];
+                other_m = o.x; other_l = o.y; other_unit = o.z;
+                if (!kQuant && !meet()) break;                      // (they lie where the next queries go)
             }
-            const float mm = fmaxf(m, other_m), mine = ex2(m - mm), theirs = ex2(other_m - mm);
+            // the next segment's queries: its first scores are on their way while this one's result is written
+            if (x < plan.end) f_after = bring(segment(a, plan, x));
+            const float mm = fmaxf(m, other_m);
+            float mine = ex2(m - mm), theirs = ex2(other_m - mm);
             const float ll = w ? other_l * theirs + l * mine : l * mine + other_l * theirs;
+            mine *= unit; theirs *= other_unit;
             const bool use_mine = w == 0 || jobs > 1, use_other = joined && (w == 1 || jobs > 1);       // (a pipeline without a job has no O)
             const uint32_t tOther = tmem + C::kColO + (w ^ 1) * D + lanes;
             const int c_from = joined ? w * (D / 2) : 0, c_to = joined ? c_from + D / 2 : D;
@@ -623,6 +731,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 }
             }
             if (joined && !meet()) break;                           // each has read the other's sums and O before the next segment's are written
+            f = f_after;
         }
     }
 #undef WAIT
@@ -673,9 +782,10 @@ cudaError_t launch_tree(const AttendArgs& a, uint32_t head_dim, int dtype, int c
     };
     using std::integral_constant;
     auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? go(bf, kind, integral_constant<int, 64>()) : go(bf, kind, integral_constant<int, 128>()); };
-    // (f16 weights over a quantised cache would have to follow the values' scales: those calls go to the row kernel)
-    if (dtype == WWWS_BF16) return cache == WWWS_CACHE_16 ? dim(std::true_type(), integral_constant<int, 0>()) : cache == WWWS_CACHE_INT8 ? dim(std::true_type(), integral_constant<int, 1>()) : dim(std::true_type(), integral_constant<int, 2>());
-    return cache == WWWS_CACHE_16 ? dim(std::false_type(), integral_constant<int, 0>()) : cudaErrorNotSupported;
+    auto kind = [&](auto bf) {
+        return cache == WWWS_CACHE_16 ? dim(bf, integral_constant<int, 0>()) : cache == WWWS_CACHE_INT8 ? dim(bf, integral_constant<int, 1>()) : dim(bf, integral_constant<int, 2>());
+    };
+    return dtype == WWWS_BF16 ? kind(std::true_type()) : kind(std::false_type());
 }
 
 }  // namespace wwws
