@@ -6,10 +6,10 @@
 //     O = O + P V          O stays in tensor memory, fp32
 // Bound by HBM: a tile of keys and values of head_dim 128 in 16 bits is 64 KB, 2,850 clocks of an SM's share of HBM, against 1,024 clocks of the tensor cores and as
 // many of the exponential unit per 128 rows.  So what counts is that loads never wait for anything:
-//   - Two pipelines, each with an S, an O and four softmax warps, take the jobs (a tile for 128 rows) in turn: while the tensor cores work for one, the
-//     other's softmax runs.  A unit of more than 128 rows (16-bit caches) gives each pipeline its own 128 rows and every tile; one of fewer
-//     gives them every other tile of the same rows, and their results are joined at the end.
-//   - One warp issues the matrix instructions in the order PV(n), S(n + 2); one issues the copies of pages, into rings of their own for keys and values.
+//   - Eight softmax warps, two S.  A unit of more than 128 rows (16-bit caches) is two row tiles, each with an S, an O and four of the warps: while the
+//     tensor cores work for one, the other's softmax runs.  One of fewer rows has a single O and its key tiles take the two S in turn: the next scores are worked out while
+//     all eight warps, 64 columns a thread, turn the last ones into weights.
+//   - One warp issues the matrix instructions in the order PV(n), S(n + 2), n counting the S; one issues the copies of pages, into rings of their own for keys and values.
 //   - Work is cut by key tiles: all (unit, tile) pairs laid end to end, an equal share for each of 148 blocks, found from a running sum over the
 //     sequences; cut units are joined by the last of their blocks, in block order.  Every role works out its segments by itself.
 //   - m is allowed to lag behind the true maximum by a factor (2^8, 2^1 over quantised caches), so that O is rescaled in the first few tiles only.
@@ -30,19 +30,21 @@ namespace {
 constexpr int kBM = 128, kBN = 128;
 constexpr float kLow = -3.0e38f;
 
-template <bool BF, int CACHE, int D> struct Cfg {
+template <bool BF, int CACHE, int D, bool kTwo> struct Cfg {
     static constexpr bool kQuant = CACHE != WWWS_CACHE_16;
     static constexpr int kSlabs = D / 64;
-    static constexpr int kQTiles = kQuant ? 1 : 2;          // row tiles of a unit, at most (a quantised cache's rings leave no room for two)
+    static_assert(!(kQuant && kTwo), "a quantised cache's rings leave no room for two row tiles");
+    static constexpr int kQTiles = kTwo ? 2 : 1;            // row tiles of a unit
     static constexpr int kTile = kBN * D * 2, kCodes = kBN * D;
     static constexpr int kQ = kBM * D * 2;
-    static constexpr int kK = kQuant ? 2 : D == 128 ? 3 : 4, kV = kQuant ? 2 : D == 128 ? 2 : 4, kStaging = kQuant ? (D == 128 ? 3 : 6) : 0;
+    static constexpr int kK = kQuant ? 2 : D == 128 ? 3 : 4, kV = kQuant || D == 128 ? 2 : 4, kStaging = kQuant ? (D == 128 ? 3 : 6) : 0;
     static constexpr int kOffK = kQTiles * kQ, kOffV = kOffK + kK * kTile, kOffStaging = kOffV + kV * kTile;
     // [keys, values][4 tiles][128]: the keys' of three more tiles may come while a tile's scores are weighted (the third's wait for that tile's product)
     static constexpr int kOffScales = kOffStaging + kStaging * kCodes;
-    static constexpr int kOffMl = kOffScales + (kQuant ? 2 * 4 * kBN * 4 : 0);
-    static constexpr int kOffBars = kOffMl + (kQuant ? 2 * kBM * 16 : 0);               // the sequences' running sum lies behind
-    static constexpr int kOffPrefix = kOffBars + 256;
+    static constexpr int kOffMl = kOffScales + (kQuant ? 2 * 4 * kBN * 4 : 0);           // [2 halves][128] sums
+    static constexpr int kOffTops = kOffMl + (kTwo ? 0 : 2 * kBM * 4);                  // [2 tiles][2 halves][128] maxima
+    static constexpr int kOffBars = kOffTops + (kTwo ? 0 : 2 * 2 * kBM * 4);            // the sequences' running sum lies behind
+    static constexpr int kOffPrefix = kOffBars + 384;
     static constexpr int kFixed = kOffPrefix + 1024;                        // the rings start at a 1,024-byte boundary
     static constexpr int kConvert = kQuant ? 4 : 1;                         // warps that widen codes, or look through 16-bit values
     static constexpr int kWarpConvert = 8, kWarpMma = kWarpConvert + kConvert, kWarpLoad = kWarpMma + 1, kThreads = (kWarpLoad + 1) * 32;
@@ -66,9 +68,7 @@ struct Seg {
     int t0, t1, tiles;                   // key tiles [t0, t1) of the unit's
     int lo, n_sink, lo_tile;             // first key that the window leaves to any row; tiles with sinks; first tile behind them
     uint32_t seq, x0;                    // sequence; position of tile t0
-    bool two;                            // two row tiles
     __device__ __forceinline__ int key_of(int t) const { return (t < n_sink ? t : lo_tile + t - n_sink) * kBN; }
-    __device__ __forceinline__ int jobs() const { return two ? 2 * (t1 - t0) : t1 - t0; }
     // whether a tile has keys that some row of the unit may not see
     __device__ __forceinline__ bool mixed(const AttendArgs& a, int key0) const
     {
@@ -101,7 +101,6 @@ __device__ __forceinline__ Seg segment(const AttendArgs& a, const Plan& p, uint3
     s.t0 = int(rel - unit * uint32_t(s.tiles));
     s.t1 = int(min(uint32_t(s.tiles), uint32_t(s.t0) + (p.end - x)));
     s.h = int(unit % hkv); s.tok0 = int(unit / hkv) * p.step;
-    s.two = p.step > p.tq && s.tok0 + p.tq < s.q_len;
     return s;
 }
 
@@ -117,11 +116,11 @@ template <int N> __device__ __forceinline__ float lifted(const uint4 (&q)[N], fl
     return __uint_as_float((254 - me) << 23);
 }
 
-template <bool BF, int CACHE, int D>
-__global__ void __launch_bounds__(Cfg<BF, CACHE, D>::kThreads, 1)
+template <bool BF, int CACHE, int D, bool kTwo>
+__global__ void __launch_bounds__(Cfg<BF, CACHE, D, kTwo>::kThreads, 1)
 k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
-    using C = Cfg<BF, CACHE, D>;
+    using C = Cfg<BF, CACHE, D, kTwo>;
     using A = Act<BF>;
     using W = Act<C::kB>;
     constexpr bool kQuant = C::kQuant;
@@ -142,8 +141,10 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
     const uint32_t q_full = bars + 8 * kMore, done = q_full + 8, drained = q_full + 16;
     auto s_full = [&](int w) { return q_full + 24 + 8 * w; };
     auto p_full = [&](int w) { return q_full + 40 + 8 * w; };
-    const uint32_t meeting = q_full + 56;
-    static_assert(8 * (kMore + 8) <= 256, "barriers fit");
+    const uint32_t meeting = q_full + 56, o_done = q_full + 64;
+    auto p_both = [&](uint32_t b) { return q_full + 72 + 8 * b; };
+    auto pair = [&](int q) { return q_full + 88 + 8 * q; };          // the two warps that share 32 rows
+    static_assert(8 * (kMore + 15) <= 384, "barriers fit");
     uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + C::kOffPrefix);
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
@@ -177,8 +178,9 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         for (int s = 0; s < C::kK; ++s) { bar_init(k_full(s), kQuant ? C::kConvert * 32 : 1); bar_init(k_empty(s), 1); }
         for (int s = 0; s < C::kV; ++s) { bar_init(v_full(s), kQuant ? C::kConvert * 32 : 1); bar_init(v_empty(s), 1); if (!kQuant) bar_init(v_ready(s), 1); }
         for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), C::kConvert * 32); }
-        bar_init(q_full, 256); bar_init(done, 1); bar_init(drained, 1); bar_init(meeting, 256);
-        for (int w = 0; w < 2; ++w) { bar_init(s_full(w), 1); bar_init(p_full(w), 128); }
+        bar_init(q_full, 256); bar_init(done, 1); bar_init(drained, 1); bar_init(meeting, 256); bar_init(o_done, 1);
+        for (int w = 0; w < 2; ++w) { bar_init(s_full(w), 1); bar_init(p_full(w), 128); bar_init(p_both(w), 256); }
+        for (int q = 0; q < 4; ++q) bar_init(pair(q), 64);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
@@ -251,26 +253,25 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         // ---- matrix instructions ----
         constexpr uint32_t kDescS = mma_desc(C::kB, false, kBN), kDescO = mma_desc(C::kB, true, D);
         const uint32_t one = elect_one();
-        uint32_t it = 0, seg = 0, jobs_of[2] = { 0, 0 };            // tiles before the segment; segments; jobs of each pipeline (the parity of p_full)
+        uint32_t it = 0, seg = 0, jobs_of[2] = { 0, 0 }, both_of[2] = { 0, 0 };     // tiles before the segment; segments; jobs of each pipeline and of each S (the parities of p_full and p_both)
         bool ok = true;
         auto commit = [&](uint32_t bar) { tc_commit_one(one, bar); };
         for (uint32_t x = plan.begin; ok && x < plan.end; ++seg) {
             const Seg g = segment(a, plan, x);
             const uint32_t n = uint32_t(g.t1 - g.t0);
             x += n;
-            const bool two = g.two;
-            const int jobs = g.jobs();
+            const int jobs = int(n) * (kTwo ? 2 : 1);
             // job k: tile k or k / 2 of the segment, row tile 0 or k % 2
             auto scores = [&](int k) {
                 const int w = k & 1;
-                const uint32_t item = it + uint32_t(two ? k >> 1 : k), s = item % C::kK;
-                if (!two || w == 0) { if (!(ok = WAIT(k_full(s), (item / C::kK) & 1))) return; tc_after(); }
-                const uint64_t qa = smem_desc(base + (two ? w : 0) * C::kQ, 16, 1024), kb = smem_desc(base + C::kOffK + s * C::kTile, 16, 1024);
+                const uint32_t item = it + uint32_t(kTwo ? k >> 1 : k), s = item % C::kK;
+                if (!kTwo || w == 0) { if (!(ok = WAIT(k_full(s), (item / C::kK) & 1))) return; tc_after(); }
+                const uint64_t qa = smem_desc(base + (kTwo ? w : 0) * C::kQ, 16, 1024), kb = smem_desc(base + C::kOffK + s * C::kTile, 16, 1024);
 #pragma unroll
                 for (int e = 0; e < D / 16; ++e)                    // (descriptors count 16 bytes)
                     mma_ss(one, tmem + C::kColS + w * 128, qa + (e / 4 * (kBM * 128) + e % 4 * 32) / 16, kb + (e / 4 * (kBN * 128) + e % 4 * 32) / 16, kDescS, e > 0);
                 commit(s_full(w));
-                if (!two || w == 1) commit(k_empty(s));
+                if (!kTwo || w == 1) commit(k_empty(s));
             };
             if (!(ok = WAIT(q_full, seg & 1))) break;
             tc_after();
@@ -278,15 +279,16 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             if (ok && jobs > 1) scores(1);
             for (int k = 0; ok && k < jobs; ++k) {
                 const int w = k & 1;
-                const uint32_t item = it + uint32_t(two ? k >> 1 : k), s = item % C::kV;
-                if (!two || w == 0) { if (!(ok = WAIT(kQuant ? v_full(s) : v_ready(s), (item / C::kV) & 1))) break; }
-                if (!(ok = WAIT(p_full(w), jobs_of[w] & 1))) break;
-                ++jobs_of[w];
+                const uint32_t item = it + uint32_t(kTwo ? k >> 1 : k), s = item % C::kV;
+                if (!kTwo || w == 0) { if (!(ok = WAIT(kQuant ? v_full(s) : v_ready(s), (item / C::kV) & 1))) break; }
+                if (!(ok = WAIT(kTwo ? p_full(w) : p_both(w), (kTwo ? jobs_of[w] : both_of[w]) & 1))) break;
+                ++(kTwo ? jobs_of[w] : both_of[w]);
                 tc_after();
                 const uint64_t vb = smem_desc(base + C::kOffV + s * C::kTile, kBN * 128, 1024);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) mma_ts(one, tmem + C::kColO + w * D, tmem + C::kColS + w * 128 + C::kColP + e * 8, vb + e * 2048 / 16, kDescO, k >= 2 || e > 0);
-                if (!two || w == 1) commit(v_empty(s));
+                for (int e = 0; e < 8; ++e) mma_ts(one, tmem + C::kColO + (kTwo ? w : 0) * D, tmem + C::kColS + w * 128 + C::kColP + e * 8, vb + e * 2048 / 16, kDescO, k >= (kTwo ? 2 : 1) || e > 0);
+                if (!kTwo) commit(o_done);
+                if (!kTwo || w == 1) commit(v_empty(s));
                 if (k + 2 < jobs) scores(k + 2);
             }
             if (ok) commit(done);
@@ -408,23 +410,21 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         // ---- softmax: pipeline w, a row per thread ----
         const int w = warp / 4, r = tid % 128;
         const uint32_t lanes = uint32_t(warp % 4 * 32) << 16;
-        const uint32_t tS = tmem + C::kColS + w * 128 + lanes, tP = tS + C::kColP, tO = tmem + C::kColO + w * D + lanes;
-        float4* ml_of = reinterpret_cast<float4*>(smem + (kQuant ? C::kOffMl : 0));         // [2][128], where there is no room over the queries of a segment that is done with them
         float f = a.scale_log2;                                     // what turns a product into x (over a quantised cache, of this row, and times the key's scale)
         const bool falling = a.scale_log2 < 0.0f;
         const uint32_t kHidden = falling ? 0x7f800000u : 0xff800000u;               // x f = -infinity
-        uint32_t it = 0, seg = 0, n_done = 0, meetings = 0;         // tiles before the segment, segments, jobs of this pipeline, meetings
+        uint32_t it = 0, seg = 0, scored[2] = { 0, 0 }, products = 0, meetings = 0, pairs = 0;      // tiles before the segment, segments, scores in each S so far, products of both halves, meetings
         bool ok = true;
         auto meet = [&] { bar_arrive(meeting); ok = WAIT(meeting, meetings & 1); ++meetings; return ok; };      // of both pipelines (bounded, as every wait here)
-        auto token_of = [&](const Seg& g) { return g.tok0 + (g.two ? w : 0) * plan.tq + r / int(G); };
+        auto token_of = [&](const Seg& g) { return g.tok0 + (kTwo ? w : 0) * plan.tq + r / int(G); };
         auto on_of = [&](const Seg& g) { return r < plan.tq * int(G) && token_of(g) < g.q_len; };
         // Brings the queries of the pipeline's row tile (where the pipelines share one, the first brings it), zeros where there is no row, and returns f.
         auto bring = [&](const Seg& g) {
             const bool on = on_of(g);
             float f = a.scale_log2;
-            if (g.two || w == 0 || (kQuant && BF)) {
+            if (kTwo || w == 0 || (kQuant && BF)) {
                 const uint4* from = reinterpret_cast<const uint4*>(a.q + (uint64_t(g.q0 + (on ? token_of(g) : 0)) * a.q_stride + (uint64_t(g.h) * G + r % int(G)) * D) * 2);
-                uint8_t* row = smem + (g.two ? w : 0) * C::kQ + r * 128;
+                uint8_t* row = smem + (kTwo ? w : 0) * C::kQ + r * 128;
                 uint4 q[D / 8];
 #pragma unroll
                 for (int e = 0; e < D / 8; ++e) q[e] = on ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
@@ -436,7 +436,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                         q[e] = make_uint4(W::pack(A::lo(q[e].x) * mul, A::hi(q[e].x) * mul), W::pack(A::lo(q[e].y) * mul, A::hi(q[e].y) * mul),
                                           W::pack(A::lo(q[e].z) * mul, A::hi(q[e].z) * mul), W::pack(A::lo(q[e].w) * mul, A::hi(q[e].w) * mul));
                 }
-                if (g.two || w == 0) {
+                if (kTwo || w == 0) {
 #pragma unroll
                     for (int e = 0; e < D / 8; ++e) *reinterpret_cast<uint4*>(row + e / 8 * (kBM * 128) + ((e ^ r) & 7) * 16) = q[e];
                     fence_async_proxy();
@@ -451,7 +451,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             const int n = g.t1 - g.t0;
             x += uint32_t(n);
             float f_after = f;
-            const int rt = g.two ? w : 0;                           // row tile of this pipeline
+            const int rt = kTwo ? w : 0;                           // row tile of this pipeline
             const int tok = token_of(g);
             const bool row_on = on_of(g);
             const bool any_on = __any_sync(0xffffffffu, row_on);
@@ -466,127 +466,138 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             }
             const int depth_place = a.window && row_on ? g.place0 + tree_depth(a.tree, a.tree_words, tree_row, tok) : 0;      // where the window counts from
             const int32_t* table = a.b.page_table + uint64_t(g.seq) * a.b.table_stride;
-            float m = kLow, l = 0.0f, unit = 0.0f, unit_inv = 0.0f; // unit: the largest value scale of this pipeline's tiles so far, what O is relative to
-            const int jobs = g.jobs();
-            for (int k = w; k < jobs; k += 2) {
-                const int tile = g.two ? k >> 1 : k, key0 = g.key_of(g.t0 + tile);
-                const uint32_t item = it + uint32_t(tile);
-                if (!(ok = WAIT(s_full(w), n_done & 1))) break;
-                tc_after();
-                if (any_on) {
-                    // which columns [c0, c0 + 32) the row sees, a bit each
-                    const bool bad = *static_cast<volatile uint32_t*>(words + 3) & 1, masked = bad || g.mixed(a, key0);
-                    auto visible = [&](int c0) {
-                        const int first = key0 + c0, rel = first - g.place0;
-                        uint32_t bits;
-                        if (short_tree) bits = rel <= -32 ? ~0u : rel >= 64 ? 0u : uint32_t(rel >= 0 ? mask >> rel : mask << -rel | ((1ull << -rel) - 1));
-                        else {
-                            const int end = min(max(tok - rel + 1, 0), 32);        // columns before `end` are not ahead of the row
-                            bits = (end == 32 ? ~0u : (1u << end) - 1) & tree_bits(a.tree, a.tree_words, tree_row, rel);
-                        }
-                        if (a.window) {
-                            const int from = min(max(depth_place - first + 1 - int(a.window), 0), min(max(-rel, 0), 32));      // context before `from` has left the window, unless it is a sink
-                            const int sunk = min(max(int(a.sinks) - first, 0), 32);
-                            bits &= (from == 32 ? 0u : ~0u << from) | (sunk == 32 ? ~0u : (1u << sunk) - 1);
-                        }
-                        if (bad)
-#pragma unroll 1
-                            for (int e = 0; e < 2; ++e)
-                                if (const int key = first + 16 * e; key >= 0 && key < g.kv && bits >> (16 * e) & 0xffffu && uint32_t(__ldg(table + (uint32_t(key) >> a.p.page_shift))) >= a.p.n_pages) bits &= ~(0xffffu << (16 * e));
-                        return row_on ? bits : 0u;
-                    };
-                    const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + item % 4 * kBN;
-                    const float* vs = ks + 4 * kBN;
-                    // (two versions: asking for every pair of weights cost a quantised cache more than the pairs)
-                    auto weigh = [&](auto masked_one) {
-                    constexpr bool kMasked = decltype(masked_one)::value;
-                    // 32 columns: times the keys' scales (which hold the softmax scale) where the cache has them, hidden ones put away
-                    auto fetch = [&](uint32_t* v, int c0) {
-                        if constexpr (kQuant) {
+            float m = kLow, l = 0.0f, unit = 0.0f, unit_inv = 0.0f; // unit: the largest value scale of the segment's tiles so far, what O is relative to
+            bool bad_met = false;
+                                auto visible = [&](int first) {        // the columns of keys [first, first + 32) that the row sees, a bit each
+                                    const int rel = first - g.place0;
+                                    uint32_t bits;
+                                    if (short_tree) bits = rel <= -32 ? ~0u : rel >= 64 ? 0u : uint32_t(rel >= 0 ? mask >> rel : mask << -rel | ((1ull << -rel) - 1));
+                                    else {
+                                        const int end = min(max(tok - rel + 1, 0), 32);        // columns before `end` are not ahead of the row
+                                        bits = (end == 32 ? ~0u : (1u << end) - 1) & tree_bits(a.tree, a.tree_words, tree_row, rel);
+                                    }
+                                    if (a.window) {
+                                        const int from = min(max(depth_place - first + 1 - int(a.window), 0), min(max(-rel, 0), 32));      // context before `from` has left the window, unless it is a sink
+                                        const int sunk = min(max(int(a.sinks) - first, 0), 32);
+                                        bits &= (from == 32 ? 0u : ~0u << from) | (sunk == 32 ? ~0u : (1u << sunk) - 1);
+                                    }
+                                    if (bad_met)
+            #pragma unroll 1
+                                        for (int e = 0; e < 2; ++e)
+                                            if (const int key = first + 16 * e; key >= 0 && key < g.kv && bits >> (16 * e) & 0xffffu && uint32_t(__ldg(table + (uint32_t(key) >> a.p.page_shift))) >= a.p.n_pages) bits &= ~(0xffffu << (16 * e));
+                                    return row_on ? bits : 0u;
+                                };
+            // The scores of one S to weights: all 128 columns by one thread (kHalf false, S and O of the pipeline), or 64 by each of two, who tell one another their maxima.
+            auto weigh = [&](auto masked_one, int key0, uint32_t item, uint32_t buffer, int tile) {
+                constexpr bool kMasked = decltype(masked_one)::value, kHalf = !kTwo;
+                const int cb = kHalf ? w * 64 : 0;
+                const uint32_t tS = tmem + C::kColS + buffer * 128 + cb + lanes, tP = tmem + C::kColS + buffer * 128 + C::kColP + cb / 2 + lanes;
+                const uint32_t tO = tmem + C::kColO + w * (kHalf ? D / 2 : D) + lanes;
+                const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + item % 4 * kBN + cb;
+                [[maybe_unused]] const float* vs = ks + 4 * kBN;
+                // 32 columns: times the keys' scales where the cache has them, hidden ones put away
+                auto fetch = [&](uint32_t* v, int c0) {
+                    if constexpr (kQuant) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(ks + c0 + e);
-                                float y0, y1, y2, y3;
-                                unpack2(mul2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), k4.x), y0, y1);
-                                unpack2(mul2(pack2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), k4.y), y2, y3);
-                                v[e] = __float_as_uint(y0); v[e + 1] = __float_as_uint(y1); v[e + 2] = __float_as_uint(y2); v[e + 3] = __float_as_uint(y3);
-                            }
+                        for (int e = 0; e < 32; e += 4) {
+                            const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(ks + c0 + e);
+                            float y0, y1, y2, y3;
+                            unpack2(mul2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), k4.x), y0, y1);
+                            unpack2(mul2(pack2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), k4.y), y2, y3);
+                            v[e] = __float_as_uint(y0); v[e + 1] = __float_as_uint(y1); v[e + 2] = __float_as_uint(y2); v[e + 3] = __float_as_uint(y3);
                         }
-                        if constexpr (kMasked) {
-                            const uint32_t bits = visible(c0);
+                    }
+                    if constexpr (kMasked) {
+                        const uint32_t bits = visible(key0 + cb + c0);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = bits & (1u << e) ? v[e] : kHidden;
-                        }
-                    };
-                    uint32_t v0[32], v1[32];
-                    float top = falling ? INFINITY : -INFINITY;
-                    auto widest = [&](const uint32_t* v) {
-                        if (!falling) {
-                            float t0 = top, t1 = -INFINITY;
+                        for (int e = 0; e < 32; ++e) v[e] = bits & (1u << e) ? v[e] : kHidden;
+                    }
+                };
+                uint32_t v0[32], v1[32];
+                float top = falling ? INFINITY : -INFINITY;
+                auto widest = [&](const uint32_t* v) {
+                    if (!falling) {
+                        float t0 = top, t1 = -INFINITY;
 #pragma unroll
-                            for (int e = 0; e < 32; e += 2) { t0 = fmaxf(t0, __uint_as_float(v[e])); t1 = fmaxf(t1, __uint_as_float(v[e + 1])); }
-                            top = fmaxf(t0, t1);
-                        } else {
+                        for (int e = 0; e < 32; e += 2) { t0 = fmaxf(t0, __uint_as_float(v[e])); t1 = fmaxf(t1, __uint_as_float(v[e + 1])); }
+                        top = fmaxf(t0, t1);
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) top = fminf(top, __uint_as_float(v[e]));
-                        }
-                    };
-                    __syncwarp();
-                    tm_ld32(tS, v0); tm_ld32(tS + 32, v1);
-                    tm_wait_ld32(v0); tie32(v1);
-                    fetch(v0, 0); widest(v0);
-                    fetch(v1, 32); widest(v1);
+                        for (int e = 0; e < 32; ++e) top = fminf(top, __uint_as_float(v[e]));
+                    }
+                };
+                __syncwarp();
+                tm_ld32(tS, v0); tm_ld32(tS + 32, v1);
+                tm_wait_ld32(v0); tie32(v1);
+                fetch(v0, 0); widest(v0);
+                fetch(v1, 32); widest(v1);
+                if constexpr (!kHalf) {
                     __syncwarp();
                     tm_ld32(tS + 64, v0); tm_ld32(tS + 96, v1);
                     tm_wait_ld32(v0); tie32(v1);
                     fetch(v0, 64); widest(v0);
                     fetch(v1, 96); widest(v1);
-                    top *= f;
-                    if (!row_on) top = m;
-                    float largest = 0.0f;
-                    if constexpr (kQuant) {
-                        if (!(ok = WAIT(v_full(item % C::kV), (item / C::kV) & 1))) return;       // the values' scales are there (the next turn of this stage waits for the product)
-                        const float4 v4 = *reinterpret_cast<const float4*>(vs + lane * 4);
-                        largest = fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w));
-                        largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(largest, unit))));      // (scales are not negative; a NaN is none here)
-                    }
-                    if (__any_sync(0xffffffffu, top > m + C::kLag) || largest > unit) {        // O so far shrinks (the products into it are done: the scores came behind them)
-                        const float mn = fmaxf(m, top);
-                        float less = ex2(m - mn);
-                        l *= less; m = mn;
-                        if (kQuant && largest > unit) { less *= __fdiv_rn(unit, largest); unit = largest; unit_inv = __fdiv_rn(1.0f, largest); }
-                        if (k >= 2) {
+                }
+                top *= f;
+                if constexpr (kHalf) {
+                    float* tops = reinterpret_cast<float*>(smem + C::kOffTops) + (tile & 1) * 2 * kBM + r;
+                    tops[w * kBM] = top;
+                    bar_arrive(pair(warp % 4));                      // (both have read S as well: weights may go over it)
+                    if (!(ok = WAIT(pair(warp % 4), pairs & 1))) return;
+                    ++pairs;
+                    top = fmaxf(top, tops[(w ^ 1) * kBM]);
+                }
+                if (!row_on) top = m;
+                float largest = 0.0f;
+                if constexpr (kQuant) {
+                    if (!(ok = WAIT(v_full(item % C::kV), (item / C::kV) & 1))) return;       // the values' scales are there (the next turn of this stage waits for the product)
+                    const float4 v4 = *reinterpret_cast<const float4*>(vs - cb + lane * 4);
+                    largest = fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w));
+                    largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(largest, unit))));      // (scales are not negative; a NaN is none here)
+                }
+                if (__any_sync(0xffffffffu, top > m + C::kLag) || largest > unit) {            // O so far shrinks
+                    const float mn = fmaxf(m, top);
+                    float less = ex2(m - mn);
+                    l *= less; m = mn;
+                    if (kQuant && largest > unit) { less *= __fdiv_rn(unit, largest); unit = largest; unit_inv = __fdiv_rn(1.0f, largest); }
+                    if (tile > 0) {
+                        // one S and O: the products into it were issued before these scores; two S and an O: the last product may be under way
+                        if constexpr (kHalf) { if (!(ok = WAIT(o_done, (products + uint32_t(tile) - 1) & 1))) return; tc_after(); }
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 16) {
-                                uint32_t o[16];
-                                tm_ld16(tO + c0, o);
-                                tm_wait_ld16(o);
+                        for (int c0 = 0; c0 < (kHalf ? D / 2 : D); c0 += 32) {
+                            uint32_t o[32];
+                            tm_ld32(tO + c0, o);
+                            tm_wait_ld32(o);
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * less);
-                                tm_st16(tO + c0, o);
-                            }
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * less);
+                            tm_st16(tO + c0, o); tm_st16(tO + c0 + 16, o + 16);
                         }
                     }
-                    const uint64_t f2 = pack2(f, f), m2 = pack2(C::kRaise - m, C::kRaise - m);
-                    uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
-                    auto weights = [&](const uint32_t* v, int c0) {
-                        uint32_t p[16];
+                }
+                const uint64_t f2 = pack2(f, f), m2 = pack2(C::kRaise - m, C::kRaise - m);
+                uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
+                auto weights = [&](const uint32_t* v, int c0) {
+                    uint32_t p[16];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float y0, y1;
-                            unpack2(fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, m2), y0, y1);
-                            y0 = ex2(y0); y1 = ex2(y1);
-                            const uint64_t y = pack2(y0, y1);
-                            if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
-                            if constexpr (kQuant) {
-                                const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(vs + c0 + e / 4 * 4);
-                                unpack2(mul2(mul2(y, pack2(unit_inv, unit_inv)), e % 4 ? v4.y : v4.x), y0, y1);
-                                if constexpr (kMasked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
-                            }
-                            p[e / 2] = W::pack(y0, y1);
+                    for (int e = 0; e < 32; e += 2) {
+                        float y0, y1;
+                        unpack2(fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, m2), y0, y1);
+                        y0 = ex2(y0); y1 = ex2(y1);
+                        const uint64_t y = pack2(y0, y1);
+                        if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
+                        if constexpr (kQuant) {
+                            const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(vs + c0 + e / 4 * 4);
+                            unpack2(mul2(mul2(y, pack2(unit_inv, unit_inv)), e % 4 ? v4.y : v4.x), y0, y1);
+                            if constexpr (kMasked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
                         }
-                        tm_st16(tP + c0 / 2, p);
-                    };
+                        p[e / 2] = W::pack(y0, y1);
+                    }
+                    tm_st16(tP + c0 / 2, p);
+                };
+                if constexpr (kHalf) {
+                    weights(v0, 0);
+                    weights(v1, 32);
+                } else {
                     weights(v0, 64);
                     tm_ld32(tS, v0);                                // read again: registers for one half only
                     weights(v1, 96);
@@ -594,42 +605,47 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     tm_wait_ld32(v0); tie32(v1);
                     fetch(v0, 0); weights(v0, 0);
                     fetch(v1, 32); weights(v1, 32);
-                    float s0, s1;
-                    unpack2(add2(sum_a, sum_b), s0, s1);
-                    l += s0 + s1;
-                    tm_wait_st();
-                    };
-                    if (masked) weigh(std::true_type()); else weigh(std::false_type());
+                }
+                float s0, s1;
+                unpack2(add2(sum_a, sum_b), s0, s1);
+                l += s0 + s1;
+                tm_wait_st();
+            };
+            for (int tile = 0; tile < n; ++tile) {
+                const int key0 = g.key_of(g.t0 + tile);
+                const uint32_t item = it + uint32_t(tile), buffer = kTwo ? uint32_t(w) : uint32_t(tile) & 1;
+                if (!(ok = WAIT(s_full(buffer), (buffer ? scored[1] : scored[0]) & 1))) break;
+                if (kTwo) { ++scored[0]; ++scored[1]; } else ++(buffer ? scored[1] : scored[0]);
+                tc_after();
+                if (any_on) {
+                    bad_met = *static_cast<volatile uint32_t*>(words + 3) & 1;
+                    const bool masked = bad_met || g.mixed(a, key0);
+                    // (versions with and without masks: asking for every pair of weights cost a quantised cache more than the pairs)
+                    using std::bool_constant;
+                    if (masked) weigh(bool_constant<true>(), key0, item, buffer, tile); else weigh(bool_constant<false>(), key0, item, buffer, tile);
                     if (!ok) break;
                 }
                 __syncwarp();
                 tc_before();
-                bar_arrive(p_full(w));
-                ++n_done;
+                bar_arrive(kTwo ? p_full(w) : p_both(buffer));
             }
             if (!ok) break;
             it += uint32_t(n);
             if (!(ok = WAIT(done, seg & 1))) break;
             tc_after();
             // ---- the segment's result: of this thread's row, or, where the pipelines shared the rows, of half its columns ----
-            const bool joined = !g.two;
-            float other_m = kLow, other_l = 0.0f, other_unit = 1.0f;
-            if (!kQuant) unit = 1.0f;
+            constexpr bool joined = !kTwo;
+            if (joined) products += uint32_t(n);
+            float ll = l;
             if (joined) {
-                ml_of[w * kBM + r] = make_float4(m, l, unit, 0.0f);
+                reinterpret_cast<float*>(smem + C::kOffMl)[w * kBM + r] = l;
                 if (!meet()) break;
-                const float4 o = ml_of[(w ^ 1) * kBM + r];
-                other_m = o.x; other_l = o.y; other_unit = o.z;
-                if (!kQuant && !meet()) break;                      // (they lie where the next queries go)
+                const float other = reinterpret_cast<const float*>(smem + C::kOffMl)[(w ^ 1) * kBM + r];
+                ll = w ? other + l : l + other;
             }
             // the next segment's queries: its first scores are on their way while this one's result is written
             if (x < plan.end) f_after = bring(segment(a, plan, x));
-            const float mm = fmaxf(m, other_m);
-            float mine = ex2(m - mm), theirs = ex2(other_m - mm);
-            const float ll = w ? other_l * theirs + l * mine : l * mine + other_l * theirs;
-            mine *= unit; theirs *= other_unit;
-            const bool use_mine = w == 0 || jobs > 1, use_other = joined && (w == 1 || jobs > 1);       // (a pipeline without a job has no O)
-            const uint32_t tOther = tmem + C::kColO + (w ^ 1) * D + lanes;
+            const uint32_t tO = tmem + C::kColO + (joined ? 0 : w) * D + lanes;
             const int c_from = joined ? w * (D / 2) : 0, c_to = joined ? c_from + D / 2 : D;
             const bool whole = g.t0 == 0 && g.t1 == g.tiles;
             const uint32_t slot = 2 * blockIdx.x + (g.x0 == plan.begin ? 0 : 1);
@@ -638,15 +654,12 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             const bool unreal_met = !kQuant && (*static_cast<volatile uint32_t*>(words + 3) & 2);
 #pragma unroll 1
             for (int c0 = c_from; c0 < c_to; c0 += 32) {
-                uint32_t v[32], o[32];
-                tm_ld32(tO + c0, v); tm_ld32(tOther + c0, o);
-                tm_wait_ld32(v); tie32(o);
+                uint32_t v[32];
+                tm_ld32(tO + c0, v);
+                tm_wait_ld32(v);
                 float y[32];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float p = use_mine ? __uint_as_float(v[e]) * mine : 0.0f, q = use_other ? __uint_as_float(o[e]) * theirs : 0.0f;
-                    y[e] = w ? q + p : p + q;                       // (the same order whichever half it is)
-                }
+                for (int e = 0; e < 32; ++e) y[e] = kQuant ? __uint_as_float(v[e]) * unit : __uint_as_float(v[e]);
                 if constexpr (!kQuant) {
                     if (unreal_met && row_on) {                     // values that are no numbers, to the rows that see them
 #pragma unroll 1
@@ -686,7 +699,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 }
                 __syncwarp();
             }
-            if (!whole && row_on && (g.two || w == 0)) a.s.part_ml[(slot * 2 + rt) * kBM + r] = make_float2(mm, ll);
+            if (!whole && row_on && (kTwo || w == 0)) a.s.part_ml[(slot * 2 + rt) * kBM + r] = make_float2(m, ll);
             tc_before();
             if (!whole) {
                 // the unit's blocks are consecutive; the last to arrive joins their parts in that order
@@ -730,7 +743,6 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     if (tid == 0) a.s.ticket[first_slot] = 0;
                 }
             }
-            if (joined && !meet()) break;                           // each has read the other's sums and O before the next segment's are written
             f = f_after;
         }
     }
@@ -771,17 +783,21 @@ cudaError_t launch_tree(const AttendArgs& a, uint32_t head_dim, int dtype, int c
                    CU_TENSOR_MAP_INTERLEAVE_NONE, quant ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return cudaErrorInvalidValue;
     }
-    auto go = [&](auto bf, auto kind, auto dim) -> cudaError_t {
-        using C = Cfg<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
+    // Two row tiles where the longest sequence has more than 128 rows (its shorter ones then leave the second empty).
+    const bool two = !quant && uint64_t(a.b.max_q_len) * a.group > uint64_t(kBM / a.group * a.group);
+    auto go = [&](auto bf, auto kind, auto dim, auto tiles) -> cudaError_t {
+        constexpr bool kTwo = decltype(tiles)::value && decltype(kind)::value == WWWS_CACHE_16;
+        using C = Cfg<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value, kTwo>;
         static_assert(C::kFixed + (kTreeSeqs + 1) * 4 <= 232448 - 256, "shared memory of a block");
-        constexpr auto kernel = k_tree<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value>;
+        constexpr auto kernel = k_tree<decltype(bf)::value, decltype(kind)::value, decltype(dim)::value, kTwo>;
         const uint32_t smem = C::kFixed + (a.b.n_seqs + 1) * 4;
         if (cudaError_t e = allow_smem<kernel>(C::kFixed + (kTreeSeqs + 1) * 4); e != cudaSuccess) return e;
         kernel<<<kTileBlocks, C::kThreads, smem, s>>>(a, maps[0], maps[1]);
         return cudaGetLastError();
     };
     using std::integral_constant;
-    auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? go(bf, kind, integral_constant<int, 64>()) : go(bf, kind, integral_constant<int, 128>()); };
+    auto row_tiles = [&](auto bf, auto kind, auto dim) { return two ? go(bf, kind, dim, std::true_type()) : go(bf, kind, dim, std::false_type()); };
+    auto dim = [&](auto bf, auto kind) { return head_dim == 64 ? row_tiles(bf, kind, integral_constant<int, 64>()) : row_tiles(bf, kind, integral_constant<int, 128>()); };
     auto kind = [&](auto bf) {
         return cache == WWWS_CACHE_16 ? dim(bf, integral_constant<int, 0>()) : cache == WWWS_CACHE_INT8 ? dim(bf, integral_constant<int, 1>()) : dim(bf, integral_constant<int, 2>());
     };
