@@ -138,7 +138,7 @@ typedef struct {
     uint32_t dim, n_axes, interleaved; /* n_axes 1 .. 8 */
 } wwws_rotation;
 
-/* Norm and turn queries and keys of n_tokens tokens (any number): q and q_out [n_tokens][n_heads][head_dim], k and k_out
+/* Norm and turn queries and keys of n_tokens tokens (< 2^31): q and q_out [n_tokens][n_heads][head_dim], k and k_out
  * [n_tokens][n_kv_heads][head_dim] of the backend's dtype, 16-byte aligned, strides in elements (multiples of 8); an output
  * may be its input with the same stride, and overlaps nothing otherwise.  positions: DEVICE [n_tokens][n_axes]. */
 wwws_status wwws_rotate(wwws_backend* b, const wwws_rotation* rotation, uint32_t n_tokens, const int32_t* positions,

@@ -144,6 +144,7 @@ class Backend:
         self._batches, self._shapings = ("batch", self.device, max_pages), ("shaping", self.device)
         self._layers, self._rotations = ("list of caches", *self._caches[1:]), ("rotation", self.device, head_dim)
         self._h = None
+        self._like, self._beam_bytes = {}, {}
         nbytes = C.c_uint64()
         self._check(self._lib.wwws_backend_workspace_bytes(C.byref(cfg), C.byref(nbytes)))
         with torch.cuda.device(self.device):
@@ -187,7 +188,13 @@ class Backend:
 
     def _empty(self, shape, dtype, aside):
         if not aside:
-            return self._torch.empty(shape, dtype=dtype, device=self.device)
+            # a new tensor like one that is kept costs half of one made from a shape, a type and a device; what is kept is one element, expanded
+            like = self._like.get((shape, dtype))
+            if like is None:
+                if len(self._like) >= 256:
+                    self._like.clear()
+                like = self._like[shape, dtype] = self._torch.empty(1, dtype=dtype, device=self.device).expand(shape)
+            return self._torch.empty_like(like)
         with self._torch.cuda.stream(self._stream):
             t = self._torch.empty(shape, dtype=dtype, device=self.device)
         t.record_stream(self._torch.cuda.current_stream(self.device))
@@ -205,11 +212,12 @@ class Backend:
 
     def _rows(self, t, heads, name):
         """[tokens, heads, head_dim] with packed heads; any stride between tokens."""
-        if t.dtype != self.dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.device != self.device:
-            raise ValueError(f"{name}: expected {self.dtype} [tokens, {heads}, {self.head_dim}] on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        if t.stride(2) != 1 or t.stride(1) != self.head_dim:
-            raise ValueError(f"{name}: the heads of a token must be packed, got strides {t.stride()}")
-        return t.stride(0) if t.shape[0] > 1 else heads * self.head_dim
+        shape, stride = t.shape, t.stride()
+        if t.dtype != self.dtype or len(shape) != 3 or shape[1] != heads or shape[2] != self.head_dim or t.device != self.device:
+            raise ValueError(f"{name}: expected {self.dtype} [tokens, {heads}, {self.head_dim}] on {self.device}, got {t.dtype} {tuple(shape)} on {t.device}")
+        if stride[2] != 1 or stride[1] != self.head_dim:
+            raise ValueError(f"{name}: the heads of a token must be packed, got strides {stride}")
+        return stride[0] if shape[0] > 1 else heads * self.head_dim
 
     # ---- records ----------------------------------------------------------------------------
     def new_cache(self):
@@ -460,16 +468,21 @@ class Backend:
             raise ValueError(f"beams must divide the {rows} rows, got {beams}")
         if keep < 1:
             raise ValueError(f"keep must be 1 or more, got {keep}")
-        nbytes = C.c_uint64()
-        self._check_plain(self._lib.wwws_beams_scratch_bytes(rows, vocab, dtype, keep, C.byref(nbytes)))
+        nbytes = self._beam_bytes.get((rows, vocab, dtype, keep))
+        if nbytes is None:
+            asked = C.c_uint64()
+            self._check_plain(self._lib.wwws_beams_scratch_bytes(rows, vocab, dtype, keep, C.byref(asked)))
+            if len(self._beam_bytes) >= 256:
+                self._beam_bytes.clear()
+            nbytes = self._beam_bytes[rows, vocab, dtype, keep] = asked.value
         aside = self._aside()
-        scratch = self._empty((nbytes.value,), self._torch.uint8, aside)
+        scratch = self._empty((nbytes,), self._torch.uint8, aside)
         shape = (rows // beams, keep)
         score, parent, token = self._empty(shape, self._torch.float32, aside), self._empty(shape, self._torch.int32, aside), self._empty(shape, self._torch.int32, aside)
         if aside:
             self._used(logits, totals)
         self._check(self._lib.wwws_select_beams(self._h, rows, beams, vocab, dtype, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, totals.data_ptr(), keep, scratch.data_ptr(),
-                                                nbytes.value, score.data_ptr(), parent.data_ptr(), token.data_ptr()))
+                                                nbytes, score.data_ptr(), parent.data_ptr(), token.data_ptr()))
         return score, parent, token
 
     def shape_logits(self, logits, shaping, out=None, tokens=True):

@@ -340,6 +340,7 @@ wwws_status wwws_rotate(wwws_backend* b, const wwws_rotation* rotation, uint32_t
     const wwws_backend_config& c = b->cfg;
     if (c.n_heads == 0) return fail(b, WWWS_ERR_ARG, "the backend was created without heads");
     if (const char* m = check_rotation(b, rotation)) return fail(b, WWWS_ERR_ARG, m);
+    if (n_tokens >= (1u << 31)) return fail(b, WWWS_ERR_ARG, "n_tokens must be < 2^31");
     if (n_tokens == 0) return WWWS_OK;
     if (!positions) return fail(b, WWWS_ERR_ARG, "positions is NULL");
     for (const char* m : { check_rows(q, q_stride, c.n_heads, c.head_dim), check_rows(k, k_stride, c.n_kv_heads, c.head_dim), check_rows(q_out, q_out_stride, c.n_heads, c.head_dim),
