@@ -427,11 +427,11 @@ class Backend:
         below 0) and pages for room[i] tokens.  refs int32 [n_pages] counts who holds a page (0: free), page_table int32 [old, max_pages] and
         held int32 [old] are what the old sequences hold; all of them end.  Returns (refs, page_table, held, moves) of the new ones; moves
         int32 [new, 3] is for `copy_pages`.  in_place: the counts are written over refs."""
-        i32 = self._torch.int32
+        i32, device = self._torch.int32, self.device
         n, m = self._array(source, i32, "source").shape[0], self._array(held, i32, "held").shape[0]
         for t, name, shape in ((refs, "refs", (self.n_pages,)), (page_table, "page_table", (m, self.max_pages)), (keep, "keep", (n,)), (room, "room", (n,))):
-            if tuple(self._array(t, i32, name, len(shape)).shape) != shape:
-                raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+            if t.shape != shape or t.dtype != i32 or t.device != device or not t.is_contiguous():
+                raise ValueError(f"{name}: expected a contiguous int32 tensor {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         aside = self._aside()
         refs_out = refs if in_place else self._empty((self.n_pages,), i32, aside)
         table_out, held_out, moves = self._empty((n, self.max_pages), i32, aside), self._empty((n,), i32, aside), self._empty((n, 3), i32, aside)

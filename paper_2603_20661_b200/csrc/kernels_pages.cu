@@ -28,42 +28,41 @@ __global__ void __launch_bounds__(kForkThreads) k_fork(ForkArgs a)
     const uint32_t page_mask = (1u << a.page_shift) - 1;
     __shared__ uint32_t prefix[kMaxNew + 1];             // fresh pages of all earlier sequences
     __shared__ uint32_t warp_sum[kForkWarps], free_of[8];
-
-    // What new sequence i is: its source (-1: none), whole pages, tokens in the page behind them, pages.  A bad one is empty.
-    struct New { int source; uint32_t full, cut, held; };
-    auto new_of = [&](uint32_t i, bool tell) {
-        New n{ __ldg(a.source + i), 0, 0, 0 };
-        const int keep = n.source < 0 ? 0 : __ldg(a.keep + i), room = __ldg(a.room + i);
-        bool ok = n.source < int(a.n_old) && keep >= 0 && room >= 0;
-        if (ok && n.source >= 0) {
-            const int held = __ldg(a.held + n.source);
-            ok = held >= 0 && uint32_t(held) <= a.max_pages && uint32_t(keep) <= uint32_t(held) << a.page_shift;
-        }
-        if (ok) {
-            n.full = uint32_t(keep) >> a.page_shift; n.cut = uint32_t(keep) & page_mask;
-            n.held = (uint32_t(max(room, keep)) + page_mask) >> a.page_shift;
-            ok = n.held <= a.max_pages;
-        }
-        if (!ok) { if (tell) report(a.err, beOffset); n = New{ -1, 0, 0, 0 }; }
-        return n;
-    };
+    // What each new sequence is, of the rows that are this block's throughout: its source (-1: none), whole pages, tokens in the page behind them and that page, pages.
+    struct New { int source; uint32_t full, cut, held, end; };
+    __shared__ New rows[kMaxNew / 8];                    // (8 blocks from 65 rows on)
+    const uint32_t most = a.n_old > a.n_new ? a.n_old : a.n_new, per_block = (most + blocks - 1) / blocks, row0 = rank * per_block, row1 = min(most, row0 + per_block);
     auto page_at = [&](uint32_t i, uint32_t k) { return uint32_t(__ldg(a.table + uint64_t(i) * a.max_pages + k)); };
 
-    // 1: refs as they are; the words in which the first claimant of a page is found
+    // 1: refs as they are; the new sequences, a bad one empty; the words in which the first claimant of a page is found
+    for (uint32_t i = row0 + tid; i < row1; i += kForkThreads) {
+        New n{ -1, 0, 0, 0, 0 };
+        if (i < a.n_new) {
+            n.source = __ldg(a.source + i);
+            const int given = __ldg(a.keep + i), keep = n.source < 0 ? 0 : given, room = __ldg(a.room + i);
+            bool ok = n.source < int(a.n_old) && keep >= 0 && room >= 0;
+            if (ok && n.source >= 0) {
+                const int held = __ldg(a.held + n.source);
+                ok = held >= 0 && uint32_t(held) <= a.max_pages && uint32_t(keep) <= uint32_t(held) << a.page_shift;
+            }
+            if (ok) {
+                n.full = uint32_t(keep) >> a.page_shift; n.cut = uint32_t(keep) & page_mask;
+                n.held = (uint32_t(max(room, keep)) + page_mask) >> a.page_shift;
+                ok = n.held <= a.max_pages;
+            }
+            if (!ok) { report(a.err, beOffset); n = New{ -1, 0, 0, 0, 0 }; }
+            a.held_out[i] = int(n.held);
+            if (n.cut) { n.end = page_at(uint32_t(n.source), n.full); if (n.end < a.n_pages) a.owner[n.end] = ~0u; }
+        }
+        rows[i - row0] = n;
+    }
     if (a.refs_out != a.refs)
         for (uint32_t p = thread; p < a.n_pages; p += threads) a.refs_out[p] = __ldg(a.refs + p);
-    for (uint32_t i = thread; i < a.n_new; i += threads) {
-        const New n = new_of(i, true);
-        a.held_out[i] = int(n.held);
-        if (n.cut) { const uint32_t p = page_at(uint32_t(n.source), n.full); if (p < a.n_pages) a.owner[p] = ~0u; }
-    }
     cluster.sync();
 
     // 2: old sequences let go, new ones take whole pages.  A sequence that continues itself keeps its pages without either.
-    const uint32_t most = a.n_old > a.n_new ? a.n_old : a.n_new;
-    for (uint32_t i = wid; i < most; i += warps) {
-        New n{ -1, 0, 0, 0 };
-        if (i < a.n_new) n = new_of(i, false);
+    for (uint32_t i = row0 + warp; i < row1; i += kForkWarps) {
+        const New n = rows[i - row0];
         int held = 0;
         if (i < a.n_old) {
             held = __ldg(a.held + i);
@@ -83,27 +82,23 @@ __global__ void __launch_bounds__(kForkThreads) k_fork(ForkArgs a)
                     else if (!same) atomicAdd(a.refs_out + p, 1);
                     to[k] = int(p);
                 } else if (k >= n.held) to[k] = 0;
-                else if (k == n.full && n.cut) {
-                    const uint32_t p = page_at(uint32_t(n.source), k);
-                    if (p < a.n_pages) atomicMin(a.owner + p, i);
-                }
             }
+            if (lane == 0 && n.cut && n.end < a.n_pages) atomicMin(a.owner + n.end, i);
         }
     }
     cluster.sync();
 
     // 3: who keeps the page it ends inside.  Only a page's first claimant writes its refs, and only the others could see that.
-    for (uint32_t i = thread; i < a.n_new; i += threads) {
-        const New n = new_of(i, false);
+    for (uint32_t i = row0 + tid; i < row1 && i < a.n_new; i += kForkThreads) {
+        const New n = rows[i - row0];
         int3 move = make_int3(-1, -1, 0);
         uint32_t need = n.held - n.full;
         if (n.cut) {
-            const uint32_t p = page_at(uint32_t(n.source), n.full);
-            if (p >= a.n_pages) { a.table_out[uint64_t(i) * a.max_pages + n.full] = int(p); --need; }        // nothing to keep or to copy: it stays outside the pool
-            else if (__ldcg(a.owner + p) == i && __ldcg(a.refs_out + p) == 0) {
-                a.refs_out[p] = 1;
-                a.table_out[uint64_t(i) * a.max_pages + n.full] = int(p); --need;
-            } else move = make_int3(int(p), -1, int(n.cut));
+            if (n.end >= a.n_pages) { a.table_out[uint64_t(i) * a.max_pages + n.full] = int(n.end); --need; }      // nothing to keep or to copy: it stays outside the pool
+            else if (__ldcg(a.owner + n.end) == i && __ldcg(a.refs_out + n.end) == 0) {
+                a.refs_out[n.end] = 1;
+                a.table_out[uint64_t(i) * a.max_pages + n.full] = int(n.end); --need;
+            } else move = make_int3(int(n.end), -1, int(n.cut));
         }
         a.moves[3 * i] = move.x; a.moves[3 * i + 1] = move.y; a.moves[3 * i + 2] = move.z;
         a.need[i] = need;
@@ -269,7 +264,7 @@ cudaError_t launch_fork(const ForkArgs& a, cudaStream_t s)
     // A block per 16 rows (a warp each) or 4,096 pages of the pool, 8 at most.
     const uint32_t rows = a.n_old > a.n_new ? a.n_old : a.n_new;
     uint32_t blocks = 1;
-    while (blocks < 8 && (blocks * kForkWarps < rows || blocks * 4096 < a.n_pages)) blocks *= 2;
+    while (blocks < 8 && (blocks * kForkWarps < rows || blocks * 4096 < a.n_pages)) blocks *= 2;        // (8 from 65 rows on, so that a block's rows fit its shared memory)
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(blocks); c.blockDim = dim3(kForkThreads); c.stream = s;
     cudaLaunchAttribute attr{};
