@@ -212,7 +212,7 @@ wwws_status attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages
     if (tree) {
         // All of a call's sequences go to one kernel: to the row kernel where the longest has few rows (the same figures), and where the tiles of
         // the longest sequences that the bounds allow could pass 31 bits.
-        const uint64_t tiles = uint64_t(kTreeSeqs) * ((uint64_t(batch->max_kv_len) + 127) / 128 + 1) * ((most + 63) / 64) * b->cfg.n_kv_heads;
+        const uint64_t tiles = uint64_t(kTreeSeqs) * ((uint64_t(batch->max_kv_len) + 127) / 128 + 4) * ((most + 63) / 64) * b->cfg.n_kv_heads;
         if (most <= a.few_rows || tiles >= (1ull << 31)) {
             a.few_rows = ~0u;
             return launched(b, launch_attend_rows_tree(a, uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend_tree");

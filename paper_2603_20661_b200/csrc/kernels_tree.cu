@@ -43,7 +43,8 @@ template <bool BF, int CACHE, int D, bool kTwo> struct Cfg {
     static constexpr int kOffScales = kOffStaging + kStaging * kCodes;
     static constexpr int kOffMl = kOffScales + (kQuant ? 2 * 4 * kBN * 4 : 0);           // [2 halves][128] sums
     static constexpr int kOffTops = kOffMl + (kTwo ? 0 : 2 * kBM * 4);                  // [2 tiles][2 halves][128] maxima
-    static constexpr int kOffBars = kOffTops + (kTwo ? 0 : 2 * 2 * kBM * 4);            // the sequences' running sum lies behind
+    static constexpr int kOffRel = kOffTops + (kTwo ? 0 : 2 * 2 * kBM * 4);             // [8 warps][64] value scales relative to the largest
+    static constexpr int kOffBars = kOffRel + (kQuant ? 8 * 64 * 4 : 0);                // the sequences' running sum lies behind
     static constexpr int kOffPrefix = kOffBars + 384;
     static constexpr int kFixed = kOffPrefix + 1024;                        // the rings start at a 1,024-byte boundary
     static constexpr int kConvert = kQuant ? 4 : 1;                         // warps that widen codes, or look through 16-bit values
@@ -55,7 +56,12 @@ template <bool BF, int CACHE, int D, bool kTwo> struct Cfg {
     static constexpr uint32_t kColS = 0, kColO = 256, kColP = 64, kCols = 512;          // P over the upper half of S
 };
 
+// The largest of three (NaN only if all are).
+__device__ __forceinline__ float max3(float a, float b, float c) { float d; asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// A unit counts kUnitCost tiles more than it has: what bringing its queries and storing its result costs, in tiles.
+constexpr uint32_t kUnitCost = 3;
 
 // What a call's sequences and a block's share of them come to.
 struct Plan {
@@ -87,21 +93,26 @@ __device__ __forceinline__ void span(const AttendArgs& a, int q_len, int kv, int
     tiles = max(1, n_sink + all - lo_tile);                  // one (empty) tile even where nothing is seen: the rows get zeros
 }
 
-// The segment that begins at position x.
-__device__ __forceinline__ Seg segment(const AttendArgs& a, const Plan& p, uint32_t x)
+// The segment that begins at position x or, where a unit's last tile lies before it, the next one; x becomes the position behind it.  False: the share has no more.
+__device__ __forceinline__ bool segment(const AttendArgs& a, const Plan& p, uint32_t& x, Seg& s)
 {
-    Seg s;
-    const uint32_t hkv = a.p.n_kv_heads, per_head = x / hkv;
-    uint32_t i = 0, hi = a.b.n_seqs;
-    while (hi - i > 1) { const uint32_t mid = (i + hi) >> 1; if (p.prefix[mid] <= per_head) i = mid; else hi = mid; }
-    s.seq = i; s.x0 = x;
-    s.q0 = __ldg(a.b.q_start + i); s.q_len = __ldg(a.b.q_start + i + 1) - s.q0; s.kv = __ldg(a.b.kv_len + i); s.place0 = s.kv - s.q_len;
-    span(a, s.q_len, s.kv, s.lo, s.lo_tile, s.n_sink, s.tiles);
-    const uint32_t rel = x - p.prefix[i] * hkv, unit = rel / uint32_t(s.tiles);
-    s.t0 = int(rel - unit * uint32_t(s.tiles));
-    s.t1 = int(min(uint32_t(s.tiles), uint32_t(s.t0) + (p.end - x)));
-    s.h = int(unit % hkv); s.tok0 = int(unit / hkv) * p.step;
-    return s;
+    const uint32_t hkv = a.p.n_kv_heads;
+    while (x < p.end) {
+        const uint32_t per_head = x / hkv;
+        uint32_t i = 0, hi = a.b.n_seqs;
+        while (hi - i > 1) { const uint32_t mid = (i + hi) >> 1; if (p.prefix[mid] <= per_head) i = mid; else hi = mid; }
+        s.seq = i;
+        s.q0 = __ldg(a.b.q_start + i); s.q_len = __ldg(a.b.q_start + i + 1) - s.q0; s.kv = __ldg(a.b.kv_len + i); s.place0 = s.kv - s.q_len;
+        span(a, s.q_len, s.kv, s.lo, s.lo_tile, s.n_sink, s.tiles);
+        const uint32_t each = uint32_t(s.tiles) + kUnitCost, rel = x - p.prefix[i] * hkv, unit = rel / each, t0 = rel - unit * each;
+        if (t0 >= uint32_t(s.tiles)) { x += each - t0; continue; }
+        s.x0 = x; s.t0 = int(t0);
+        s.t1 = int(min(uint32_t(s.tiles), t0 + (p.end - x)));
+        s.h = int(unit % hkv); s.tok0 = int(unit / hkv) * p.step;
+        x += uint32_t(s.t1) - t0;
+        return true;
+    }
+    return false;
 }
 
 // The power of two that brings the largest of a row of bf16 into [2^14, 2^15); returns its inverse.  (A row of zeros, subnormals or with a NaN or an infinity stays.)
@@ -158,7 +169,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         uint32_t v = 0;
         if (b0 + tid < a.b.n_seqs) {
             int q0, q_len, kv, lo, lt, ns, tiles;
-            if (sequence(a.b, b0 + tid, q0, q_len, kv, a.err) && q_len) { span(a, q_len, kv, lo, lt, ns, tiles); v = uint32_t((q_len + plan.step - 1) / plan.step) * uint32_t(tiles); }
+            if (sequence(a.b, b0 + tid, q0, q_len, kv, a.err) && q_len) { span(a, q_len, kv, lo, lt, ns, tiles); v = uint32_t((q_len + plan.step - 1) / plan.step) * (uint32_t(tiles) + kUnitCost); }
         }
         uint32_t inc = v;
 #pragma unroll
@@ -198,9 +209,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         const int n_box = kBN / int(page_tokens) * kBoxSlabs;
         uint32_t it = 0, staged = 0, k_sent = 0, v_sent = 0;        // tiles before the segment; copies so far
         bool ok = true;
-        for (uint32_t x = plan.begin; ok && x < plan.end;) {
-            const Seg g = segment(a, plan, x);
-            x += uint32_t(g.t1 - g.t0);
+        uint32_t x = plan.begin;
+        for (Seg g; ok && segment(a, plan, x, g);) {
             // keys of a tile, then the values of the one before: the next scores do not wait for a place among the values
             int row = 0;
             for (int t = g.t0; ok && t <= g.t1; ++t) {
@@ -256,10 +266,9 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         uint32_t it = 0, seg = 0, jobs_of[2] = { 0, 0 }, both_of[2] = { 0, 0 };     // tiles before the segment; segments; jobs of each pipeline and of each S (the parities of p_full and p_both)
         bool ok = true;
         auto commit = [&](uint32_t bar) { tc_commit_one(one, bar); };
-        for (uint32_t x = plan.begin; ok && x < plan.end; ++seg) {
-            const Seg g = segment(a, plan, x);
+        uint32_t x = plan.begin;
+        for (Seg g; ok && segment(a, plan, x, g); ++seg) {
             const uint32_t n = uint32_t(g.t1 - g.t0);
-            x += n;
             const int jobs = int(n) * (kTwo ? 2 : 1);
             // job k: tile k or k / 2 of the segment, row tile 0 or k % 2
             auto scores = [&](int k) {
@@ -316,9 +325,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 next_scale[0] = __ldg(a.p.k_scale + cell); next_scale[1] = __ldg(a.p.v_scale + cell);
             }
         };
-        for (uint32_t x = plan.begin; ok && x < plan.end;) {
-            const Seg g = segment(a, plan, x);
-            x += uint32_t(g.t1 - g.t0);
+        uint32_t x = plan.begin;
+        for (Seg g; ok && segment(a, plan, x, g);) {
             const int32_t* table = a.b.page_table + uint64_t(g.seq) * a.b.table_stride;
             auto page_of = [&](int key) { return uint32_t(__ldg(table + (uint32_t(key) >> a.p.page_shift))); };
             if constexpr (kQuant) {
@@ -445,11 +453,12 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             bar_arrive(q_full);
             return f;
         };
-        if (plan.begin < plan.end) f = bring(segment(a, plan, plan.begin));
-        for (uint32_t x = plan.begin; ok && x < plan.end; ++seg) {
-            const Seg g = segment(a, plan, x);
+        uint32_t x = plan.begin;
+        Seg g;
+        bool more = segment(a, plan, x, g);
+        if (more) f = bring(g);
+        for (; ok && more; ++seg) {
             const int n = g.t1 - g.t0;
-            x += uint32_t(n);
             float f_after = f;
             const int rt = kTwo ? w : 0;                           // row tile of this pipeline
             const int tok = token_of(g);
@@ -519,7 +528,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     if (!falling) {
                         float t0 = top, t1 = -INFINITY;
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) { t0 = fmaxf(t0, __uint_as_float(v[e])); t1 = fmaxf(t1, __uint_as_float(v[e + 1])); }
+                        for (int e = 0; e < 32; e += 4) { t0 = max3(t0, __uint_as_float(v[e]), __uint_as_float(v[e + 1])); t1 = max3(t1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])); }
                         top = fmaxf(t0, t1);
                     } else {
 #pragma unroll
@@ -574,6 +583,14 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                         }
                     }
                 }
+                // (by every thread for itself they cost 32 multiplications a tile)
+                [[maybe_unused]] float* rel = reinterpret_cast<float*>(smem + C::kOffRel) + (kQuant ? warp * 64 : 0);
+                if constexpr (kQuant) {
+                    const float2 v2 = *reinterpret_cast<const float2*>(vs + lane * 2);
+                    __syncwarp();
+                    *reinterpret_cast<float2*>(rel + lane * 2) = make_float2(v2.x * unit_inv, v2.y * unit_inv);
+                    __syncwarp();
+                }
                 const uint64_t f2 = pack2(f, f), m2 = pack2(C::kRaise - m, C::kRaise - m);
                 uint64_t sum_a = pack2(0.0f, 0.0f), sum_b = sum_a;
                 auto weights = [&](const uint32_t* v, int c0) {
@@ -586,8 +603,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                         const uint64_t y = pack2(y0, y1);
                         if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
                         if constexpr (kQuant) {
-                            const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(vs + c0 + e / 4 * 4);
-                            unpack2(mul2(mul2(y, pack2(unit_inv, unit_inv)), e % 4 ? v4.y : v4.x), y0, y1);
+                            const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(rel + c0 + e / 4 * 4);
+                            unpack2(mul2(y, e % 4 ? v4.y : v4.x), y0, y1);
                             if constexpr (kMasked) { y0 = v[e] == kHidden ? 0.0f : y0; y1 = v[e + 1] == kHidden ? 0.0f : y1; }      // a hidden value's scale may be NaN
                         }
                         p[e / 2] = W::pack(y0, y1);
@@ -644,7 +661,9 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 ll = w ? other + l : l + other;
             }
             // the next segment's queries: its first scores are on their way while this one's result is written
-            if (x < plan.end) f_after = bring(segment(a, plan, x));
+            Seg after;
+            more = segment(a, plan, x, after);
+            if (more) f_after = bring(after);
             const uint32_t tO = tmem + C::kColO + (joined ? 0 : w) * D + lanes;
             const int c_from = joined ? w * (D / 2) : 0, c_to = joined ? c_from + D / 2 : D;
             const bool whole = g.t0 == 0 && g.t1 == g.tiles;
@@ -744,6 +763,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 }
             }
             f = f_after;
+            g = after;
         }
     }
 #undef WAIT
