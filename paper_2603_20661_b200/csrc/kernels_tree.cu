@@ -14,7 +14,7 @@
 //     sequences; cut units are joined by the last of their blocks, in block order.  Every role works out its segments by itself.
 //   - m is allowed to lag behind the true maximum by a factor (2^8, 2^1 over quantised caches), so that O is rescaled in the first few tiles only.
 //   - Quantised caches: codes land in a staging ring, four warps widen them into the operands' layout, to f16 whatever the backend (exactly, and for e4m3 by the
-//     hardware: widening to bf16 took three times the instructions and the whole call 168 us instead of @@); scales multiply the scores (keys) and the weights (values) in fp32.
+//     hardware: widening to bf16 took three times the instructions); scales multiply the scores (keys) and the weights (values) in fp32.
 //     bf16 queries become f16 by a power of two per row (exact down to 2^-28 of the row's largest); weights are kept relative to the largest value scale of the segment so far.
 //   - Pages that no row sees are read from page 0 and their values put to zero before they are used, as is everything else of a tile that no row sees.
 #include <cuda.h>
@@ -359,7 +359,6 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                         uint4 codes[kChunks];
 #pragma unroll
                         for (int e = 0; e < kChunks; ++e) codes[e] = *reinterpret_cast<const uint4*>(from + t / 32 * 32 * D + (e * 32 + lane) * 16);
-                        bar_arrive(st_empty(ss));
 #pragma unroll
                         for (int e = 0; e < kChunks; ++e) {
                             const int c = lane % kChunks, r = t / 32 * 32 + e * (32 / kChunks) + lane / kChunks;
@@ -374,6 +373,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                         }
                         reinterpret_cast<float*>(smem + C::kOffScales)[(kv * 4 + item % 4) * kBN + t] = scale[kv];
                         fence_async_proxy();
+                        bar_arrive(st_empty(ss));                   // (not before the codes have been used: right behind their loads, the next copy overtook some of those)
                         bar_arrive(kv ? v_full(s) : k_full(s));
                     }
                 }

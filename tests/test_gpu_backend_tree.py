@@ -117,6 +117,18 @@ def test_long_contexts_split_over_blocks(lens, cache, window):
     check(Case(lens, kv_heads=2, group=4, dim=128, page=64, dtype=BF16, cache=cache, seed=4), masks(lens, 4), window, 5)
 
 
+@pytest.mark.parametrize("cache", ["16", "int8", "e4m3"])
+@pytest.mark.parametrize("tokens", [30, 61])
+def test_shares_of_a_few_tiles(cache, tokens):
+    """Contexts so short that a block gets two or three tiles: each meets its rings, barriers and clock rates cold, and fresh backends meet cold caches as well."""
+    lens = [(tokens, 3000)]
+    for rep in range(4):
+        case = Case(lens, kv_heads=2, group=4, dim=128, page=64, dtype=BF16, cache=cache, seed=13 + rep)
+        bits = masks(lens, 13 + rep)
+        for _ in range(3):
+            check(case, bits)
+
+
 @pytest.mark.parametrize("cache", ["16", "e4m3"])
 @pytest.mark.parametrize("lens", [FEW, LONG], ids=["few", "long"])
 def test_a_chain_is_attention_without_a_tree(cache, lens):
