@@ -12,10 +12,11 @@
 //   - One warp issues the matrix instructions in the order PV(n), S(n + 2), n counting the S; one issues the copies of pages, into rings of their own for keys and values.
 //   - Work is cut by key tiles: all (unit, tile) pairs laid end to end, an equal share for each of 148 blocks, found from a running sum over the
 //     sequences; cut units are joined by the last of their blocks, in block order.  Every role works out its segments by itself.
-//   - m is allowed to lag behind the true maximum by a factor (2^8, 2^1 over quantised caches), so that O is rescaled in the first few tiles only.
+//   - m is allowed to lag behind the true maximum by a factor (2^8, 2^4 over quantised caches), so that O is rescaled in the first few tiles only.
 //   - Quantised caches: codes land in a staging ring, four warps widen them into the operands' layout, to f16 whatever the backend (exactly, and for e4m3 by the
 //     hardware: widening to bf16 took three times the instructions); scales multiply the scores (keys) and the weights (values) in fp32.
-//     bf16 queries become f16 by a power of two per row (exact down to 2^-28 of the row's largest); weights are kept relative to the largest value scale of the segment so far.
+//     bf16 queries become f16 by a power of two per row (exact down to 2^-28 of the row's largest); weights are kept relative to twice the largest value scale of
+//     the segment when that last grew beyond it.
 //   - Pages that no row sees are read from page 0 and their values put to zero before they are used, as is everything else of a tile that no row sees.
 #include <cuda.h>
 
@@ -51,14 +52,45 @@ template <bool BF, int CACHE, int D, bool kTwo> struct Cfg {
     static constexpr int kWarpConvert = 8, kWarpMma = kWarpConvert + kConvert, kWarpLoad = kWarpMma + 1, kThreads = (kWarpLoad + 1) * 32;
     static constexpr bool kB = BF && !kQuant;                               // the operands' type
     // How far (log2) m may lag behind, and the factor that weights in f16 and their sums carry: 2^15 at most together.  Over a quantised cache bf16 backends are
-    // held to bf16's range, so the factor is the larger part there: what is lost is 2^-38 of the row's largest weight (2^-31 failed columns of faint weights alone).
-    static constexpr float kLag = kQuant ? 1.0f : 8.0f, kRaise = kQuant ? 14.0f : kB ? 0.0f : 7.0f;
-    static constexpr uint32_t kColS = 0, kColO = 256, kColP = 64, kCols = 512;          // P over the upper half of S
+    // held to bf16's range, so the factor is the larger part there: what is lost is 2^-34 of the row's largest weight and the largest scale (2^-31 failed columns of faint
+    // weights alone; a lag of 2^1 would lose 2^-38 and took 24 x 21 over e4m3 from 100 to 103 us).
+    static constexpr float kLag = kQuant ? 4.0f : 8.0f, kRaise = kQuant ? 11.0f : kB ? 0.0f : 7.0f;
+    static constexpr uint32_t kColS = 0, kColO = 256, kColP = 64, kCols = 512;
+    // P's step e of 16 keys: over the upper half of S or, where two threads have a row, each over the first half of its own columns.
+    static __device__ constexpr uint32_t col_p(int e) { return kTwo ? kColP + e * 8 : e / 4 * 64 + e % 4 * 8; }
 };
 
 // The largest of three (NaN only if all are).
 __device__ __forceinline__ float max3(float a, float b, float c) { float d; asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// 2^y of two numbers on the units that add and multiply (the one for 2^y takes eight clocks a warp): y = n + f, |f| <= 1/2, 2^f by the polynomial of degree 5 whose
+// largest relative error is least, 2^-23.7, and 2^-22.8 with the coefficients in fp32.  For y < 128; below -126 it is 2^-126.  A NaN stays one.
+__device__ __forceinline__ uint64_t ex2_both(uint64_t y)
+{
+    float y0, y1;
+    unpack2(y, y0, y1);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(y0) : "f"(-126.0f)); asm("max.NaN.f32 %0, %0, %1;" : "+f"(y1) : "f"(-126.0f));
+    y = pack2(y0, y1);
+    constexpr float kRound = 12582912.0f + 127.0f;             // 1.5 2^23, and the exponent's bias: the sum's low bits are 2^n's exponent
+    const uint64_t j = add2(y, pack2(kRound, kRound)), f = fma2(add2(j, pack2(-kRound, -kRound)), pack2(-1.0f, -1.0f), y);
+    auto both = [](float c) { return pack2(c, c); };
+    uint64_t r = both(0.0013248048f);
+    r = fma2(r, f, both(0.009675051f)); r = fma2(r, f, both(0.055507995f)); r = fma2(r, f, both(0.24022135f)); r = fma2(r, f, both(0.69314694f)); r = fma2(r, f, both(1.0000001f));
+    float j0, j1;
+    unpack2(j, j0, j1);
+    return mul2(r, pack2(__uint_as_float(__float_as_uint(j0) << 23), __uint_as_float(__float_as_uint(j1) << 23)));
+}
+
+// Four codes to f16, exactly: e4m3 by the hardware; int8 with its sign turned is the low byte of 1,024 + 128 + code.
+template <int CACHE> __device__ __forceinline__ void widen4(uint32_t four, uint32_t& lo, uint32_t& hi)
+{
+    if constexpr (CACHE == WWWS_CACHE_INT8) {
+        four ^= 0x80808080u;
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(__byte_perm(four, 0x64646464u, 0x4140)), "r"(0x64806480u));
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(__byte_perm(four, 0x64646464u, 0x4342)), "r"(0x64806480u));
+    } else { lo = widen<false, CACHE>(four & 0xffffu); hi = widen<false, CACHE>(four >> 16); }
+}
 
 // A unit counts kUnitCost tiles more than it has: what bringing its queries and storing its result costs, in tiles.
 constexpr uint32_t kUnitCost = 3;
@@ -155,7 +187,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
     const uint32_t meeting = q_full + 56, o_done = q_full + 64;
     auto p_both = [&](uint32_t b) { return q_full + 72 + 8 * b; };
     auto pair = [&](int q) { return q_full + 88 + 8 * q; };          // the two warps that share 32 rows
-    static_assert(8 * (kMore + 15) <= 384, "barriers fit");
+    auto p_half = [&](int w) { return q_full + 120 + 8 * w; };       // the weights of columns 64 to 127 are there
+    static_assert(8 * (kMore + 17) <= 384, "barriers fit");
     uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + C::kOffPrefix);
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
@@ -190,7 +223,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         for (int s = 0; s < C::kV; ++s) { bar_init(v_full(s), kQuant ? C::kConvert * 32 : 1); bar_init(v_empty(s), 1); if (!kQuant) bar_init(v_ready(s), 1); }
         for (int s = 0; s < C::kStaging; ++s) { bar_init(st_full(s), 1); bar_init(st_empty(s), C::kConvert * 32); }
         bar_init(q_full, 256); bar_init(done, 1); bar_init(drained, 1); bar_init(meeting, 256); bar_init(o_done, 1);
-        for (int w = 0; w < 2; ++w) { bar_init(s_full(w), 1); bar_init(p_full(w), 128); bar_init(p_both(w), 256); }
+        for (int w = 0; w < 2; ++w) { bar_init(s_full(w), 1); bar_init(p_full(w), 128); bar_init(p_both(w), 256); bar_init(p_half(w), 128); }
         for (int q = 0; q < 4; ++q) bar_init(pair(q), 64);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -263,7 +296,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         // ---- matrix instructions ----
         constexpr uint32_t kDescS = mma_desc(C::kB, false, kBN), kDescO = mma_desc(C::kB, true, D);
         const uint32_t one = elect_one();
-        uint32_t it = 0, seg = 0, jobs_of[2] = { 0, 0 }, both_of[2] = { 0, 0 };     // tiles before the segment; segments; jobs of each pipeline and of each S (the parities of p_full and p_both)
+        uint32_t it = 0, seg = 0, jobs_of[2] = { 0, 0 };            // tiles before the segment; segments; jobs of each pipeline or S
         bool ok = true;
         auto commit = [&](uint32_t bar) { tc_commit_one(one, bar); };
         uint32_t x = plan.begin;
@@ -290,12 +323,19 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 const int w = k & 1;
                 const uint32_t item = it + uint32_t(kTwo ? k >> 1 : k), s = item % C::kV;
                 if (!kTwo || w == 0) { if (!(ok = WAIT(kQuant ? v_full(s) : v_ready(s), (item / C::kV) & 1))) break; }
-                if (!(ok = WAIT(kTwo ? p_full(w) : p_both(w), (kTwo ? jobs_of[w] : both_of[w]) & 1))) break;
-                ++(kTwo ? jobs_of[w] : both_of[w]);
-                tc_after();
                 const uint64_t vb = smem_desc(base + C::kOffV + s * C::kTile, kBN * 128, 1024);
+                auto product = [&](int e, bool more) { mma_ts(one, tmem + C::kColO + (kTwo ? w : 0) * D, tmem + C::kColS + w * 128 + C::col_p(e), vb + e * 2048 / 16, kDescO, more); };
+                if constexpr (kTwo) {                               // the second half's weights come first: its product runs while the first's are worked out
+                    if (!(ok = WAIT(p_half(w), jobs_of[w] & 1))) break;
+                    tc_after();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) mma_ts(one, tmem + C::kColO + (kTwo ? w : 0) * D, tmem + C::kColS + w * 128 + C::kColP + e * 8, vb + e * 2048 / 16, kDescO, k >= (kTwo ? 2 : 1) || e > 0);
+                    for (int e = 4; e < 8; ++e) product(e, k >= 2 || e > 4);
+                }
+                if (!(ok = WAIT(kTwo ? p_full(w) : p_both(w), jobs_of[w] & 1))) break;
+                ++jobs_of[w];
+                tc_after();
+#pragma unroll
+                for (int e = 0; e < (kTwo ? 4 : 8); ++e) product(e, kTwo || k > 0 || e > 0);
                 if (!kTwo) commit(o_done);
                 if (!kTwo || w == 1) commit(v_empty(s));
                 if (k + 2 < jobs) scores(k + 2);
@@ -364,8 +404,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                             const int c = lane % kChunks, r = t / 32 * 32 + e * (32 / kChunks) + lane / kChunks;
                             uint4 v = codes[e];
                             if (!(on >> (r & 31) & 1)) v = make_uint4(0, 0, 0, 0);
-                            const uint4 lo = make_uint4(widen<false, CACHE>(v.x & 0xffffu), widen<false, CACHE>(v.x >> 16), widen<false, CACHE>(v.y & 0xffffu), widen<false, CACHE>(v.y >> 16));
-                            const uint4 hi = make_uint4(widen<false, CACHE>(v.z & 0xffffu), widen<false, CACHE>(v.z >> 16), widen<false, CACHE>(v.w & 0xffffu), widen<false, CACHE>(v.w >> 16));
+                            uint4 lo, hi;
+                            widen4<CACHE>(v.x, lo.x, lo.y); widen4<CACHE>(v.y, lo.z, lo.w); widen4<CACHE>(v.z, hi.x, hi.y); widen4<CACHE>(v.w, hi.z, hi.w);
                             uint8_t* row = to + c / 4 * (kBN * 128) + r * 128;
                             const int p0 = ((2 * (c % 4)) ^ (r & 7)) * 16, p1 = ((2 * (c % 4) + 1) ^ (r & 7)) * 16;
                             if (c < 4) { *reinterpret_cast<uint4*>(row + p0) = lo; *reinterpret_cast<uint4*>(row + p1) = hi; }
@@ -475,7 +515,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             }
             const int depth_place = a.window && row_on ? g.place0 + tree_depth(a.tree, a.tree_words, tree_row, tok) : 0;      // where the window counts from
             const int32_t* table = a.b.page_table + uint64_t(g.seq) * a.b.table_stride;
-            float m = kLow, l = 0.0f, unit = 0.0f, unit_inv = 0.0f; // unit: the largest value scale of the segment's tiles so far, what O is relative to
+            float m = kLow, l = 0.0f, unit = 0.0f, unit_inv = 0.0f; // unit: what the values' scales and so O are relative to, at least the largest of the segment's tiles so far
             bool bad_met = false;
                                 auto visible = [&](int first) {        // the columns of keys [first, first + 32) that the row sees, a bit each
                                     const int rel = first - g.place0;
@@ -500,7 +540,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
             auto weigh = [&](auto masked_one, int key0, uint32_t item, uint32_t buffer, int tile) {
                 constexpr bool kMasked = decltype(masked_one)::value, kHalf = !kTwo;
                 const int cb = kHalf ? w * 64 : 0;
-                const uint32_t tS = tmem + C::kColS + buffer * 128 + cb + lanes, tP = tmem + C::kColS + buffer * 128 + C::kColP + cb / 2 + lanes;
+                const uint32_t tS = tmem + C::kColS + buffer * 128 + cb + lanes, tP = tmem + C::kColS + buffer * 128 + (kHalf ? cb : int(C::kColP)) + lanes;
                 const uint32_t tO = tmem + C::kColO + w * (kHalf ? D / 2 : D) + lanes;
                 const float* ks = reinterpret_cast<const float*>(smem + C::kOffScales) + item % 4 * kBN + cb;
                 [[maybe_unused]] const float* vs = ks + 4 * kBN;
@@ -522,7 +562,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                         for (int e = 0; e < 32; ++e) v[e] = bits & (1u << e) ? v[e] : kHidden;
                     }
                 };
-                uint32_t v0[32], v1[32];
+                uint32_t v0[32];
+                [[maybe_unused]] uint32_t v1[32];
                 float top = falling ? INFINITY : -INFINITY;
                 auto widest = [&](const uint32_t* v) {
                     if (!falling) {
@@ -536,10 +577,19 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     }
                 };
                 __syncwarp();
-                tm_ld32(tS, v0); tm_ld32(tS + 32, v1);
-                tm_wait_ld32(v0); tie32(v1);
-                fetch(v0, 0); widest(v0);
-                fetch(v1, 32); widest(v1);
+                if constexpr (kQuant) {                             // (the upper columns are read again: there are no registers to hold them, and spilling them cost more)
+                    tm_ld32(tS + 32, v0);
+                    tm_wait_ld32(v0);
+                    fetch(v0, 32); widest(v0);
+                    tm_ld32(tS, v0);
+                    tm_wait_ld32(v0);
+                    fetch(v0, 0); widest(v0);
+                } else {
+                    tm_ld32(tS, v0); tm_ld32(tS + 32, v1);
+                    tm_wait_ld32(v0); tie32(v1);
+                    fetch(v0, 0); widest(v0);
+                    fetch(v1, 32); widest(v1);
+                }
                 if constexpr (!kHalf) {
                     __syncwarp();
                     tm_ld32(tS + 64, v0); tm_ld32(tS + 96, v1);
@@ -568,7 +618,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     const float mn = fmaxf(m, top);
                     float less = ex2(m - mn);
                     l *= less; m = mn;
-                    if (kQuant && largest > unit) { less *= __fdiv_rn(unit, largest); unit = largest; unit_inv = __fdiv_rn(1.0f, largest); }
+                    if (kQuant && largest > unit) { largest *= 2.0f; less *= __fdiv_rn(unit, largest); unit = largest; unit_inv = __fdiv_rn(1.0f, largest); }
                     if (tile > 0) {
                         // one S and O: the products into it were issued before these scores; two S and an O: the last product may be under way
                         if constexpr (kHalf) { if (!(ok = WAIT(o_done, (products + uint32_t(tile) - 1) & 1))) return; tc_after(); }
@@ -598,9 +648,11 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
                         float y0, y1;
-                        unpack2(fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, m2), y0, y1);
-                        y0 = ex2(y0); y1 = ex2(y1);
-                        const uint64_t y = pack2(y0, y1);
+                        uint64_t y = fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, m2);
+                        // every fourth pair by a polynomial (12 x 61 tokens behind 16,001: 212 -> 207 us, every second one 214; quantised caches have no registers left for it).
+                        // It needs weights of 2^-126 at least, so tiles with hidden columns go without, and rows that are none may come out as they like.
+                        if (kTwo && !kMasked && e % 8 == 6) { y = ex2_both(y); unpack2(y, y0, y1); }
+                        else { unpack2(y, y0, y1); y0 = ex2(y0); y1 = ex2(y1); y = pack2(y0, y1); }
                         if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
                         if constexpr (kQuant) {
                             const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(rel + c0 + e / 4 * 4);
@@ -613,11 +665,19 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 };
                 if constexpr (kHalf) {
                     weights(v0, 0);
-                    weights(v1, 32);
+                    if constexpr (kQuant) {
+                        tm_ld32(tS + 32, v0);
+                        tm_wait_ld32(v0);
+                        fetch(v0, 32); weights(v0, 32);
+                    } else weights(v1, 32);
                 } else {
                     weights(v0, 64);
                     tm_ld32(tS, v0);                                // read again: registers for one half only
                     weights(v1, 96);
+                    tm_wait_st();
+                    __syncwarp();
+                    tc_before();
+                    bar_arrive(p_half(w));
                     tm_ld32(tS + 32, v1);
                     tm_wait_ld32(v0); tie32(v1);
                     fetch(v0, 0); weights(v0, 0);
@@ -641,7 +701,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     using std::bool_constant;
                     if (masked) weigh(bool_constant<true>(), key0, item, buffer, tile); else weigh(bool_constant<false>(), key0, item, buffer, tile);
                     if (!ok) break;
-                }
+                } else if (kTwo) bar_arrive(p_half(w));
                 __syncwarp();
                 tc_before();
                 bar_arrive(kTwo ? p_full(w) : p_both(buffer));
