@@ -244,6 +244,13 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         bool ok = true;
         uint32_t x = plan.begin;
         for (Seg g; ok && segment(a, plan, x, g);) {
+            // the unit's queries and masks will be read by others in some tiles' time
+            for (int r = lane; r < C::kQTiles * kBM; r += 32)
+                if (const int tok = g.tok0 + r / int(G); r < plan.step * int(G) && tok < g.q_len) {
+                    const uint8_t* q = a.q + (uint64_t(g.q0 + tok) * a.q_stride + (uint64_t(g.h) * G + r % int(G)) * D) * 2;
+                    for (int e = 0; e < D * 2; e += 128) asm volatile("prefetch.global.L1 [%0];" :: "l"(q + e));
+                    if (r % int(G) == 0) asm volatile("prefetch.global.L1 [%0];" :: "l"(a.tree + uint64_t(uint32_t(g.q0 + tok)) * a.tree_words));
+                }
             // keys of a tile, then the values of the one before: the next scores do not wait for a place among the values
             int row = 0;
             for (int t = g.t0; ok && t <= g.t1; ++t) {
@@ -499,7 +506,6 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
         if (more) f = bring(g);
         for (; ok && more; ++seg) {
             const int n = g.t1 - g.t0;
-            float f_after = f;
             const int rt = kTwo ? w : 0;                           // row tile of this pipeline
             const int tok = token_of(g);
             const bool row_on = on_of(g);
@@ -720,10 +726,10 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 const float other = reinterpret_cast<const float*>(smem + C::kOffMl)[(w ^ 1) * kBM + r];
                 ll = w ? other + l : l + other;
             }
-            // the next segment's queries: its first scores are on their way while this one's result is written
+            // the next segment's queries: its first scores are on their way while this one's result is written (before the last product was awaited it took no less)
             Seg after;
             more = segment(a, plan, x, after);
-            if (more) f_after = bring(after);
+            if (more) f = bring(after);
             const uint32_t tO = tmem + C::kColO + (joined ? 0 : w) * D + lanes;
             const int c_from = joined ? w * (D / 2) : 0, c_to = joined ? c_from + D / 2 : D;
             const bool whole = g.t0 == 0 && g.t1 == g.tiles;
@@ -784,7 +790,6 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 // the unit's blocks are consecutive; the last to arrive joins their parts in that order
                 const uint32_t u0 = g.x0 - uint32_t(g.t0), u1 = u0 + uint32_t(g.tiles);
                 const uint32_t blk0 = u0 / plan.share, blk1 = (u1 - 1) / plan.share, first_slot = 2 * blk0 + (u0 % plan.share ? 1 : 0);
-                __threadfence();
                 if (!meet()) break;
                 if (tid == 0) { __threadfence(); words[2] = atomicAdd(&a.s.ticket[first_slot], 1u) == blk1 - blk0; }
                 __syncwarp();
@@ -822,7 +827,6 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     if (tid == 0) a.s.ticket[first_slot] = 0;
                 }
             }
-            f = f_after;
             g = after;
         }
     }
