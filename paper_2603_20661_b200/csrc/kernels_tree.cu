@@ -17,6 +17,8 @@
 //     hardware: widening to bf16 took three times the instructions); scales multiply the scores (keys) and the weights (values) in fp32.
 //     bf16 queries become f16 by a power of two per row (exact down to 2^-28 of the row's largest); weights are kept relative to twice the largest value scale of
 //     the segment when that last grew beyond it.
+//   - Measured: 12 x 61 tokens behind 16,001 of 16 bits, 32 on 8 heads of 128: 205 us, 3,900 GB/s, bound by the chain scores - weights - product of a row tile (for seconds 250 us,
+//     at the power cap); 24 x 21 behind 3,001 on average in e4m3: 98 us, bound by widening, scales and exponentials (behind 16,000: 305 us, 2,700 GB/s).
 //   - Pages that no row sees are read from page 0 and their values put to zero before they are used, as is everything else of a tile that no row sees.
 #include <cuda.h>
 
@@ -65,12 +67,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) { float d; asm(
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // 2^y of two numbers on the units that add and multiply (the one for 2^y takes eight clocks a warp): y = n + f, |f| <= 1/2, 2^f by the polynomial of degree 5 whose
-// largest relative error is least, 2^-23.7, and 2^-22.8 with the coefficients in fp32.  For y < 128; below -126 it is 2^-126.  A NaN stays one.
+// largest relative error is least, 2^-23.7, and 2^-22.8 with the coefficients in fp32.  For y < 127; what is below 2^-126.5 is 0 (an exponent field of 0).  A NaN stays one.
 __device__ __forceinline__ uint64_t ex2_both(uint64_t y)
 {
     float y0, y1;
     unpack2(y, y0, y1);
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(y0) : "f"(-126.0f)); asm("max.NaN.f32 %0, %0, %1;" : "+f"(y1) : "f"(-126.0f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(y0) : "f"(-127.0f)); asm("max.NaN.f32 %0, %0, %1;" : "+f"(y1) : "f"(-127.0f));
     y = pack2(y0, y1);
     constexpr float kRound = 12582912.0f + 127.0f;             // 1.5 2^23, and the exponent's bias: the sum's low bits are 2^n's exponent
     const uint64_t j = add2(y, pack2(kRound, kRound)), f = fma2(add2(j, pack2(-kRound, -kRound)), pack2(-1.0f, -1.0f), y);
@@ -624,7 +626,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     const float mn = fmaxf(m, top);
                     float less = ex2(m - mn);
                     l *= less; m = mn;
-                    if (kQuant && largest > unit) { largest *= 2.0f; less *= __fdiv_rn(unit, largest); unit = largest; unit_inv = __fdiv_rn(1.0f, largest); }
+                    if (kQuant && largest > unit) { largest *= largest < 0x1p126f ? 2.0f : 1.0f; less *= __fdiv_rn(unit, largest); unit = largest; unit_inv = __fdiv_rn(1.0f, largest); }
                     if (tile > 0) {
                         // one S and O: the products into it were issued before these scores; two S and an O: the last product may be under way
                         if constexpr (kHalf) { if (!(ok = WAIT(o_done, (products + uint32_t(tile) - 1) & 1))) return; tc_after(); }
@@ -655,9 +657,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                     for (int e = 0; e < 32; e += 2) {
                         float y0, y1;
                         uint64_t y = fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, m2);
-                        // every fourth pair by a polynomial (12 x 61 tokens behind 16,001: 212 -> 207 us, every second one 214; quantised caches have no registers left for it).
-                        // It needs weights of 2^-126 at least, so tiles with hidden columns go without, and rows that are none may come out as they like.
-                        if (kTwo && !kMasked && e % 8 == 6) { y = ex2_both(y); unpack2(y, y0, y1); }
+                        // every fourth pair by a polynomial (12 x 61 tokens behind 16,001: 212 -> 207 us, every second one 214; quantised caches have no registers left for it)
+                        if (kTwo && e % 8 == 6) { y = ex2_both(y); unpack2(y, y0, y1); }
                         else { unpack2(y, y0, y1); y0 = ex2(y0); y1 = ex2(y1); y = pack2(y0, y1); }
                         if (e % 4) sum_b = add2(sum_b, y); else sum_a = add2(sum_a, y);
                         if constexpr (kQuant) {

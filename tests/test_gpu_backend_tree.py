@@ -130,6 +130,12 @@ def test_shares_of_a_few_tiles(cache, tokens):
 
 
 @pytest.mark.parametrize("cache", ["16", "e4m3"])
+def test_more_sequences_than_a_launch_takes(cache):
+    lens = [(1 + 7 * k % 23, 23 + 11 * k % 90) for k in range(275)] + [(0, 40), (23, 23), (2, 130)]
+    check(Case(lens, kv_heads=1, group=4, dim=64, page=16, dtype=F16, cache=cache, seed=6), masks(lens, 6))
+
+
+@pytest.mark.parametrize("cache", ["16", "e4m3"])
 @pytest.mark.parametrize("lens", [FEW, LONG], ids=["few", "long"])
 def test_a_chain_is_attention_without_a_tree(cache, lens):
     """The masks of a chain hide what causal order hides."""
