@@ -119,7 +119,9 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
  * come before their children, and a new token sees the context and, of the new tokens j up to itself, those whose bit is set in
  * its row of `tree` (DEVICE [n_tokens][tree_words], 32 places a word, lowest bit first; tree_words * 32 >= max_q_len):
  * its ancestors and itself, as a rule.  It stands d places behind the context, d being how many new tokens it sees but itself
- * (none if it sees none); the window is counted from there and hides context alone. */
+ * (none if it sees none); the window is counted from there and hides context alone.  Where the longest sequence has more than 32 rows
+ * per kv head (48 over a quantised cache) the call is launched 256 sequences at a time, and over a quantised cache a weight below 2^-34 of its
+ * row's largest may be lost. */
 wwws_status wwws_attend_tree(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
                              uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window,
                              uint32_t sinks, const uint32_t* tree, uint32_t tree_words);
