@@ -431,11 +431,11 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 for (int tile = g.t0; ok && tile < g.t1; ++tile, ++it) {
                     const int key0 = g.key_of(tile);
                     // ---- 16-bit values: those that no row of the unit sees become zeros (a weight of 0 does not silence a NaN), and so do, where some rows see them
-                    // and others do not, those that are no numbers: they are added to the rows that see them at the segment's end ----
+                    // and others do not (mixed tiles alone), those that are no numbers: they are added to the rows that see them at the segment's end ----
                     const uint32_t s = it % C::kV;
                     if (!(ok = WAIT(v_full(s), (it / C::kV) & 1))) break;
-                    const bool bad = *static_cast<volatile uint32_t*>(words + 3) & 1;
-                    if (bad || g.mixed(a, key0)) {
+                    const bool bad = *static_cast<volatile uint32_t*>(words + 3) & 1, mixed = g.mixed(a, key0);
+                    if (bad || mixed) {
 #pragma unroll 1
                         for (int r = t; r < kBN; r += 32) {
                             const int key = key0 + r;
@@ -443,7 +443,7 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                             uint8_t* row = smem + C::kOffV + s * C::kTile + r * 128;
                             auto piece = [&](int e) { return reinterpret_cast<uint4*>(row + e / 8 * (kBN * 128) + ((e ^ r) & 7) * 16); };     // (neighbours meet no bank twice)
                             uint32_t top = 0;
-                            if (seen) {
+                            if (seen && mixed) {
 #pragma unroll
                                 for (int e = 0; e < 8 * C::kSlabs; ++e) largest_halves(top, *piece(e));
                             }
