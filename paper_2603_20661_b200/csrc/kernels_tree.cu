@@ -488,6 +488,8 @@ k_tree(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_con
                 if constexpr (kQuant && BF) {
                     float mul;
                     f *= lifted(q, mul);
+                    // an infinity at a hidden key times f has to stay one (f rounded to 0 made NaN rows of faint queries at scales near 0); sums are below 2^128, so x moves by 2^-21 at most
+                    if (f == 0.0f) f = copysignf(0x1p-149f, a.scale_log2);
 #pragma unroll
                     for (int e = 0; e < D / 8; ++e)
                         q[e] = make_uint4(W::pack(A::lo(q[e].x) * mul, A::hi(q[e].x) * mul), W::pack(A::lo(q[e].y) * mul, A::hi(q[e].y) * mul),
