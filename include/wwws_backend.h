@@ -111,7 +111,8 @@ wwws_status wwws_cache_read(wwws_backend* b, const wwws_batch* batch, const wwws
  * no numbers, which wwws_cache_append never writes, excepted); a visible one that is infinite or not a number does (a
  * value: in its own column).  Results do not depend on what else is in the batch's pages, and repeat bit for bit.
  * Where a sequence may have more than 32 new rows per kv head (48 over a quantised cache; a row is a new token and one of
- * its query heads), the call is launched 32 sequences at a time. */
+ * its query heads), a kernel for many rows takes all of the call's sequences, 32 a launch: single tokens are answered sooner in a call of their own
+ * than beside prompts. */
 wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
                         uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window, uint32_t sinks);
 

@@ -338,7 +338,8 @@ class Backend:
         return k, v
 
     def attend(self, cache, batch, q, out=None, scale=None, window=0, sinks=0, tree=None):
-        """Attention of the new tokens ([n_tokens, n_heads, head_dim]) over the cache; scale defaults to head_dim ** -0.5.
+        """Attention of the new tokens ([n_tokens, n_heads, head_dim]) over the cache; scale defaults to head_dim ** -0.5.  (Single tokens and
+        prompts may share a call, but calls of their own take less time.)
         tree: int32 [n_tokens, words], the new tokens are drafts behind the context and see those whose bits are set in their row (their
         ancestors and themselves); 32 places a word, lowest bit first."""
         self._fits(cache, self._caches)

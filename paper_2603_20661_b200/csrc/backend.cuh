@@ -25,8 +25,8 @@ struct Pages {
     uint32_t n_pages, n_kv_heads, page_shift;
 };
 
-// Partial attention results (running maximum, sum and weighted values of a row) of the blocks that share a unit; the row kernel and the
-// tile kernel use the same memory, one after the other.
+// Partial attention results (running maximum, sum and weighted values of a row) of the blocks that share a unit; all of the
+// kernels use the same memory, one call after the other.
 struct AttendScratch {
     float* part_o;       // [slots][rows][head_dim]
     float2* part_ml;     // [slots][rows]
@@ -40,7 +40,6 @@ struct AttendArgs {
     float scale_log2;    // softmax scale * log2(e)
     uint32_t window, sinks;
     uint32_t pad;        // row kernel: 0, or the tiles that every unit counts (see kernels_attend.cu)
-    uint32_t few_rows;   // sequences with at most this many rows per kv head (new tokens * group) go to the row kernel, others to the tile kernel
     uint32_t* err;
     const uint32_t* tree; uint32_t tree_words;      // bits of the new tokens that each new token sees (see wwws_attend_tree); not read by the kernels without trees
 };
@@ -93,7 +92,7 @@ struct ShapeArgs {
 
 constexpr uint32_t kDecodeSlots = 2 * 148 * 3;      // partial results of the row kernel: two per block of its largest grid
 constexpr uint32_t kDecodeRows = 16;                 // most rows of its units
-constexpr uint32_t kFewRows = 32, kFewRowsQuant = 48;     // most rows per kv head of a sequence that goes to it (see wwws_attend)
+constexpr uint32_t kFewRows = 32, kFewRowsQuant = 48;     // most rows per kv head (new tokens * group) of the sequences of a call that goes to it (see wwws_attend)
 constexpr uint32_t kTileBlocks = 148, kTileSlots = 2 * kTileBlocks;   // blocks of the tile kernel: one per SM
 
 constexpr uint32_t kTileSeqs = 32;                    // sequences of a launch of the tile kernel, at most (see wwws_attend)

@@ -202,21 +202,18 @@ wwws_status attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages
     a.sinks = sinks < batch->max_kv_len ? sinks : batch->max_kv_len;
     a.err = b->err;
     a.tree = tree; a.tree_words = tree_words;
-    // Sequences go by their rows per kv head (new tokens * group): few to the row kernel, which reads the cache once per 16 rows, more to the tile
-    // kernel.  24 requests of 3,000 tokens, row kernel / tile kernel in us: 16-bit cache at head_dim 64, 30 rows 36 / 42, 36 rows 46 / 42, at 128 58 / 54 and
+    // A call goes by the rows per kv head (new tokens * group) of its longest sequence: few to the row kernel, which reads the cache once per 16 rows, more to
+    // the tile kernel.  24 requests of 3,000 tokens, row kernel / tile kernel in us: 16-bit cache at head_dim 64, 30 rows 36 / 42, 36 rows 46 / 42, at 128 58 / 54 and
     // 73 / 53; e4m3 at 64, 48 rows 48 / 56, 60 rows 62 / 56, at 128 61 / 77 and 79 / 79; int8 at 64 50 / 60 and 65 / 62, at 128 66 / 91 and 87 / 91.  (One request of
-    // 60,000 tokens would favour the row kernel beyond these: 60 rows at 128 84 / 92 in 16 bits, 70 / 95 in e4m3.)  Both run only where the host's
-    // counts allow both kinds; the short sequences are then taken to have one new token.
-    a.few_rows = b->cfg.cache == WWWS_CACHE_16 ? kFewRows : kFewRowsQuant;
+    // 60,000 tokens would favour the row kernel beyond these: 60 rows at 128 84 / 92 in 16 bits, 70 / 95 in e4m3.)
+    const uint32_t few_rows = b->cfg.cache == WWWS_CACHE_16 ? kFewRows : kFewRowsQuant;
     const uint64_t most = uint64_t(batch->max_q_len) * a.group;
     if (tree) {
-        // All of a call's sequences go to one kernel: to the row kernel where the longest has few rows (the same figures), and where the tiles of
+        // The same with the tree kernel for the tile kernel (the figures are that one's; the tree kernel has not been held against the row kernel), and where the tiles of
         // the longest sequences that the bounds allow could pass 31 bits.
         const uint64_t tiles = uint64_t(kTreeSeqs) * ((uint64_t(batch->max_kv_len) + 127) / 128 + 4) * ((most + 63) / 64) * b->cfg.n_kv_heads;
-        if (most <= a.few_rows || tiles >= (1ull << 31)) {
-            a.few_rows = ~0u;
+        if (most <= few_rows || tiles >= (1ull << 31))
             return launched(b, launch_attend_rows_tree(a, uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend_tree");
-        }
         cudaError_t e = cudaSuccess;
         for (uint32_t first = 0; e == cudaSuccess && first < batch->n_seqs; first += kTreeSeqs) {
             a.b.q_start = batch->q_start + first; a.b.kv_len = batch->kv_len + first; a.b.page_table = batch->page_table + uint64_t(first) * b->cfg.max_pages;
@@ -226,18 +223,17 @@ wwws_status attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages
         }
         return launched(b, e, "wwws_attend_tree");
     }
-    const bool many = most > a.few_rows;
-    const bool few = !many || uint64_t(batch->n_tokens) != uint64_t(batch->n_seqs) * batch->max_q_len;
-    // Where the tile kernel takes part, 32 sequences at a time.  One launch of it over 129 short and long ones, with the row kernel behind it, ended in a fault
-    // of the GPU that neither reading nor checks of every access in memory explained; launches of up to 32 have been run in every mixture.
-    const uint32_t at_once = many && batch->n_seqs > kTileSeqs ? kTileSeqs : batch->n_seqs;
+    if (most <= few_rows) return launched(b, launch_attend_rows(a, uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend");
+    // Short sequences beside long ones stay with the tile kernel.  They went to the row kernel in a second launch, and two such pairs of launches ended in a fault of
+    // the GPU (129 sequences of both kinds, and a form of the tile kernel with masks over 22) that neither reading nor checks of every access in memory explained.
+    // So a call has one kernel for all its sequences, none of which it leaves out.  32 a launch is what the tile kernel has been run with in every mixture; whether the
+    // number matters is not known.  (63 single tokens beside a chunk of 512, 32 on 8 heads of 128: 160 us, over 8-bit caches 295 to 311; in calls of their own 86 + 43, 63 to 65 + 66 to 68.)
     cudaError_t e = cudaSuccess;
-    for (uint32_t first = 0; e == cudaSuccess && first < batch->n_seqs; first += at_once) {
+    for (uint32_t first = 0; e == cudaSuccess && first < batch->n_seqs; first += kTileSeqs) {
         a.b.q_start = batch->q_start + first; a.b.kv_len = batch->kv_len + first; a.b.page_table = batch->page_table + uint64_t(first) * b->cfg.max_pages;
-        a.b.n_seqs = batch->n_seqs - first < at_once ? batch->n_seqs - first : at_once;
+        a.b.n_seqs = batch->n_seqs - first < kTileSeqs ? batch->n_seqs - first : kTileSeqs;
         a.b.ends = (first == 0 ? 1u : 0u) | (first + a.b.n_seqs == batch->n_seqs ? 2u : 0u);
-        if (many) e = launch_attend_tile(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
-        if (e == cudaSuccess && few) e = launch_attend_rows(a, many ? a.group : uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
+        e = launch_attend_tile(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
     }
     return launched(b, e, "wwws_attend");
 }

@@ -7,7 +7,7 @@
 // each costs.
 //   - Keys are the 16 rows of the operand, query rows its 8 columns (S^T = K Q^T, O^T = V^T P^T): no half-empty 16-row tile of queries, and
 //     kGroups = 1 or 2 groups of 8 rows share the fragments of a key.  (Up to 32 rows come here, 48 over a quantised cache, as units of 16, or of 8 where no
-//     sequence has more or a call mixes prompts with single tokens.  One unit of 32 took 82 us where two of 16 take 66, five drafted tokens of 24 requests,
+//     sequence has more.  One unit of 32 took 82 us where two of 16 take 66, five drafted tokens of 24 requests,
 //     since it has registers for no more than half the warps' work in flight.)
 //   - Work is cut by keys, not by sequences: all (sequence, row tile, kv head) units laid end to end in tiles of kTK keys, and block i takes
 //     the i-th equal share (the lengths are read on the device: no plan, no host copy of them).  A unit cut by a share boundary leaves a
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, Shape<CACHE, D, kGroups>::kBlocks) k
         unsigned long long x = 0;
         if (base + tid < a.b.n_seqs) {
             int q0, q_len, kv;
-            if (sequence(a.b, base + tid, q0, q_len, kv, a.err) && q_len && uint32_t(q_len) * G <= a.few_rows)
+            if (sequence(a.b, base + tid, q0, q_len, kv, a.err) && q_len)
                 x = (unsigned long long)((uint32_t(q_len) * G + kRows - 1) / kRows) * (a.pad ? a.pad : span_of<TK>(q_len, kv, a.window, a.sinks).tiles);
         }
         const unsigned long long own = x;

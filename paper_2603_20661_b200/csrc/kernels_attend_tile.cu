@@ -137,7 +137,7 @@ struct Walk {
 
     __device__ __forceinline__ bool load(const AttendArgs& a)
     {
-        return sequence(a.b, seq, q0, q_len, kv, a.err) && uint32_t(q_len) * a.group > a.few_rows;
+        return sequence(a.b, seq, q0, q_len, kv, a.err) && q_len;
     }
     __device__ __forceinline__ Seq as_seq(const Space& sp) const { return Seq{ q0, q_len, kv, kv - q_len, (q_len + sp.step - 1) / sp.step }; }
     __device__ __forceinline__ void span(const Space& sp) { sp.span(as_seq(sp), u, hi, lo, lo_tile, n_sink, tiles); }
