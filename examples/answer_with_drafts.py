@@ -103,12 +103,17 @@ class Answers:
 
     def with_drafts(self):
         """Greedy answers, several tokens a step where the drafts are right: (answers, steps)."""
-        torch, n = self.torch, len(self.prompts)
+        torch = self.torch
         lengths, texts, steps = self._prompts(self.prompts), [list(p) for p in self.prompts], 0
-        while min(len(t) - len(p) for t, p in zip(texts, self.prompts)) < self.most_new:
-            trees = [drafted_tree(t, self.drafts) for t in texts]
+        rows = list(range(len(texts)))                           # the request of each sequence; one that is answered leaves, and gives its pages back
+        while True:
+            source = [i for i, r in enumerate(rows) if len(texts[r]) - len(self.prompts[r]) < self.most_new]
+            if not source:
+                break
+            rows, lengths = [rows[i] for i in source], [lengths[i] for i in source]
+            trees = [drafted_tree(texts[r], self.drafts) for r in rows]
             new = [len(t) for t, _ in trees]
-            self.pages.go_on(range(n), lengths, [c + q for c, q in zip(lengths, new)])
+            self.pages.go_on(source, lengths, [c + q for c, q in zip(lengths, new)])
             batch, starts = self._batch(new, [c + q for c, q in zip(lengths, new)])
             masks, depth = np.zeros((starts[-1], -(-max(new) // 32)), np.uint32), np.zeros(starts[-1], np.int32)
             for i, (_, parents) in enumerate(trees):
@@ -127,7 +132,7 @@ class Answers:
                 while True:
                     want = best[starts[i] + path[-1]]
                     follow = [j for j in range(len(tokens)) if parents[j] == path[-1] and tokens[j] == want]
-                    texts[i].append(want)
+                    texts[rows[i]].append(want)
                     if not follow:
                         break
                     path.append(follow[0])
