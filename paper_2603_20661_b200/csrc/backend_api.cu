@@ -209,15 +209,16 @@ wwws_status attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages
     const uint32_t few_rows = b->cfg.cache == WWWS_CACHE_16 ? kFewRows : kFewRowsQuant;
     const uint64_t most = uint64_t(batch->max_q_len) * a.group;
     if (tree) {
-        // The same with the tree kernel for the tile kernel (the figures are that one's; the tree kernel has not been held against the row kernel), and where the tiles of
-        // the longest sequences that the bounds allow could pass 31 bits.
-        const uint64_t tiles = uint64_t(kTreeSeqs) * ((uint64_t(batch->max_kv_len) + 127) / 128 + 4) * ((most + 63) / 64) * b->cfg.n_kv_heads;
-        if (most <= few_rows || tiles >= (1ull << 31))
-            return launched(b, launch_attend_rows_tree(a, uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend_tree");
+        // The same with the tree kernel for the tile kernel (the figures are that one's; the tree kernel has not been held against the row kernel).  It counts tiles in
+        // 31 bits: a launch takes as many sequences as the bounds allow to fit, and what does not fit even alone goes to the row kernel.
+        const uint64_t tiles = ((uint64_t(batch->max_kv_len) + 127) / 128 + 4) * ((most + 63) / 64) * b->cfg.n_kv_heads;       // of a sequence, at most, with its units' fixed cost
+        const uint64_t fit = most <= few_rows ? 0 : ((1ull << 31) - 1) / tiles;
+        if (fit == 0) return launched(b, launch_attend_rows_tree(a, uint32_t(most), b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream), "wwws_attend_tree");
+        const uint32_t at_once = uint32_t(fit < kTreeSeqs ? fit : kTreeSeqs);
         cudaError_t e = cudaSuccess;
-        for (uint32_t first = 0; e == cudaSuccess && first < batch->n_seqs; first += kTreeSeqs) {
+        for (uint32_t first = 0; e == cudaSuccess && first < batch->n_seqs; first += at_once) {
             a.b.q_start = batch->q_start + first; a.b.kv_len = batch->kv_len + first; a.b.page_table = batch->page_table + uint64_t(first) * b->cfg.max_pages;
-            a.b.n_seqs = batch->n_seqs - first < kTreeSeqs ? batch->n_seqs - first : kTreeSeqs;
+            a.b.n_seqs = batch->n_seqs - first < at_once ? batch->n_seqs - first : at_once;
             a.b.ends = (first == 0 ? 1u : 0u) | (first + a.b.n_seqs == batch->n_seqs ? 2u : 0u);
             e = launch_tree(a, b->cfg.head_dim, b->cfg.dtype, b->cfg.cache, b->stream);
         }
