@@ -189,7 +189,7 @@ wwws_status wwws_cache_compact(wwws_backend* b, const wwws_batch* batch, const w
 /* The best `keep` (1 .. 128) continuations of each request: row r of logits (dtype as for wwws_shape_logits, stride in elements) is
  * beam r % beams of request r / beams, beams 1 .. 256; n_rows is a multiple of beams and <= max_rows; vocab <= 2^24.
  *   score(r, v) = total[r] + logits[r][v] - log sum_w exp(logits[r][w])
- * with the sum's terms in fp32 and the rest in 64 bits; largest first, ties to the lowest (row, token), within a row in the logits' order.
+ * with the sum's terms in fp32 and the rest in 64 bits; largest first, ties to the lowest (row, token).
  * score [requests][keep] is rounded to fp32, parent (the row) and token are int32; where a request has fewer continuations above
  * -infinity: -infinity, -1, -1.  A row whose total is -infinity, infinite or NaN, or that holds a NaN or +infinity, has none.
  * scratch: DEVICE, 16-byte aligned, of wwws_beams_scratch_bytes, free again when the stream has passed the call. */

@@ -203,24 +203,29 @@ template <int DT, bool kSkewed> __device__ __noinline__ void join_slowly(const B
     auto score = [&](uint32_t b, float x) { return score_of(a, s, seq, b, x); };
     // Too many at a bound: the best element of every chunk, then the best of these `keep` times over, its chunk looked through again for what comes behind it.
     unsigned long long* heads = a.heads + uint64_t(seq) * n;
-    auto head = [&](uint32_t i, unsigned long long last) {       // the largest key of chunk i below `last`, by a warp
+    auto head = [&](uint32_t i, unsigned long long last, uint32_t last_token) {       // the best element of chunk i behind (last, last_token), by a warp
         const uint32_t b = i / a.chunks, c = i - b * a.chunks;
         uint4 x[kVecs];
         Row<DT, kSkewed>(a, seq * a.beams + b).chunk(x, c, lane, a.vocab);
-        unsigned long long best = 0;
+        unsigned long long best = 0, key = 0;                    // (by score, not by logit: logits that differ may have equal scores beside a large total)
+        uint32_t best_token = ~0u;
 #pragma unroll
         for (int u = 0; u < kVecs; ++u)
 #pragma unroll
             for (int e = 0; e < E::kPer; ++e) {
                 const float v = E::at(x[u], e);
-                const unsigned long long k = v > -INFINITY ? key_of(v, c * E::kChunk + (u * 32 + lane) * E::kPer + e) : 0;
-                if (k < last && k > best) best = k;
+                const uint32_t token = c * E::kChunk + (u * 32 + lane) * E::kPer + e;
+                if (const unsigned long long y = score(b, v); y && before(last, last_token, y, token) && before(y, token, best, best_token)) { best = y; best_token = token; key = key_of(v, token); }
             }
 #pragma unroll
-        for (int k = 1; k < 32; k <<= 1) { const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, k); best = o > best ? o : best; }
-        if (lane == 0) heads[i] = best;
+        for (int k = 1; k < 32; k <<= 1) {
+            const unsigned long long z = __shfl_xor_sync(0xffffffffu, best, k), other = __shfl_xor_sync(0xffffffffu, key, k);
+            const uint32_t token = __shfl_xor_sync(0xffffffffu, best_token, k);
+            if (before(z, token, best, best_token)) { best = z; best_token = token; key = other; }
+        }
+        if (lane == 0) heads[i] = key;
     };
-    for (uint32_t i = warp; i < n; i += kWarps) head(i, ~0ull);
+    for (uint32_t i = warp; i < n; i += kWarps) head(i, ~0ull, 0);
     for (uint32_t r = 0; r < a.keep; ++r) {
         __syncthreads();                                                                         // (orders the block's writes to the heads too)
         unsigned long long best = 0, id = ~0ull;
@@ -234,9 +239,7 @@ template <int DT, bool kSkewed> __device__ __noinline__ void join_slowly(const B
         if (tid == 0) put(a, seq, r, w.y, w.id);
         if (w.y && warp == 0) {
             const uint32_t b = uint32_t(w.id >> 32), token = uint32_t(w.id), i = b * a.chunks + token / E::kChunk;
-            const unsigned long long k = __ldcg(heads + i);
-            __syncwarp();
-            head(i, k);
+            head(i, w.y, token);
         }
     }
 }
