@@ -110,6 +110,9 @@ wwws_status wwws_cache_read(wwws_backend* b, const wwws_batch* batch, const wwws
  * out of its subnormals.  A hidden key never reaches a row's result, whatever its key and value hold (e4m3 codes that are
  * no numbers, which wwws_cache_append never writes, excepted); a visible one that is infinite or not a number does (a
  * value: in its own column).  Results do not depend on what else is in the batch's pages, and repeat bit for bit.
+ * Over a quantised cache weights in f16 are kept relative to the value scales of a sequence's kv head, so what each key adds to a row,
+ * relative to its largest weight, may be off by 2^-35 of the largest value that any new token of the sequence sees there: a value 2^20 times the
+ * others takes precision from the rows that do not see it as well.  (bf16 backends: wwws_attend_tree, and few rows.)
  * Where a sequence may have more than 32 new rows per kv head (48 over a quantised cache; a row is a new token and one of
  * its query heads), a kernel for many rows takes all of the call's sequences, 32 a launch: single tokens are answered sooner in a call of their own
  * than beside prompts. */
@@ -121,8 +124,7 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
  * its row of `tree` (DEVICE [n_tokens][tree_words], 32 places a word, lowest bit first; tree_words * 32 >= max_q_len):
  * its ancestors and itself, as a rule.  It stands d places behind the context, d being how many new tokens it sees but itself
  * (none if it sees none); the window is counted from there and hides context alone.  Where the longest sequence has more than 32 rows
- * per kv head (48 over a quantised cache) the call is launched 256 sequences at a time, and over a quantised cache a weight below 2^-34 of its
- * row's largest may be lost. */
+ * per kv head (48 over a quantised cache) the call is launched up to 256 sequences at a time. */
 wwws_status wwws_attend_tree(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
                              uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window,
                              uint32_t sinks, const uint32_t* tree, uint32_t tree_words);

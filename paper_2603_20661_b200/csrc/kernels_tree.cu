@@ -54,8 +54,8 @@ template <bool BF, int CACHE, int D, bool kTwo> struct Cfg {
     static constexpr int kWarpConvert = 8, kWarpMma = kWarpConvert + kConvert, kWarpLoad = kWarpMma + 1, kThreads = (kWarpLoad + 1) * 32;
     static constexpr bool kB = BF && !kQuant;                               // the operands' type
     // How far (log2) m may lag behind, and the factor that weights in f16 and their sums carry: 2^15 at most together.  Over a quantised cache bf16 backends are
-    // held to bf16's range, so the factor is the larger part there: what is lost is 2^-34 of the row's largest weight and the largest scale (2^-31 failed columns of faint
-    // weights alone; a lag of 2^1 would lose 2^-38 and took 24 x 21 over e4m3 from 100 to 103 us).
+    // held to bf16's range, so the factor is the larger part there: what is lost is 2^-35 of the row's largest weight times the largest value of any key so far, whether the row sees it or
+    // not (a factor of 2^8 failed columns of faint weights alone; a lag of 2^1 would lose 2^-38 and took 24 x 21 over e4m3 from 100 to 103 us).
     static constexpr float kLag = kQuant ? 4.0f : 8.0f, kRaise = kQuant ? 11.0f : kB ? 0.0f : 7.0f;
     static constexpr uint32_t kColS = 0, kColO = 256, kColP = 64, kCols = 512;
     // P's step e of 16 keys: over the upper half of S or, where two threads have a row, each over the first half of its own columns.
