@@ -42,6 +42,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_append(SeqBatch b, Pages p, 
     __shared__ int32_t start[kMaxSeqs + 1];
     for (uint32_t i = threadIdx.x; i <= b.n_seqs; i += kThreads) start[i] = b.q_start[i];
     __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x == 0 && (start[0] != 0 || uint32_t(start[b.n_seqs]) != b.n_tokens)) report(err, beOffset);
     const uint32_t lane = threadIdx.x % 32, part = lane % L;
     const uint32_t rows = 2 * p.n_kv_heads;              // keys' heads, then values'
     const uint32_t warps = gridDim.x * (kThreads / 32);
@@ -51,7 +52,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_append(SeqBatch b, Pages p, 
         if (const uint32_t tok = run * kRun + lane; lane < kRun && tok < b.n_tokens) {
             const uint32_t i = find_seq(start, b.n_seqs, int(tok));
             const int q_len = start[i + 1] - start[i], kv = b.kv_len[i], pos = kv - q_len + int(tok) - start[i];
-            if (uint32_t(q_len) > b.max_q_len || uint32_t(kv) > b.max_kv_len || start[i] < 0 || start[i] > int(tok) || start[i + 1] <= int(tok)) report(err, beOffset);
+            if (uint32_t(q_len) > b.max_q_len || uint32_t(kv) > b.max_kv_len || start[i] < 0 || start[i] > int(tok) || start[i + 1] <= int(tok) || uint32_t(start[i + 1]) > b.n_tokens) report(err, beOffset);
             else if (pos >= 0) mine = cell_of(b, p, i, pos, err);
         }
         for (int t = 0; t < kRun; ++t) {

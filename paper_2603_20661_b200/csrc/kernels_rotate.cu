@@ -33,6 +33,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_rotate(RotateArgs g)
     if constexpr (kAppend) {
         for (uint32_t i = threadIdx.x; i <= g.b.n_seqs; i += kThreads) start[i] = g.b.q_start[i];
         __syncthreads();
+        if (blockIdx.x == 0 && threadIdx.x == 0 && (start[0] != 0 || uint32_t(start[g.b.n_seqs]) != g.n_tokens)) report(g.err, beOffset);
     }
     const uint32_t lane = threadIdx.x % 32, j = lane % L, sub = lane / L;
     const wwws_rotation& r = g.r;
@@ -62,7 +63,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_rotate(RotateArgs g)
             uint32_t i = 0, hi = g.b.n_seqs;
             while (hi - i > 1) { const uint32_t mid = (i + hi) >> 1; if (start[mid] <= int(tok)) i = mid; else hi = mid; }
             const int q_len = start[i + 1] - start[i], kv = __ldg(g.b.kv_len + i);
-            if (uint32_t(q_len) > g.b.max_q_len || uint32_t(kv) > g.b.max_kv_len || start[i] < 0 || start[i] > int(tok) || start[i + 1] <= int(tok)) { report(g.err, beOffset); continue; }
+            if (uint32_t(q_len) > g.b.max_q_len || uint32_t(kv) > g.b.max_kv_len || start[i] < 0 || start[i] > int(tok) || start[i + 1] <= int(tok) || uint32_t(start[i + 1]) > g.n_tokens) { report(g.err, beOffset); continue; }
             place = kv - q_len + int(tok) - start[i];
             if (place >= 0) {
                 const uint32_t page = uint32_t(__ldg(g.b.page_table + uint64_t(i) * g.b.table_stride + (uint32_t(place) >> g.p.page_shift)));
