@@ -166,7 +166,7 @@ wwws_status wwws_rotate_append(wwws_backend* b, const wwws_batch* batch, const w
  *   - The page that keep[i] ends inside will be written further: it stays with the first new sequence that ends inside it if nobody
  *     holds it otherwise; every other one gets a page of its own and a row of `moves`: from, to, tokens (else -1, -1, 0).
  *   - Fresh pages are the free ones of lowest number, in the order of (sequence, place).  Where the pool runs out a place gets
- *     -1, a page outside the pool, and the next wwws_backend_sync says WWWS_ERR_ALLOC.
+ *     -1, a page outside the pool, and the next wwws_backend_sync says WWWS_ERR_ALLOC.  Such places may be let go, not continued.
  * A bad new sequence is reported and left empty; entries behind a row's pages are 0.  refs_out may be refs; nothing else may overlap. */
 typedef struct {
     const int32_t* refs; int32_t* refs_out;                                          /* [n_pages] */

@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kForkThreads) k_fork(ForkArgs a)
         const bool same = n.source == int(i);
         for (uint32_t k = (same ? n.full : 0) + lane; k < uint32_t(held); k += 32) {
             const uint32_t p = page_at(i, k);
-            if (p < a.n_pages) atomicAdd(a.refs_out + p, -1); else report(a.err, bePage);
+            if (p < a.n_pages) atomicAdd(a.refs_out + p, -1); else if (p != ~0u) report(a.err, bePage);       // (-1: a place that an earlier call found no page for)
         }
         if (i < a.n_new) {
             int32_t* to = a.table_out + uint64_t(i) * a.max_pages;
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kForkThreads) k_fork(ForkArgs a)
         int3 move = make_int3(-1, -1, 0);
         uint32_t need = n.held - n.full;
         if (n.cut) {
-            if (n.end >= a.n_pages) { a.table_out[uint64_t(i) * a.max_pages + n.full] = int(n.end); --need; }      // nothing to keep or to copy: it stays outside the pool
+            if (n.end >= a.n_pages) { report(a.err, bePage); a.table_out[uint64_t(i) * a.max_pages + n.full] = int(n.end); --need; }      // nothing to keep or to copy: it stays outside the pool
             else if (__ldcg(a.owner + n.end) == i && __ldcg(a.refs_out + n.end) == 0) {
                 a.refs_out[n.end] = 1;
                 a.table_out[uint64_t(i) * a.max_pages + n.full] = int(n.end); --need;
