@@ -25,7 +25,8 @@
  * the stream given at creation and is asynchronous (wwws_backend_sync and wwws_destroy_backend synchronise it); the
  * library allocates no device memory (one workspace from the caller); "HOST" / "DEVICE" say where a pointer points;
  * a handle is not thread-safe and lives on the GPU that holds its workspace.  Arrays handed to a call must stay valid
- * until the stream has passed it, and must have been written by work that the stream waits for.
+ * until the stream has passed it, and must have been written by work that the stream waits for.  Calls captured into graphs use the
+ * handle's workspace when they are replayed: no two of them, nor one beside a call, at the same time.
  * Ids read from device memory (pages, tokens, masks, offsets) are range-checked by the kernels: a bad one is skipped
  * (a page outside the pool reads as hidden keys and is not written) and reported by the next wwws_backend_sync.
  */
@@ -122,8 +123,9 @@ wwws_status wwws_attend(wwws_backend* b, const wwws_batch* batch, const wwws_kv_
 /* The same for new tokens that are a tree of drafts behind the context, the kv_len[i] - q_len tokens before them: parents
  * come before their children, and a new token sees the context and, of the new tokens j up to itself, those whose bit is set in
  * its row of `tree` (DEVICE [n_tokens][tree_words], 32 places a word, lowest bit first; tree_words * 32 >= max_q_len):
- * its ancestors and itself, as a rule.  It stands d places behind the context, d being how many new tokens it sees but itself
- * (none if it sees none); the window is counted from there and hides context alone.  Where the longest sequence has more than 32 rows
+ * its ancestors and itself, as a rule.  It stands d places behind the context, d being one less than the new tokens that it sees
+ * (0 if it sees none); the window is counted from there and hides context alone: what `tree` shows stays visible however far above, so
+ * that a chain deeper than the window sees more than wwws_attend shows its tokens.  Where the longest sequence has more than 32 rows
  * per kv head (48 over a quantised cache) the call is launched up to 256 sequences at a time. */
 wwws_status wwws_attend_tree(wwws_backend* b, const wwws_batch* batch, const wwws_kv_pages* pages, const void* q,
                              uint64_t q_stride, void* out, uint64_t out_stride, float scale, uint32_t window,
@@ -133,7 +135,7 @@ wwws_status wwws_attend_tree(wwws_backend* b, const wwws_batch* batch, const www
  * is (i, dim / 2 + i), or (2 i, 2 i + 1) where interleaved is 1; the elements behind them stay where they are.  At position p
  * pair (a, b) becomes (a cos t - b sin t, b cos t + a sin t), t = 2 pi p turns[i] / 2^64; the product wraps around exactly, so
  * that no position is too far.  A weight makes x into x * weight / sqrt(mean(x^2) + eps) over the whole head before that.
- * In fp32, rounded once. */
+ * In fp32, rounded once; cosines and sines are within 2^-21 of theirs. */
 typedef struct {
     const uint64_t* turns;  /* DEVICE [dim / 2] turns of pair i per position, times 2^64: f / (2 pi) * 2^64 of f radians */
     const uint8_t* axis;    /* DEVICE [dim / 2] by which of a token's positions pair i turns, < n_axes; NULL: the first */

@@ -341,7 +341,7 @@ class Backend:
         """Attention of the new tokens ([n_tokens, n_heads, head_dim]) over the cache; scale defaults to head_dim ** -0.5.  (Single tokens and
         prompts may share a call, but calls of their own take less time.)
         tree: int32 [n_tokens, words], the new tokens are drafts behind the context and see those whose bits are set in their row (their
-        ancestors and themselves); 32 places a word, lowest bit first."""
+        ancestors and themselves); 32 places a word, lowest bit first.  With a tree the window hides context alone."""
         self._fits(cache, self._caches)
         self._fits(batch, self._batches)
         qs = self._rows(q, self.n_heads, "q")

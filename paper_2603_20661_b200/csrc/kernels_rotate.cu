@@ -5,7 +5,7 @@
 // twice but the positions.
 //   - Angles are kept as fractions of a turn in 64-bit whole numbers: position * turns wraps around exactly, so a position of 2^30 costs no
 //     precision that one of 2 does not, without 64-bit floating point.  cos and sin are then of an argument in [-pi, pi), where the hardware's are within
-//     2^-21 (a quarter of the error that a bf16 result of size 1 is rounded with 2^-8 times over), and take a tenth of the exact ones' instructions.
+//     2^-21 (absolute; a rounding to f16 is off by up to 2^-12 of a result of size 1, to bf16 by 2^-9), and take a tenth of the exact ones' instructions.
 //   - A lane holds 16 elements of a head as two 16-byte pieces that contain both halves of its 8 pairs: elements 8 j and dim / 2 + 8 j on (head_dim / 2 + 8 j where
 //     neighbours are paired).  So head_dim / 16 lanes share a head, a warp turns 4 or 8 heads at once, its 8 angles a lane
 //     are worked out once a token and the norm is a shuffle over 3 or 2 steps.

@@ -17,8 +17,8 @@
 //     hardware: widening to bf16 took three times the instructions); scales multiply the scores (keys) and the weights (values) in fp32.
 //     bf16 queries become f16 by a power of two per row (exact down to 2^-28 of the row's largest); weights are kept relative to twice the largest value scale of
 //     the segment when that last grew beyond it.
-//   - Measured: 12 x 61 tokens behind 16,001 of 16 bits, 32 on 8 heads of 128: 205 us, 3,900 GB/s, bound by the chain scores - weights - product of a row tile (for seconds 250 us,
-//     at the power cap); 24 x 21 behind 3,001 on average in e4m3: 98 us, bound by widening, scales and exponentials (behind 16,000: 305 us, 2,700 GB/s).
+//   - Measured: 12 x 61 tokens behind 16,001 of 16 bits, 32 on 8 heads of 128: 208 us, 3,850 GB/s, bound by the chain scores - weights - product of a row tile (from some hundred calls
+//     on end 229 to 247 us: the power cap, 1,460 MHz); 24 x 21 behind 3,001 on average in e4m3: 98 us, bound by widening, scales and exponentials (behind 16,000: 305 us, 2,700 GB/s).
 //   - Pages that no row sees are read from page 0 and their values put to zero before they are used, as is everything else of a tile that no row sees.
 #include <cuda.h>
 
