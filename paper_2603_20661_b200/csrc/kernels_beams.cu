@@ -203,29 +203,48 @@ template <int DT, bool kSkewed> __device__ __noinline__ void join_slowly(const B
     auto score = [&](uint32_t b, float x) { return score_of(a, s, seq, b, x); };
     // Too many at a bound: the best element of every chunk, then the best of these `keep` times over, its chunk looked through again for what comes behind it.
     unsigned long long* heads = a.heads + uint64_t(seq) * n;
-    auto head = [&](uint32_t i, unsigned long long last, uint32_t last_token) {       // the best element of chunk i behind (last, last_token), by a warp
+    // The best element of chunk i behind the one of logit `last` at `last_token`, by a warp; the first of all where last is infinite.  By score, not by logit: beside a large
+    // total unequal logits may have equal scores.  Scores do not fall as logits rise, and logits further apart than `near` have different ones (two roundings of
+    // 2^-53 of numbers no larger than the terms together, on either side), so 64-bit scores are worked out for unequal logits nearer than that alone.
+    auto head = [&](uint32_t i, float last, uint32_t last_token) {
         const uint32_t b = i / a.chunks, c = i - b * a.chunks;
         uint4 x[kVecs];
         Row<DT, kSkewed>(a, seq * a.beams + b).chunk(x, c, lane, a.vocab);
-        unsigned long long best = 0, key = 0;                    // (by score, not by logit: logits that differ may have equal scores beside a large total)
-        uint32_t best_token = ~0u;
+        const float terms = fabsf(__ldg(a.total + uint64_t(seq) * a.beams + b)) + fabsf(float(s.lse[b]));
+        auto near = [&](float v) { return (fabsf(v) + terms) * 0x1p-50f; };
+        const float under = last < INFINITY ? __fsub_rd(last, near(last)) : last, over = last < INFINITY ? __fadd_ru(last, near(last)) : last;
+        const unsigned long long last_y = score(b, last);
+        auto token_of = [&](int u, int e) { return c * E::kChunk + (u * 32 + lane) * E::kPer + e; };
+        uint32_t left = 0;                                       // elements behind the last one, a bit each
+        float most = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kVecs; ++u)
 #pragma unroll
             for (int e = 0; e < E::kPer; ++e) {
                 const float v = E::at(x[u], e);
-                const uint32_t token = c * E::kChunk + (u * 32 + lane) * E::kPer + e;
-                if (const unsigned long long y = score(b, v); y && before(last, last_token, y, token) && before(y, token, best, best_token)) { best = y; best_token = token; key = key_of(v, token); }
+                bool mine = v < under;
+                if (v == last) mine = token_of(u, e) > last_token;
+                else if (!mine && !(v > over)) { const unsigned long long y = score(b, v); mine = y && before(last_y, last_token, y, token_of(u, e)); }
+                left |= uint32_t(mine) << (u * E::kPer + e);
+                if (mine) most = fmaxf(most, v);
             }
+        most = unordered(__reduce_max_sync(0xffffffffu, ordered(most + 0.0f)));
+        const unsigned long long y = score(b, most);
+        const float least = __fsub_rd(most, near(most));
+        uint32_t token = ~0u;
+        float w = 0.0f;
 #pragma unroll
-        for (int k = 1; k < 32; k <<= 1) {
-            const unsigned long long z = __shfl_xor_sync(0xffffffffu, best, k), other = __shfl_xor_sync(0xffffffffu, key, k);
-            const uint32_t token = __shfl_xor_sync(0xffffffffu, best_token, k);
-            if (before(z, token, best, best_token)) { best = z; best_token = token; key = other; }
-        }
-        if (lane == 0) heads[i] = key;
+        for (int u = kVecs - 1; u >= 0; --u)
+#pragma unroll
+            for (int e = E::kPer - 1; e >= 0; --e) {
+                const float v = E::at(x[u], e);
+                if (left >> (u * E::kPer + e) & 1u && !(v < least) && (v == most || score(b, v) == y)) { token = token_of(u, e); w = v; }
+            }
+        const uint32_t first = __reduce_min_sync(0xffffffffu, token);
+        if (first == ~0u || y == 0) { if (lane == 0) heads[i] = 0; }
+        else if (token == first) heads[i] = key_of(w, token);
     };
-    for (uint32_t i = warp; i < n; i += kWarps) head(i, ~0ull, 0);
+    for (uint32_t i = warp; i < n; i += kWarps) head(i, INFINITY, 0);
     for (uint32_t r = 0; r < a.keep; ++r) {
         __syncthreads();                                                                         // (orders the block's writes to the heads too)
         unsigned long long best = 0, id = ~0ull;
@@ -239,7 +258,9 @@ template <int DT, bool kSkewed> __device__ __noinline__ void join_slowly(const B
         if (tid == 0) put(a, seq, r, w.y, w.id);
         if (w.y && warp == 0) {
             const uint32_t b = uint32_t(w.id >> 32), token = uint32_t(w.id), i = b * a.chunks + token / E::kChunk;
-            head(i, w.y, token);
+            const unsigned long long k = __ldcg(heads + i);
+            __syncwarp();
+            head(i, unordered(uint32_t(k >> 32)), token);
         }
     }
 }
